@@ -1,0 +1,483 @@
+"""Training a block of the MatMul-free model: the operators around the layer's
+own backward, as measurable cases.
+
+``run`` computes an operator in its plain form, elementary torch operations,
+or, where ``own`` is true, through the framework's entry points.  ``exact``
+gives the same values in 64 bits.
+
+Kinds of case:
+
+  add      residual addition + RMSNorm + int8 quantisation of each token (the
+           branch's output joins the residual stream and the next mixer's
+           activations are quantised): s, q, a_scale, q_rowsum, rstd
+  add_bwd  its backward: the gradient of the sum from the gradient of the
+           quantised activations (straight through the quantiser) and of the
+           residual stream, the same in bfloat16, and dgamma
+  glu      the gate's gradients of the GLU channel mixer: both projections
+           again from the int8 activations and the packed ternary weights,
+           the activation's and the product's derivative, [dgate | dup] in
+           bfloat16 as the layer's backward takes it
+  scan     the MLGRU recurrence in training form, forward and backward: from
+           the pre-activations z of the three gates to o', then from the
+           gradient of o' to that of z in bfloat16, of the first state and of
+           the forget gate's lower bound
+  clip     the global norm of a set of gradients, and the set scaled to it
+
+q is an array of integers that the contraction takes as integers, so it is
+returned as it is; gradients are returned whole.
+"""
+import math
+
+import torch
+
+own = False
+
+F32, F64, BF16 = torch.float32, torch.float64, torch.bfloat16
+
+
+def listed():
+    return [
+        # One token joining the residual stream in generation (1.3B width):
+        # pure latency.
+        {"name": "add_m1", "kind": "add", "M": 1, "K": 2048, "f32": False, "branch_f32": True, "gamma": True},
+        # A running batch at the 13B width, float32 residual stream.
+        {"name": "add_m45", "kind": "add", "M": 45, "K": 5120, "f32": True, "branch_f32": True, "gamma": True},
+        # Prefill at the 13B width, the residual stream in bfloat16.
+        {"name": "add_prefill", "kind": "add", "M": 16384, "K": 5120, "f32": False, "branch_f32": True,
+         "gamma": True},
+        # Backward over the 1.3B model's training batch.
+        {"name": "add_bwd_train", "kind": "add_bwd", "M": 8192, "K": 2048, "f32": False, "dy_f32": True,
+         "gamma": True, "res": True},
+        # The same with nothing aligned: float32 stream, bfloat16 gradient.
+        {"name": "add_bwd_ragged", "kind": "add_bwd", "M": 1937, "K": 2288, "f32": True, "dy_f32": False,
+         "gamma": True, "res": True},
+        # A short ragged batch through a small model's channel mixer.
+        {"name": "glu_ragged", "kind": "glu", "M": 357, "K": 1040, "L": 2832, "dp_f32": False},
+        # The 1.3B model's channel mixer over a training batch, the gradient
+        # in float32 as the down-projection's backward leaves it.
+        {"name": "glu_train", "kind": "glu", "M": 8192, "K": 2048, "L": 5632, "dp_f32": True},
+        # A few short sequences of a small model.
+        {"name": "scan_ragged", "kind": "scan", "B": 3, "T": 357, "d": 1040, "lb": True, "h0": True,
+         "do_f32": False},
+        # Four sequences of the paper's length at the 1.3B width.
+        {"name": "scan_train", "kind": "scan", "B": 4, "T": 2048, "d": 2048, "lb": True, "h0": False,
+         "do_f32": True},
+        # One long sequence.
+        {"name": "scan_long", "kind": "scan", "B": 1, "T": 16384, "d": 2048, "lb": True, "h0": True,
+         "do_f32": True},
+        # The gradients of a model's norm scales and biases: many small
+        # tensors, odd sizes among them.
+        {"name": "clip_vectors", "kind": "clip", "layers": 12, "d": 2048, "L": 0, "odd": 3, "bf16": False,
+         "max_norm": 1.0},
+        # The gradients of four layers of the 1.3B model.
+        {"name": "clip_layers", "kind": "clip", "layers": 4, "d": 2048, "L": 5632, "odd": 0, "bf16": False,
+         "max_norm": 1.0},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _log16(rng, lo, hi):
+    return max(lo, min(hi, 16 * int(round(_log(rng, lo, hi) / 16))))
+
+
+def draw(rng):
+    """One case of the same ranges: sizes spread over their logarithms, K, d
+    and L multiples of 16 (what the format needs), everything else any."""
+    kind = rng.choice(["add", "add", "add_bwd", "glu", "scan", "scan", "clip"])
+    if kind == "add":
+        return {"kind": kind, "M": _log(rng, 1, 16384), "K": _log16(rng, 256, 5120), "f32": rng.random() < 0.4,
+                "branch_f32": rng.random() < 0.7, "gamma": rng.random() < 0.8}
+    if kind == "add_bwd":
+        return {"kind": kind, "M": _log(rng, 64, 8192), "K": _log16(rng, 256, 5120), "f32": rng.random() < 0.4,
+                "dy_f32": rng.random() < 0.6, "gamma": rng.random() < 0.8, "res": rng.random() < 0.8}
+    if kind == "glu":
+        K = _log16(rng, 256, 2048)
+        return {"kind": kind, "M": _log(rng, 16, 8192), "K": K, "L": _log16(rng, K, 5632),
+                "dp_f32": rng.random() < 0.5}
+    if kind == "scan":
+        d = _log16(rng, 256, 4096)
+        B = rng.choice([1, 1, 2, 3, 4, 7, 16])
+        most = min(16384, 16384 * 2048 // (B * d))
+        return {"kind": kind, "B": B, "T": _log(rng, 1 if rng.random() < 0.2 else 64, most), "d": d,
+                "lb": rng.random() < 0.8, "h0": rng.random() < 0.6, "do_f32": rng.random() < 0.6}
+    d = _log16(rng, 256, 2048)
+    return {"kind": kind, "layers": rng.randint(1, 4), "d": d, "L": _log16(rng, d, 5632) if rng.random() < 0.7 else 0,
+            "odd": rng.randint(0, 5), "bf16": rng.random() < 0.4, "max_norm": rng.choice([0.5, 1.0, 1.0, 1e6])}
+
+
+# ---------------------------------------------------------------------------
+# inputs, from the seed alone
+# ---------------------------------------------------------------------------
+
+class _Draw:
+    def __init__(self, seed):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(240602528 + int(seed))
+
+    def normal(self, *shape, scale=1.0, dtype=F32):
+        t = torch.randn(shape, generator=self.g, device="cuda", dtype=F32)
+        return t.mul_(scale).to(dtype) if scale != 1.0 else t.to(dtype)
+
+    def uniform(self, lo, hi, *shape):
+        return torch.rand(shape, generator=self.g, device="cuda", dtype=F32).mul_(hi - lo).add_(lo)
+
+
+def _kind(f32):
+    return F32 if f32 else BF16
+
+
+def _empty(*shape, dtype=F32):
+    return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _shift():
+    """Bit of the code of k = 16 j + e within word j: 8 (e % 4) + 2 (e // 4)."""
+    e = torch.arange(16, device="cuda", dtype=torch.int32)
+    return 8 * (e % 4) + 2 * (e // 4)
+
+
+def _pack(t):
+    """t [N][K] in {-1, 0, 1} -> the packed words [K/16][N]."""
+    N, K = t.shape
+    c = (t + 1).to(torch.int64).reshape(N, K // 16, 16)
+    w = (c << _shift().to(torch.int64)).sum(2)
+    return torch.where(w >= 2 ** 31, w - 2 ** 32, w).to(torch.int32).t().contiguous()
+
+
+def _interleave(Wg, Wu):
+    """Blocks of 16 gate and 16 up columns in turn, [K/16][2L]."""
+    J, L = Wg.shape
+    return torch.stack([Wg.reshape(J, L // 16, 16), Wu.reshape(J, L // 16, 16)], 2).reshape(J, 2 * L).contiguous()
+
+
+def _ternary(d, L, K):
+    W = d.normal(L, K, scale=0.02)
+    s = W.double().abs().mean()
+    return (W.double() / s).round_().clamp_(-1, 1), s.float()
+
+
+def _inputs_add(case, seed):
+    d = _Draw(seed)
+    M, K = case["M"], case["K"]
+    return {"x": d.normal(M, K, scale=2.0, dtype=_kind(case["f32"])),
+            "branch": d.normal(M, K, dtype=_kind(case["branch_f32"])),
+            "gamma": d.uniform(0.5, 1.5, K) if case["gamma"] else None}
+
+
+def _inputs_add_bwd(case, seed):
+    d = _Draw(seed)
+    M, K = case["M"], case["K"]
+    s = d.normal(M, K, scale=2.0, dtype=_kind(case["f32"]))
+    return {"s": s, "dy": d.normal(M, K, dtype=_kind(case["dy_f32"])),
+            "ds_out": d.normal(M, K) if case["res"] else None,
+            "gamma": d.uniform(0.5, 1.5, K) if case["gamma"] else None,
+            "rstd": (s.double().square().mean(1) + 1e-6).rsqrt().float()}
+
+
+def _inputs_glu(case, seed):
+    d = _Draw(seed)
+    M, K, L = case["M"], case["K"], case["L"]
+    x = d.normal(M, K)
+    a = x.abs().amax(1)
+    q = (x * (127.0 / a)[:, None]).round_().to(torch.int8)
+    tg, sg = _ternary(d, L, K)
+    tu, su = _ternary(d, L, K)
+    return {"q": q, "a_scale": a / 127.0, "rowsum": q.sum(1, dtype=torch.int32), "tg": tg, "tu": tu,
+            "w_scales": torch.stack([sg, su]), "dp": d.normal(M, L, dtype=_kind(case["dp_f32"]))}
+
+
+def _inputs_scan(case, seed):
+    g = _Draw(seed)
+    B, T, d = case["B"], case["T"], case["d"]
+    return {"z": g.normal(B * T, 3 * d), "lb": g.uniform(0.0, 0.95, d) if case["lb"] else None,
+            "h0": g.normal(B, d, scale=0.5) if case["h0"] else None,
+            "do": g.normal(B * T, d, dtype=_kind(case["do_f32"])), "dh": g.normal(B, d)}
+
+
+def _clip_shapes(case):
+    d, L = case["d"], case["L"]
+    layer = [(3 * d,), (d,), (d,), (d,)]
+    if L:
+        layer += [(3 * d, d), (d, d), (2 * L, d), (d, L), (L,)]
+    return layer * case["layers"] + [(2 * i + 1,) if i % 2 else (d - i - 1, 3) for i in range(case["odd"])]
+
+
+def _inputs_clip(case, seed):
+    g = _Draw(seed)
+    # matrices in bfloat16 where gradients are kept so; vectors always in float32
+    return [g.normal(*s, scale=0.05, dtype=BF16 if case["bf16"] and len(s) > 1 else F32) for s in _clip_shapes(case)]
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    if kind == "add":
+        M, K = case["M"], case["K"]
+        v = _inputs_add(case, seed)
+        v.update(kind=kind, s=_empty(M, K, dtype=v["x"].dtype), q=_empty(M, K, dtype=torch.int8), a_scale=_empty(M),
+                 rowsum=_empty(M, dtype=torch.int32), rstd=_empty(M))
+        return v
+    if kind == "add_bwd":
+        M, K = case["M"], case["K"]
+        v = _inputs_add_bwd(case, seed)
+        v.update(kind=kind, ds=_empty(M, K), ds_bf16=_empty(M, K, dtype=BF16), dgamma=_empty(K))
+        return v
+    if kind == "glu":
+        v = _inputs_glu(case, seed)
+        v.update(kind=kind, W=_interleave(_pack(v.pop("tg")), _pack(v.pop("tu"))),
+                 dgu=_empty(case["M"], 2 * case["L"], dtype=BF16))
+        return v
+    if kind == "scan":
+        B, T, d = case["B"], case["T"], case["d"]
+        v = _inputs_scan(case, seed)
+        v.update(kind=kind, B=B, T=T, o=_empty(B * T, d), h=_empty(B, d), dz=_empty(B * T, 3 * d, dtype=BF16),
+                 dh0=_empty(B, d), dlb=_empty(d) if case["lb"] else None)
+        return v
+    grads = _inputs_clip(case, seed)
+    return {"kind": kind, "grads": grads, "outs": [torch.empty_like(g) for g in grads], "norm": _empty(1),
+            "max_norm": case["max_norm"]}
+
+
+# ---------------------------------------------------------------------------
+# one pass, plain
+# ---------------------------------------------------------------------------
+
+def _plain_add(v):
+    s = (v["x"].float() + v["branch"].float()).to(v["x"].dtype)
+    f = s.float()
+    # the row's statistic in 64 bits, rounded once, and the two quotients
+    # correctly rounded: q sits on borders between integers
+    r = torch.sqrt(f.double().square().sum(1) / f.shape[1] + 1e-6).reciprocal_().float()
+    y = f * r[:, None]
+    if v["gamma"] is not None:
+        y = y * v["gamma"]
+    a = y.abs().amax(1).clamp_min(1e-5)
+    n = torch.full_like(a, 127.0, dtype=F64)
+    q = (y * (n / a.double()).float()[:, None]).round_().clamp_(-128, 127).to(torch.int8)
+    return {"s": s, "q": q, "a_scale": (a.double() / n).float(), "rowsum": q.sum(1, dtype=torch.int32), "rstd": r}
+
+
+def _plain_add_bwd(v):
+    s, dy, r = v["s"].float(), v["dy"].float(), v["rstd"][:, None]
+    g = dy if v["gamma"] is None else dy * v["gamma"]
+    t = (g.double() * s).sum(1, keepdim=True)
+    ds = r * g - (r.double() ** 3 * t / s.shape[1]).float() * s
+    if v["ds_out"] is not None:
+        ds = ds + v["ds_out"]
+    return {"ds": ds, "ds_bf16": ds.to(BF16), "dgamma": (dy * s * r).sum(0, dtype=F64).float()}
+
+
+def _unpack(W):
+    """The interleaved words [K/16][2L] -> gate and up, [L][K] float32 each."""
+    J, N = W.shape
+    t = ((W.t().reshape(N // 32, 2, 16, J, 1) >> _shift()) & 3).float() - 1.0
+    return t[:, 0].reshape(N // 2, 16 * J), t[:, 1].reshape(N // 2, 16 * J)
+
+
+def _plain_glu(v):
+    tg, tu = _unpack(v["W"])
+    q, dp = v["q"].float(), v["dp"].float()
+    g = (q @ tg.t()) * (v["a_scale"] * v["w_scales"][0])[:, None]
+    u = (q @ tu.t()) * (v["a_scale"] * v["w_scales"][1])[:, None]
+    s = torch.reciprocal(1.0 + torch.exp(-g))
+    return {"dgu": torch.cat([dp * u * s * (1.0 + g * (1.0 - s)), dp * g * s], 1).to(BF16)}
+
+
+def _sigmoid(z):
+    return torch.reciprocal(1.0 + torch.exp(-z))
+
+
+def _scan(a, b):
+    """h_t = a_t h_{t-1} + b_t along dimension 1 from 0, by doubling: after a
+    step of k, element t is the map of the 2k tokens that end at t."""
+    a, b, k = a.clone(), b.clone(), 1
+    while k < a.shape[1]:
+        b[:, k:] = a[:, k:] * b[:, :-k] + b[:, k:]
+        a[:, k:] = a[:, k:] * a[:, :-k]
+        k *= 2
+    return b
+
+
+def _plain_scan(v):
+    B, T, d = v["B"], v["T"], v["o"].shape[1]
+    z = v["z"].reshape(B, T, 3, d)
+    zc, zg = z[:, :, 1], z[:, :, 2]
+    sf, sc = _sigmoid(z[:, :, 0]), _sigmoid(zc)
+    lb = torch.zeros(d, device="cuda") if v["lb"] is None else v["lb"]
+    h0 = torch.zeros((B, d), device="cuda") if v["h0"] is None else v["h0"]
+    f, c = lb + (1.0 - lb) * sf, zc * sc
+    b = (1.0 - f) * c
+    b[:, 0] += f[:, 0] * h0
+    h = _scan(f, b)
+    sh = _sigmoid(h)
+    do = v["do"].float().reshape(B, T, d)
+    e = do * zg * sh * (1.0 - sh)
+    e[:, -1] += v["dh"]
+    # dh_t = e_t + f_{t+1} dh_{t+1}
+    back = torch.cat([torch.zeros_like(f[:, :1]), f[:, 1:].flip(1)], 1)
+    dh = _scan(back, e.flip(1)).flip(1)
+    df = dh * (torch.cat([h0[:, None], h[:, :-1]], 1) - c)
+    dz = torch.stack([df * ((1.0 - lb) * sf * (1.0 - sf)), dh * (1.0 - f) * (sc * (1.0 + zc * (1.0 - sc))), do * sh], 2)
+    out = {"o": (zg * sh).reshape(B * T, d), "h": h[:, -1].contiguous(), "dz": dz.reshape(B * T, 3 * d).to(BF16),
+           "dh0": f[:, 0] * dh[:, 0]}
+    if v["lb"] is not None:
+        out["dlb"] = (df * (1.0 - sf)).sum((0, 1), dtype=F64).float()
+    return out
+
+
+def _plain_clip(v):
+    total = torch.stack([g.float().square().sum(dtype=F64) for g in v["grads"]]).sum()
+    norm = total.sqrt().float()
+    c = (v["max_norm"] / (norm + 1e-6)).clamp(max=1.0)
+    return {"norm": norm.reshape(1), "grads": [(g.float() * c).to(g.dtype) for g in v["grads"]]}
+
+
+# ---------------------------------------------------------------------------
+# one pass through the framework
+# ---------------------------------------------------------------------------
+
+def _kept(v, bytes_of):
+    """The program's workspace, made at its first call and kept."""
+    if "ws" not in v:
+        v["ws"] = torch.empty(max(int(bytes_of()), 256), dtype=torch.uint8, device="cuda")
+    return v["ws"]
+
+
+def _run_own(v):
+    import paper_2406_02528_amd as mmf
+    kind = v["kind"]
+    if kind == "add":
+        mmf.mmf_add_act_quant(v["x"], v["branch"], v["gamma"], v["s"], v["q"], v["a_scale"], v["rowsum"], v["rstd"])
+        return {k: v[k] for k in ("s", "q", "a_scale", "rowsum", "rstd")}
+    if kind == "add_bwd":
+        ws = _kept(v, lambda: mmf.mmf_add_act_quant_bwd_workspace_bytes(*v["s"].shape))
+        mmf.mmf_add_act_quant_bwd(v["dy"], v["ds_out"], v["s"], v["gamma"], v["rstd"], v["ds"], v["ds_bf16"],
+                                  v["dgamma"], ws)
+        return {k: v[k] for k in ("ds", "ds_bf16", "dgamma")}
+    if kind == "glu":
+        mmf.mmf_glu_gate_bwd(v["q"], v["a_scale"], v["rowsum"], v["W"], v["w_scales"], v["dp"], v["dgu"])
+        return {"dgu": v["dgu"]}
+    if kind == "scan":
+        B, T, d = v["B"], v["T"], v["o"].shape[1]
+        ws = _kept(v, lambda: mmf.mmf_mlgru_scan_bwd_workspace_bytes(B, T, d))
+        mmf.mmf_mlgru_train_scan(v["z"], B, T, v["lb"], v["h0"], v["o"], v["h"], ws)
+        mmf.mmf_mlgru_scan_bwd(v["z"], B, T, v["lb"], v["h0"], v["do"], v["dh"], v["dz"], v["dh0"], v["dlb"], ws)
+        out = {k: v[k] for k in ("o", "h", "dz", "dh0")}
+        if v["dlb"] is not None:
+            out["dlb"] = v["dlb"]
+        return out
+    ws = _kept(v, lambda: mmf.mmf_grad_norm_workspace_bytes([g.numel() for g in v["grads"]]))
+    mmf.mmf_grad_norm(v["grads"], v["norm"], ws)
+    mmf.mmf_grad_clip(v["grads"], v["norm"], v["max_norm"], v["outs"])
+    return {"norm": v["norm"], "grads": v["outs"]}
+
+
+_PLAIN = {"add": _plain_add, "add_bwd": _plain_add_bwd, "glu": _plain_glu, "scan": _plain_scan, "clip": _plain_clip}
+
+
+def run(state):
+    return _run_own(state) if own else _PLAIN[state["kind"]](state)
+
+
+def work(case):
+    kind = case["kind"]
+    size = lambda f32: 4 if f32 else 2  # noqa: E731
+    if kind == "add":
+        M, K, xb = case["M"], case["K"], size(case["f32"])
+        return {"bytes": M * K * (2 * xb + size(case["branch_f32"]) + 1) + 12 * M + (4 * K if case["gamma"] else 0),
+                "flops": 8 * M * K}
+    if kind == "add_bwd":
+        M, K = case["M"], case["K"]
+        return {"bytes": M * K * (size(case["f32"]) + size(case["dy_f32"]) + (4 if case["res"] else 0) + 4 + 2)
+                + 4 * M + (4 * K if case["gamma"] else 0) + 4 * K, "flops": 10 * M * K}
+    if kind == "glu":
+        M, K, L = case["M"], case["K"], case["L"]
+        return {"bytes": M * K + 8 * M + K * L // 2 + M * L * (size(case["dp_f32"]) + 4), "flops": 4 * M * K * L}
+    if kind == "scan":
+        M, d, B = case["B"] * case["T"], case["d"], case["B"]
+        return {"bytes": M * d * (12 + 4 + 12 + size(case["do_f32"]) + 6) + B * d * (12 + (4 if case["h0"] else 0))
+                + (8 * d if case["lb"] else 0), "flops": 60 * M * d}
+    n = [(math.prod(s), 2 if case["bf16"] and len(s) > 1 else 4) for s in _clip_shapes(case)]
+    return {"bytes": sum(3 * c * b for c, b in n) + 4, "flops": 3 * sum(c for c, _ in n)}
+
+
+# ---------------------------------------------------------------------------
+# the same values in 64 bits
+# ---------------------------------------------------------------------------
+
+def _exact_add(case, seed):
+    v = _inputs_add(case, seed)
+    # the stored sum is what is normalised: its rounding to the stream's type
+    # is part of the definition
+    s = (v["x"].double() + v["branch"].double()).float().to(v["x"].dtype).double()
+    var = torch.linalg.vector_norm(s, dim=1) ** 2 / case["K"]
+    r = 1.0 / torch.sqrt(var + 1e-6)
+    y = s * r.unsqueeze(1) * (1.0 if v["gamma"] is None else v["gamma"].double())
+    a = torch.clamp(torch.linalg.vector_norm(y, ord=math.inf, dim=1), min=1e-5)
+    return {"s": s, "q": None, "a_scale": a / 127.0, "rowsum": None, "rstd": r}
+
+
+def _exact_add_bwd(case, seed):
+    v = _inputs_add_bwd(case, seed)
+    s, dy, r = v["s"].double(), v["dy"].double(), v["rstd"].double().unsqueeze(1)
+    n = s * r
+    g = dy if v["gamma"] is None else dy * v["gamma"].double()
+    ds = r * (g - n * torch.mean(g * n, dim=1, keepdim=True))
+    if v["ds_out"] is not None:
+        ds += v["ds_out"].double()
+    return {"ds": ds, "ds_bf16": ds, "dgamma": torch.einsum("mk,mk->k", dy, n)}
+
+
+def _exact_glu(case, seed):
+    v = _inputs_glu(case, seed)
+    x = v["q"].double() * v["a_scale"].double().unsqueeze(1)
+    g = torch.mm(x, v["tg"].t() * v["w_scales"][0].double())
+    u = torch.mm(x, v["tu"].t() * v["w_scales"][1].double())
+    dp, s = v["dp"].double(), torch.sigmoid(g)
+    silu = g * s
+    return {"dgu": torch.cat([dp * u * (s + silu - silu * s), dp * silu], dim=1)}
+
+
+def _exact_scan(case, seed):
+    v = _inputs_scan(case, seed)
+    B, T, d = case["B"], case["T"], case["d"]
+    z = v["z"].double().reshape(B, T, 3 * d)
+    lb = v["lb"].double() if case["lb"] else torch.zeros(d, dtype=F64, device="cuda")
+    h0 = v["h0"].double() if case["h0"] else torch.zeros((B, d), dtype=F64, device="cuda")
+    sf, c = torch.sigmoid(z[..., :d]), z[..., d:2 * d] * torch.sigmoid(z[..., d:2 * d])
+    f = lb + (1 - lb) * sf
+    h = torch.empty((B, T + 1, d), dtype=F64, device="cuda")
+    h[:, 0] = h0
+    for t in range(T):
+        h[:, t + 1] = torch.lerp(c[:, t], h[:, t], f[:, t])
+    sh = torch.sigmoid(h[:, 1:])
+    do = v["do"].double().reshape(B, T, d)
+    dh = do * z[..., 2 * d:] * sh * (1 - sh)
+    run = v["dh"].double()
+    for t in range(T - 1, -1, -1):
+        run = dh[:, t] + run
+        dh[:, t] = run
+        run = run * f[:, t]
+    df = dh * (h[:, :-1] - c)
+    sc = torch.sigmoid(z[..., d:2 * d])
+    dz = torch.cat([df * (1 - lb) * sf * (1 - sf), dh * (1 - f) * (sc + c * (1 - sc)), do * sh], dim=2)
+    out = {"o": (z[..., 2 * d:] * sh).reshape(B * T, d), "h": h[:, T].contiguous(), "dz": dz.reshape(B * T, 3 * d),
+           "dh0": run}
+    if case["lb"]:
+        out["dlb"] = torch.einsum("btd,btd->d", df, 1 - sf)
+    return out
+
+
+def _exact_clip(case, seed):
+    grads = [g.double() for g in _inputs_clip(case, seed)]
+    norm = math.sqrt(sum(float(torch.dot(g.flatten(), g.flatten())) for g in grads))
+    c = min(1.0, case["max_norm"] / (norm + 1e-6))
+    return {"norm": torch.tensor([norm], dtype=F64, device="cuda"), "grads": [g * c for g in grads]}
+
+
+def exact(case, seed):
+    kind = case["kind"]
+    return {"add": _exact_add, "add_bwd": _exact_add_bwd, "glu": _exact_glu, "scan": _exact_scan,
+            "clip": _exact_clip}[kind](case, seed)
