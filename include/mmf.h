@@ -129,6 +129,49 @@ int mmf_act_quant_ex(const void *x, int x_is_f32, const float *gamma, int8_t *q,
                      hipStream_t stream);
 
 /*
+ * Residual addition and the quantisation of the sum in one pass (the step
+ * between two mixers of a block: the branch's output joins the residual
+ * stream, and the stream's new value is the next layer's input).  For each
+ * token m:
+ *   s = x + branch                  (fp32, stored in the type of x)
+ *   r, q, a_scale, q_rowsum         as mmf_act_quant_ex of the stored s
+ * the same bits as an addition followed by that call.  x and s [M][K] bf16
+ * bits or float32 (x_is_f32), branch [M][K] bf16 bits or float32
+ * (branch_is_f32; NULL: no branch, s = x, and s may be NULL, not stored);
+ * gamma [K] or NULL; q [M][K], a_scale [M], q_rowsum [M] (or NULL) out; rstd
+ * [M] out (or NULL), r = 1/sqrt(mean s^2 + 1e-6), as the backwards take it.
+ * s may be the same array as x (the stream updated in place); no other
+ * overlap is allowed.
+ */
+int mmf_add_act_quant(const void *x, int x_is_f32, const void *branch, int branch_is_f32,
+                      const float *gamma, void *s, int8_t *q, float *a_scale,
+                      int32_t *q_rowsum, float *rstd, int64_t M, int64_t K,
+                      hipStream_t stream);
+
+/*
+ * Its backward (the straight-through estimator passes the gradient through
+ * the quantiser unchanged), for activations y = (s r) gamma that other
+ * operators than the layer's own backward consume: from the gradient dY of y
+ * and the gradient ds_out that reaches s through the residual stream,
+ *   ds = r g - (r^3 t / K) s + ds_out,  g = gamma (.) dY,  t = sum_k g_k s_k
+ *   dgamma = sum over tokens of dY (.) s r
+ * ds is the gradient of x and of branch alike.  dY [M][K] bf16 bits or float32
+ * (dy_is_f32); ds_out [M][K] float32 or NULL (zero); s [M][K] bf16 bits or
+ * float32 (s_is_f32) and rstd [M] from the forward; gamma [K] or NULL (ones).
+ * Outputs: ds [M][K] float32 (may be the same array as ds_out); ds_bf16
+ * [M][K], ds rounded to bf16 as mmf_bitlinear_bwd takes the gradient of its
+ * output (NULL: not stored); dgamma [K] float32 (NULL: not computed).  t and
+ * dgamma are summed in fp64, in a fixed order.  M == 0 is a no-op.  Workspace
+ * (needed for dgamma only; 256-byte aligned, MMF_ERR_WORKSPACE), or NULL: then
+ * allocated stream-ordered on `stream` and freed there.
+ */
+size_t mmf_add_act_quant_bwd_workspace_bytes(int64_t M, int64_t K);
+int mmf_add_act_quant_bwd(const void *dY, int dy_is_f32, const float *ds_out, const void *s,
+                          int s_is_f32, const float *gamma, const float *rstd, float *ds,
+                          uint16_t *ds_bf16, float *dgamma, int64_t M, int64_t K,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * The fused BitLinear forward (Algorithm 1, forward_pass, bias 0):
  *   y[m][n] = a_scale[m] * w_scale * sum_k q[m][k] t[n][k]
  * with q, a_scale from the act-quant step above and t from Wpacked.  The

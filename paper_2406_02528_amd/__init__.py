@@ -47,6 +47,10 @@ _SIGNATURES = {
     "mmf_act_quant": ([_P, _P, _P, _P, _I64, _I64, _P], ctypes.c_int),
     "mmf_act_quant_f32": ([_P, _P, _P, _P, _I64, _I64, _P], ctypes.c_int),
     "mmf_act_quant_ex": ([_P, ctypes.c_int, _P, _P, _P, _P, _I64, _I64, _P], ctypes.c_int),
+    "mmf_add_act_quant": ([_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _I64, _I64, _P], ctypes.c_int),
+    "mmf_add_act_quant_bwd_workspace_bytes": ([_I64, _I64], _SZ),
+    "mmf_add_act_quant_bwd": ([_P, ctypes.c_int, _P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _I64, _I64, _P, _SZ, _P],
+                              ctypes.c_int),
     "mmf_bitlinear_fwd": ([_P, _P, _P, _P, _P, _I64, _I64, _I64, _P], ctypes.c_int),
     "mmf_bitlinear_fwd_f32": ([_P, _P, _P, _P, _P, _I64, _I64, _I64, _P], ctypes.c_int),
     "mmf_bitlinear_workspace_bytes": ([_I64, _I64], _SZ),
@@ -132,6 +136,13 @@ def _need(t: torch.Tensor, name: str, dtype, shape) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+def _need_here(t: torch.Tensor, name: str, dtype, shape) -> None:
+    """_need, and on the current device: the call is enqueued there."""
+    _need(t, name, dtype, shape)
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current device, cuda:{torch.cuda.current_device()}")
+
+
 def _x_kind(x: torch.Tensor) -> bool:
     """True for float32 activations, False for bfloat16."""
     if x.dtype == torch.float32:
@@ -139,6 +150,15 @@ def _x_kind(x: torch.Tensor) -> bool:
     if x.dtype == torch.bfloat16:
         return False
     raise TypeError(f"x must be bfloat16 or float32, got {x.dtype}")
+
+
+def _kind(t: torch.Tensor, name: str) -> bool:
+    """_x_kind of a tensor with another name."""
+    if t.dtype == torch.float32:
+        return True
+    if t.dtype == torch.bfloat16:
+        return False
+    raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
 
 
 def mmf_version() -> int:
@@ -206,6 +226,65 @@ def mmf_act_quant_ex(x: torch.Tensor, gamma: torch.Tensor | None, q: torch.Tenso
                      a_scale: torch.Tensor, q_rowsum: torch.Tensor | None, stream=None) -> None:
     """mmf_act_quant with the row sums q_rowsum i32 [M] (None: not written)."""
     mmf_act_quant(x, gamma, q, a_scale, q_rowsum, stream)
+
+
+def mmf_add_act_quant(x: torch.Tensor, branch: torch.Tensor | None, gamma: torch.Tensor | None,
+                      s: torch.Tensor | None, q: torch.Tensor, a_scale: torch.Tensor,
+                      q_rowsum: torch.Tensor | None = None, rstd: torch.Tensor | None = None,
+                      stream=None) -> None:
+    """s = x + branch (bf16/f32 [M][K], in the type of x; may be x) and its
+    quantisation as mmf_act_quant gives it: q int8 [M][K], a_scale f32 [M],
+    q_rowsum i32 [M], rstd f32 [M].  branch bf16/f32 [M][K], or None: s = x,
+    which may be None."""
+    M, K = x.shape
+    is_f32 = _x_kind(x)
+    _need_here(x, "x", x.dtype, (M, K))
+    branch_f32 = False
+    if branch is not None:
+        branch_f32 = _kind(branch, "branch")
+        _need_here(branch, "branch", branch.dtype, (M, K))
+    if gamma is not None:
+        _need_here(gamma, "gamma", torch.float32, (K,))
+    if s is not None or branch is not None:
+        _need_here(s, "s", x.dtype, (M, K))
+    _need_here(q, "q", torch.int8, (M, K))
+    _need_here(a_scale, "a_scale", torch.float32, (M,))
+    if q_rowsum is not None:
+        _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
+    if rstd is not None:
+        _need_here(rstd, "rstd", torch.float32, (M,))
+    _check(_lib.mmf_add_act_quant(_ptr(x), is_f32, _ptr(branch), branch_f32, _ptr(gamma), _ptr(s), _ptr(q),
+                                  _ptr(a_scale), _ptr(q_rowsum), _ptr(rstd), M, K, _stream(stream)))
+
+
+def mmf_add_act_quant_bwd_workspace_bytes(M: int, K: int) -> int:
+    return int(_lib.mmf_add_act_quant_bwd_workspace_bytes(M, K))
+
+
+def mmf_add_act_quant_bwd(dY: torch.Tensor, ds_out: torch.Tensor | None, s: torch.Tensor,
+                          gamma: torch.Tensor | None, rstd: torch.Tensor, ds: torch.Tensor,
+                          ds_bf16: torch.Tensor | None, dgamma: torch.Tensor | None,
+                          workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Backward: ds f32 [M][K] (may be ds_out), the same in bf16 (or None) and
+    dgamma f32 [K] (or None) from dY bf16/f32 [M][K], the residual stream's
+    gradient ds_out f32 [M][K] (or None) and the forward's s and rstd."""
+    M, K = s.shape
+    s_f32, dy_f32 = _kind(s, "s"), _kind(dY, "dY")
+    _need_here(dY, "dY", dY.dtype, (M, K))
+    if ds_out is not None:
+        _need_here(ds_out, "ds_out", torch.float32, (M, K))
+    _need_here(s, "s", s.dtype, (M, K))
+    if gamma is not None:
+        _need_here(gamma, "gamma", torch.float32, (K,))
+    _need_here(rstd, "rstd", torch.float32, (M,))
+    _need_here(ds, "ds", torch.float32, (M, K))
+    if ds_bf16 is not None:
+        _need_here(ds_bf16, "ds_bf16", torch.bfloat16, (M, K))
+    if dgamma is not None:
+        _need_here(dgamma, "dgamma", torch.float32, (K,))
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_add_act_quant_bwd(_ptr(dY), dy_f32, _ptr(ds_out), _ptr(s), s_f32, _ptr(gamma), _ptr(rstd),
+                                      _ptr(ds), _ptr(ds_bf16), _ptr(dgamma), M, K, wp, wn, _stream(stream)))
 
 
 def mmf_bitlinear_fwd(x: torch.Tensor, gamma: torch.Tensor | None, Wpacked: torch.Tensor,
@@ -571,6 +650,17 @@ def bitlinear(x: torch.Tensor, gamma: torch.Tensor | None, Wpacked: torch.Tensor
     y = torch.empty((x.shape[0], Wpacked.shape[1]), dtype=torch.float32, device=x.device)
     mmf_bitlinear_fwd(x, gamma, Wpacked, w_scale, y, stream)
     return y
+
+
+def add_act_quant(x: torch.Tensor, branch: torch.Tensor | None, gamma: torch.Tensor | None, stream=None):
+    """Returns (s in the type of x [M][K], q int8 [M][K], a_scale float32 [M],
+    q_rowsum int32 [M], rstd float32 [M])."""
+    M, K = x.shape
+    s, q = torch.empty_like(x), torch.empty((M, K), dtype=torch.int8, device=x.device)
+    a_scale, rstd = (torch.empty((M,), dtype=torch.float32, device=x.device) for _ in range(2))
+    q_rowsum = torch.empty((M,), dtype=torch.int32, device=x.device)
+    mmf_add_act_quant(x, branch, gamma, s, q, a_scale, q_rowsum, rstd, stream)
+    return s, q, a_scale, q_rowsum, rstd
 
 
 def glu_pack(Wg_packed: torch.Tensor, Wu_packed: torch.Tensor, stream=None) -> torch.Tensor:

@@ -1,0 +1,455 @@
+// Residual addition + RMSNorm + per-token absmax int8 quantisation, and its
+// backward.
+//
+// Forward, per token row: s = x + branch (fp32, stored in the type of x), then
+// the quantisation of the stored sum exactly as act_quant.hip does it.  The
+// row is read once and stays in registers through its three statistics.
+//
+// Backward (straight through the quantiser): with y = (s r) gamma and the
+// gradient dY of y,
+//   ds = r g - (r^3 t / K) s + ds_out,  g = gamma dY,  t = sum_k g_k s_k,
+//   dgamma = sum over rows of dY s r.
+// Both are streams: what bounds them is HBM.
+#include "mmf_device.h"
+#include "mmf_launch.h"
+#include "row_vec.h"
+
+namespace mmf {
+namespace {
+
+constexpr int64_t kMaxBlocks = int64_t(1) << 20;  // rows past them: further passes of the row loop
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+struct FwdArgs {
+  const void* x;
+  const void* branch;  // nullptr: none
+  const float* gamma;
+  void* s;             // nullptr (without a branch): not stored
+  int8_t* q;
+  float* a_scale;
+  int32_t* q_rowsum;
+  float* rstd;
+  int64_t M;
+  int K;
+};
+
+// One row per W waves, VPL vectors of E values per lane (VPL == 0: any K, the
+// stored sum read again for each further pass).  x and s may be the same
+// array: every element is read and written by one lane.
+template <typename XT, typename BT, int E, int W, int VPL>
+__global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const FwdArgs a) {
+  constexpr int kBlockWaves = W > 4 ? W : 4;
+  constexpr int kRows = kBlockWaves / W;
+  __shared__ double s_ss[kBlockWaves];
+  __shared__ float s_amax[kBlockWaves];
+  __shared__ int s_rs[kBlockWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rl = (wave % W) * kWave + (threadIdx.x & 63);  // lane within the row
+  const int K = a.K, nvec = K / E;
+  const XT* const x = static_cast<const XT*>(a.x);
+  const BT* const branch = static_cast<const BT*>(a.branch);
+  XT* const sum = static_cast<XT*>(a.s);
+  const __amdgpu_buffer_rsrc_t grsrc = row_rsrc(a.gamma, K, a.gamma != nullptr);
+  const auto addd = [](double u, double v) { return u + v; };
+  const auto addi = [](int u, int v) { return u + v; };
+  const auto maxf = [](float u, float v) { return fmaxf(u, v); };
+
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.M; r0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const int64_t row = r0 + wave / W;
+    const bool live = row < a.M;  // uniform per wave
+    const int64_t at = (live ? row : 0) * K;
+    int8_t* const qr = a.q + at;
+    const __amdgpu_buffer_rsrc_t xrsrc = row_rsrc(x + at, K, live);
+    const __amdgpu_buffer_rsrc_t brsrc = row_rsrc(branch == nullptr ? branch : branch + at, K, live && branch != nullptr);
+    float r, amax = 0.0f;
+    int rs = 0;
+    auto quantise = [&](int v, const float* y, float sc) {
+      uint32_t w[E / 4];
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        w[i] = quantise4(y + 4 * i, sc);
+        rs = byte_sum4(w[i], rs);
+      }
+      if constexpr (E == 8) *reinterpret_cast<uint2*>(qr + v * E) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint32_t*>(qr + v * E) = w[0];
+    };
+    if constexpr (VPL > 0) {
+      RowVec<XT, E> xv[VPL];
+      RowVec<BT, E> bv[VPL];
+      RowVec<float, E> gv[VPL];
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) xv[i].load(xrsrc, rl + W * kWave * i);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) bv[i].load(brsrc, rl + W * kWave * i);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) gv[i].load(grsrc, rl + W * kWave * i);
+      __builtin_amdgcn_sched_barrier(0);  // all loads before the first wait
+      double ss = 0.0;
+      float f[VPL][E];
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const int v = rl + W * kWave * i;
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[i][e] = xv[i].get(e) + bv[i].get(e);
+        xv[i].set(f[i]);
+        if (sum != nullptr && live && v < nvec) xv[i].store(sum + at, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          f[i][e] = xv[i].get(e);  // the stored value
+          ss = sum_sq(ss, f[i][e]);
+        }
+      }
+      ss = row_combine<W>(wave_sum_f64(ss), s_ss, wave, addd);
+      r = rms_rstd(ss, K);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          f[i][e] = f[i][e] * r;
+          if (a.gamma != nullptr) f[i][e] = f[i][e] * gv[i].get(e);
+          amax = fmaxf(amax, fabsf(f[i][e]));
+        }
+      amax = fmaxf(row_combine<W>(wave_max_f32(amax), s_amax, wave, maxf), 1e-5f);
+      const float sc = 127.0f / amax;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const int v = rl + W * kWave * i;
+        if (live && v < nvec) quantise(v, f[i], sc);
+      }
+    } else {
+      // each lane reads back the sums that it stored itself
+      const XT* const src = sum != nullptr ? sum + at : x + at;
+      double ss = 0.0;
+      for (int v = rl; v < nvec; v += W * kWave) {
+        RowVec<XT, E> xv;
+        RowVec<BT, E> bv;
+        xv.load(xrsrc, v);
+        bv.load(brsrc, v);
+        float f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = xv.get(e) + bv.get(e);
+        xv.set(f);
+        if (sum != nullptr && live) xv.store(sum + at, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) ss = sum_sq(ss, xv.get(e));
+      }
+      ss = row_combine<W>(wave_sum_f64(ss), s_ss, wave, addd);
+      r = rms_rstd(ss, K);
+      auto normed = [&](int v, float* f) {
+        RowVec<float, E> gv;
+        gv.load(grsrc, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if constexpr (sizeof(XT) == 4) f[e] = src[v * E + e];
+          else f[e] = bf16_to_f32(src[v * E + e]);
+          f[e] = f[e] * r;
+          if (a.gamma != nullptr) f[e] = f[e] * gv.get(e);
+        }
+      };
+      for (int v = rl; live && v < nvec; v += W * kWave) {
+        float f[E];
+        normed(v, f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) amax = fmaxf(amax, fabsf(f[e]));
+      }
+      amax = fmaxf(row_combine<W>(wave_max_f32(amax), s_amax, wave, maxf), 1e-5f);
+      const float sc = 127.0f / amax;
+      for (int v = rl; live && v < nvec; v += W * kWave) {
+        float f[E];
+        normed(v, f);
+        quantise(v, f, sc);
+      }
+    }
+    rs = row_combine<W>(wave_sum_i32(rs), s_rs, wave, addi);
+    if (live && rl == 0) {
+      a.a_scale[row] = amax / 127.0f;
+      if (a.q_rowsum != nullptr) a.q_rowsum[row] = rs;
+      if (a.rstd != nullptr) a.rstd[row] = r;
+    }
+    if constexpr (W > 1) __syncthreads();  // the slots are the next row's
+  }
+}
+
+template <typename XT, typename BT, int E, int W, int VPL>
+hipError_t launch_fwd_one(const FwdArgs& a, hipStream_t stream) {
+  constexpr int kBlockWaves = W > 4 ? W : 4;
+  constexpr int kRows = kBlockWaves / W;
+  const int64_t blocks = (a.M + kRows - 1) / kRows;
+  const dim3 grid(static_cast<unsigned>(blocks < kMaxBlocks ? blocks : kMaxBlocks));
+  hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+// The smallest compiled number of vectors per lane that holds the row (loads
+// past the row's end return zeros but cost nearly a real load each).
+template <typename XT, typename BT, int E, int W>
+hipError_t launch_fwd_w(const FwdArgs& a, hipStream_t stream) {
+  const int vpl = (a.K / E + W * kWave - 1) / (W * kWave);
+  switch (vpl) {
+    case 1: return launch_fwd_one<XT, BT, E, W, 1>(a, stream);
+    case 2: return launch_fwd_one<XT, BT, E, W, 2>(a, stream);
+    case 3: return launch_fwd_one<XT, BT, E, W, 3>(a, stream);
+    case 4: return launch_fwd_one<XT, BT, E, W, 4>(a, stream);
+    default: break;
+  }
+  if constexpr (E == 4) {
+    switch (vpl) {
+      case 5: return launch_fwd_one<XT, BT, E, W, 5>(a, stream);
+      case 6: return launch_fwd_one<XT, BT, E, W, 6>(a, stream);
+      case 7: case 8: return launch_fwd_one<XT, BT, E, W, 8>(a, stream);
+      default: break;
+    }
+  }
+  if constexpr (W == 16) return launch_fwd_one<XT, BT, E, W, 0>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+// Waves per row: up to 32 values per lane stay in registers (K <= 32768);
+// with few rows, when most of the chip idles anyway, more waves share a row.
+constexpr int64_t kFewRows = 64;
+template <typename XT, typename BT, int E>
+hipError_t launch_fwd(const FwdArgs& a, hipStream_t stream) {
+  int w = a.K <= kWave * 32 ? 1 : a.K <= 4 * kWave * 32 ? 4 : 16;
+  if (a.M <= kFewRows && w < 16 && a.K > w * kWave * 8) w *= 4;
+  if (w == 1) return launch_fwd_w<XT, BT, E, 1>(a, stream);
+  if (w == 4) return launch_fwd_w<XT, BT, E, 4>(a, stream);
+  return launch_fwd_w<XT, BT, E, 16>(a, stream);
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+struct BwdArgs {
+  const void* dy;
+  const float* ds_out;  // nullptr: zero; may be ds
+  const void* s;
+  const float* gamma;
+  const float* rstd;
+  float* ds;
+  uint16_t* ds_bf16;    // nullptr: not stored
+  double* dg_part;      // [gridDim.x][K], nullptr: not computed
+  int64_t M;
+  int K;
+};
+
+// Workgroups of W waves, each taking rows blockIdx.x, + gridDim.x, ...; every
+// lane owns the same columns of each row and keeps their gamma and their
+// dgamma sums (fp64) in registers.  The next row's loads are in flight while
+// a row is reduced and written (not with 16 waves, whose 128 registers hold
+// one row only).  VPL == 0: any K; the row is read twice and the column sums
+// are kept in dg_part.
+template <typename ST, typename DT, int E, int W, int VPL>
+__global__ __launch_bounds__(kWave* W) void add_quant_bwd_kernel(const BwdArgs a) {
+  __shared__ double s_t[2][W];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rl = threadIdx.x;
+  const int K = a.K, nvec = K / E;
+  const DT* const dy = static_cast<const DT*>(a.dy);
+  const ST* const s = static_cast<const ST*>(a.s);
+  const __amdgpu_buffer_rsrc_t grsrc = row_rsrc(a.gamma, K, a.gamma != nullptr);
+  const auto addd = [](double u, double v) { return u + v; };
+  double* const part = a.dg_part == nullptr ? nullptr : a.dg_part + static_cast<int64_t>(blockIdx.x) * K;
+  auto coef = [&](double t, float r) {
+    const double rd = static_cast<double>(r);
+    return static_cast<float>(rd * rd * rd * t / static_cast<double>(K));
+  };
+  auto emit = [&](int64_t at, int v, const float* o) {
+    RowVec<float, E> ov;
+    ov.set(o);
+    ov.store(a.ds + at, v);
+    if (a.ds_bf16 != nullptr) {
+      RowVec<uint16_t, E> hv;
+      hv.set(o);
+      hv.store(a.ds_bf16 + at, v);
+    }
+  };
+  int parity = 0;
+  if constexpr (VPL > 0) {
+    struct Row {
+      RowVec<DT, E> dy[VPL];
+      RowVec<ST, E> s[VPL];
+      RowVec<float, E> res[VPL];
+      float r;
+    };
+    auto load = [&](Row& w, int64_t row) {
+      const bool live = row < a.M;
+      const int64_t at = (live ? row : 0) * K;
+      const __amdgpu_buffer_rsrc_t drsrc = row_rsrc(dy + at, K, live), srsrc = row_rsrc(s + at, K, live);
+      const __amdgpu_buffer_rsrc_t orsrc =
+          row_rsrc(a.ds_out == nullptr ? a.ds_out : a.ds_out + at, K, live && a.ds_out != nullptr);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) w.dy[i].load(drsrc, rl + W * kWave * i);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) w.s[i].load(srsrc, rl + W * kWave * i);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) w.res[i].load(orsrc, rl + W * kWave * i);
+      w.r = a.rstd[live ? row : 0];
+    };
+    RowVec<float, E> gv[VPL];
+    double dg[VPL][E];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      gv[i].load(grsrc, rl + W * kWave * i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) dg[i][e] = 0.0;
+    }
+    if (a.gamma == nullptr) {  // uniform
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) gv[i].w[e] = __float_as_uint(1.0f);
+    }
+    constexpr bool kAhead = W < 16;
+    Row cur;
+    if constexpr (kAhead) load(cur, blockIdx.x);
+    for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+      Row next;
+      load(kAhead ? next : cur, row + (kAhead ? gridDim.x : 0));
+      __builtin_amdgcn_sched_barrier(0);
+      const int64_t at = row * K;
+      double t = 0.0;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float d = cur.dy[i].get(e), sv = cur.s[i].get(e);
+          t += static_cast<double>(gv[i].get(e) * d) * static_cast<double>(sv);
+          dg[i][e] += static_cast<double>(d * (sv * cur.r));
+        }
+      t = row_combine<W>(wave_sum_f64(t), s_t[parity], wave, addd);
+      parity ^= 1;
+      const float c = coef(t, cur.r);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const int v = rl + W * kWave * i;
+        float o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          o[e] = (cur.r * (gv[i].get(e) * cur.dy[i].get(e)) - c * cur.s[i].get(e)) + cur.res[i].get(e);
+        if (v < nvec) emit(at, v, o);
+      }
+      if constexpr (kAhead) cur = next;
+    }
+    if (part != nullptr) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const int v = rl + W * kWave * i;
+        if (v < nvec) {
+#pragma unroll
+          for (int e = 0; e < E; e += 2)
+            *reinterpret_cast<double2*>(part + v * E + e) = make_double2(dg[i][e], dg[i][e + 1]);
+        }
+      }
+    }
+  } else {
+    for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+      const int64_t at = row * K;
+      const __amdgpu_buffer_rsrc_t drsrc = row_rsrc(dy + at, K, true), srsrc = row_rsrc(s + at, K, true);
+      const __amdgpu_buffer_rsrc_t orsrc = row_rsrc(a.ds_out == nullptr ? a.ds_out : a.ds_out + at, K, a.ds_out != nullptr);
+      const float r = a.rstd[row];
+      double t = 0.0;
+      for (int v = rl; v < nvec; v += W * kWave) {
+        RowVec<DT, E> dv;
+        RowVec<ST, E> sv;
+        RowVec<float, E> gv;
+        dv.load(drsrc, v);
+        sv.load(srsrc, v);
+        gv.load(grsrc, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float g = a.gamma != nullptr ? gv.get(e) * dv.get(e) : dv.get(e);
+          t += static_cast<double>(g) * static_cast<double>(sv.get(e));
+        }
+      }
+      t = row_combine<W>(wave_sum_f64(t), s_t[parity], wave, addd);
+      parity ^= 1;
+      const float c = coef(t, r);
+      for (int v = rl; v < nvec; v += W * kWave) {
+        RowVec<DT, E> dv;
+        RowVec<ST, E> sv;
+        RowVec<float, E> gv, rv;
+        dv.load(drsrc, v);
+        sv.load(srsrc, v);
+        gv.load(grsrc, v);
+        rv.load(orsrc, v);
+        float o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float g = a.gamma != nullptr ? gv.get(e) * dv.get(e) : dv.get(e);
+          o[e] = (r * g - c * sv.get(e)) + rv.get(e);
+          if (part != nullptr) {
+            const double dg = static_cast<double>(dv.get(e) * (sv.get(e) * r));
+            part[v * E + e] = (row == blockIdx.x ? 0.0 : part[v * E + e]) + dg;
+          }
+        }
+        emit(at, v, o);
+      }
+    }
+  }
+}
+
+template <typename ST, typename DT, int E, int W>
+hipError_t launch_bwd_w(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
+  const int vpl = (a.K / E + W * kWave - 1) / (W * kWave);
+#define MMF_LAUNCH(V) hipLaunchKernelGGL((add_quant_bwd_kernel<ST, DT, E, W, V>), dim3(blocks), dim3(kWave * W), 0, stream, a)
+  switch (vpl) {
+    case 1: MMF_LAUNCH(1); break;
+    case 2: MMF_LAUNCH(2); break;
+    case 3: MMF_LAUNCH(3); break;
+    case 4: MMF_LAUNCH(4); break;
+    default:
+      if constexpr (W == 16) MMF_LAUNCH(0);
+      else return hipErrorInvalidValue;
+  }
+#undef MMF_LAUNCH
+  return hipGetLastError();
+}
+
+// Waves per row: at most 16 values per lane (gamma, the fp64 column sums and
+// two rows of operands are all in registers).
+int bwd_waves(int K) {
+  int w = 1;
+  while (w < 16 && K > w * kWave * 16) w *= w == 1 ? 4 : 2;
+  return w;
+}
+
+template <typename ST, typename DT>
+hipError_t launch_bwd(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
+  switch (bwd_waves(a.K)) {
+    case 1: return launch_bwd_w<ST, DT, 4, 1>(a, blocks, stream);
+    case 4: return launch_bwd_w<ST, DT, 4, 4>(a, blocks, stream);
+    case 8: return launch_bwd_w<ST, DT, 4, 8>(a, blocks, stream);
+    default: return launch_bwd_w<ST, DT, 4, 16>(a, blocks, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_add_quant(const AddQuantArgs& p, hipStream_t stream) {
+  if (p.M == 0) return hipSuccess;
+  const FwdArgs a{p.x, p.branch, p.gamma, p.s, p.q, p.a_scale, p.q_rowsum, p.rstd, p.M, p.K};
+  if (p.x_is_f32)
+    return p.branch_is_f32 ? launch_fwd<float, float, 4>(a, stream) : launch_fwd<float, uint16_t, 4>(a, stream);
+  return p.branch_is_f32 ? launch_fwd<uint16_t, float, 4>(a, stream) : launch_fwd<uint16_t, uint16_t, 8>(a, stream);
+}
+
+// Workgroups of the backward, each with a row of column sums: two waves per
+// SIMD over 256 compute units, at most one per row.
+int64_t add_quant_bwd_parts(int64_t M, int K) {
+  const int64_t most = 2048 / bwd_waves(K);
+  return M < most ? M : most;
+}
+
+hipError_t launch_add_quant_bwd(const AddQuantBwdArgs& p, hipStream_t stream) {
+  if (p.M == 0) return hipSuccess;
+  const BwdArgs a{p.dy, p.ds_out, p.s, p.gamma, p.rstd, p.ds, p.ds_bf16, p.dg_part, p.M, p.K};
+  const unsigned blocks = static_cast<unsigned>(add_quant_bwd_parts(p.M, p.K));
+  if (p.s_is_f32)
+    return p.dy_is_f32 ? launch_bwd<float, float>(a, blocks, stream) : launch_bwd<float, uint16_t>(a, blocks, stream);
+  return p.dy_is_f32 ? launch_bwd<uint16_t, float>(a, blocks, stream)
+                     : launch_bwd<uint16_t, uint16_t>(a, blocks, stream);
+}
+
+}  // namespace mmf

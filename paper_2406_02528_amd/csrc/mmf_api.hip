@@ -296,6 +296,12 @@ int glu_alloc(const void* x, bool x_is_f32, const float* gamma, const uint32_t* 
 
 bool aligned16_or_null(const void* p) { return p == nullptr || aligned16(p); }
 
+// ---- residual addition + quantisation, backward ----
+size_t add_quant_bwd_bytes(int64_t M, int64_t K) {
+  const int64_t parts = mmf::add_quant_bwd_parts(M, static_cast<int>(K));
+  return round_up(sizeof(double) * static_cast<size_t>(parts * K), kScratchAlign);
+}
+
 // ---- MLGRU ----
 constexpr uint32_t kMlgruActs = mmf::kActSigmoidLb | (mmf::kActSilu << 2) | (mmf::kActIdentity << 4);
 
@@ -563,6 +569,49 @@ int mmf_bitlinear_fwd_noalloc(const void* x, int x_is_f32, const float* gamma,
     if (ws == nullptr) return st;
   }
   return run_from_x(path, route, x, f32, gamma, Wpacked, w_scale, y, M, K, N, ep, {}, ws, stream);
+}
+
+int mmf_add_act_quant(const void* x, int x_is_f32, const void* branch, int branch_is_f32, const float* gamma,
+                      void* s, int8_t* q, float* a_scale, int32_t* q_rowsum, float* rstd, int64_t M, int64_t K,
+                      hipStream_t stream) {
+  if (int st = check_dtype(x_is_f32)) return st;
+  if (int st = check_dtype(branch_is_f32)) return st;
+  if (int st = check_shape(M, K, 0)) return st;
+  if (M == 0) return MMF_OK;
+  if (!x || (branch && !s) || !q || !a_scale) return MMF_ERR_NULL;
+  if (!aligned16(x) || !aligned16_or_null(branch) || !aligned16_or_null(gamma) || !aligned16_or_null(s) ||
+      !aligned16(q) || !aligned16(a_scale) || !aligned16_or_null(q_rowsum) || !aligned16_or_null(rstd))
+    return MMF_ERR_ALIGN;
+  return hip_status(mmf::launch_add_quant({x, x_is_f32 == 1, branch, branch_is_f32 == 1, gamma, s, q, a_scale,
+                                           q_rowsum, rstd, M, static_cast<int>(K)},
+                                          stream));
+}
+
+size_t mmf_add_act_quant_bwd_workspace_bytes(int64_t M, int64_t K) {
+  if (check_shape(M, K, 0) != MMF_OK) return 0;
+  return add_quant_bwd_bytes(M, K);
+}
+
+int mmf_add_act_quant_bwd(const void* dY, int dy_is_f32, const float* ds_out, const void* s, int s_is_f32,
+                          const float* gamma, const float* rstd, float* ds, uint16_t* ds_bf16, float* dgamma,
+                          int64_t M, int64_t K, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_dtype(dy_is_f32)) return st;
+  if (int st = check_dtype(s_is_f32)) return st;
+  if (int st = check_shape(M, K, 0)) return st;
+  if (M == 0) return MMF_OK;
+  if (!dY || !s || !rstd || !ds) return MMF_ERR_NULL;
+  if (!aligned16(dY) || !aligned16_or_null(ds_out) || !aligned16(s) || !aligned16_or_null(gamma) ||
+      !aligned16(rstd) || !aligned16(ds) || !aligned16_or_null(ds_bf16) || !aligned16_or_null(dgamma))
+    return MMF_ERR_ALIGN;
+  const size_t need = dgamma ? add_quant_bwd_bytes(M, K) : 0;
+  return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
+    const int Ki = static_cast<int>(K);
+    double* part = dgamma ? reinterpret_cast<double*>(scratch) : nullptr;
+    if (mmf::launch_add_quant_bwd({dY, dy_is_f32 == 1, ds_out, s, s_is_f32 == 1, gamma, rstd, ds, ds_bf16, part, M, Ki},
+                                  stream) != hipSuccess)
+      return MMF_ERR_HIP;
+    return hip_status(mmf::launch_col_final({part, mmf::add_quant_bwd_parts(M, Ki), K, dgamma}, {}, stream));
+  });
 }
 
 int mmf_ternary_gemm_dequant(const int8_t* q, const float* a_scale, const int32_t* q_rowsum,

@@ -22,6 +22,44 @@ hipError_t launch_act_quant_mlgru(const float* fcg, const float* h_in, float* h_
                                   float* a_scale, int32_t* q_rowsum, int64_t M, int K, hipStream_t stream,
                                   bool tiled);
 
+// Residual addition + the quantisation of the sum (add_quant.hip): s = x +
+// branch in the type of x (branch nullptr: s = x; s nullptr: not stored), then
+// as launch_act_quant on s.  s may be x.
+struct AddQuantArgs {
+  const void* x;
+  bool x_is_f32;
+  const void* branch;
+  bool branch_is_f32;
+  const float* gamma;
+  void* s;
+  int8_t* q;
+  float* a_scale;
+  int32_t* q_rowsum;
+  float* rstd;
+  int64_t M;
+  int K;
+};
+hipError_t launch_add_quant(const AddQuantArgs& a, hipStream_t stream);
+// Its backward: ds [M][K] (and rounded in ds_bf16), dgamma's column sums in
+// dg_part [add_quant_bwd_parts(M, K)][K]; ds_out, ds_bf16 and dg_part may be
+// nullptr, ds may be ds_out.
+struct AddQuantBwdArgs {
+  const void* dy;
+  bool dy_is_f32;
+  const float* ds_out;
+  const void* s;
+  bool s_is_f32;
+  const float* gamma;
+  const float* rstd;
+  float* ds;
+  uint16_t* ds_bf16;
+  double* dg_part;
+  int64_t M;
+  int K;
+};
+int64_t add_quant_bwd_parts(int64_t M, int K);
+hipError_t launch_add_quant_bwd(const AddQuantBwdArgs& a, hipStream_t stream);
+
 // q_rowsum[m] = sum_k q[m][k].
 hipError_t launch_row_sum(const int8_t* q, int32_t* q_rowsum, int64_t M, int K,
                           hipStream_t stream);
