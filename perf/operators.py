@@ -338,11 +338,11 @@ def _plain_clip(v):
 # one pass through the framework
 # ---------------------------------------------------------------------------
 
-def _kept(v, bytes_of):
+def _kept(v, bytes_of, name="ws"):
     """The program's workspace, made at its first call and kept."""
-    if "ws" not in v:
-        v["ws"] = torch.empty(max(int(bytes_of()), 256), dtype=torch.uint8, device="cuda")
-    return v["ws"]
+    if name not in v:
+        v[name] = torch.empty(max(int(bytes_of()), 256), dtype=torch.uint8, device="cuda")
+    return v[name]
 
 
 def _run_own(v):
@@ -362,8 +362,10 @@ def _run_own(v):
     if kind == "scan":
         B, T, d = v["B"], v["T"], v["o"].shape[1]
         ws = _kept(v, lambda: mmf.mmf_mlgru_scan_bwd_workspace_bytes(B, T, d))
-        mmf.mmf_mlgru_train_scan(v["z"], B, T, v["lb"], v["h0"], v["o"], v["h"], ws)
-        mmf.mmf_mlgru_scan_bwd(v["z"], B, T, v["lb"], v["h0"], v["do"], v["dh"], v["dz"], v["dh0"], v["dlb"], ws)
+        # what the forward leaves for the backward: the states entering chunks of tokens
+        states = _kept(v, lambda: mmf.mmf_mlgru_train_states_bytes(B, T, d), "states")
+        mmf.mmf_mlgru_train_scan(v["z"], B, T, v["lb"], v["h0"], v["o"], v["h"], states, ws)
+        mmf.mmf_mlgru_scan_bwd(v["z"], B, T, v["lb"], states, v["do"], v["dh"], v["dz"], v["dh0"], v["dlb"], ws)
         out = {k: v[k] for k in ("o", "h", "dz", "dh0")}
         if v["dlb"] is not None:
             out["dlb"] = v["dlb"]
