@@ -393,6 +393,45 @@ int mmf_mlgru_fwd(const void *x, int x_is_f32, const float *gamma, const uint32_
                   int64_t d, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * The recurrence in training form.  The three projections come as
+ * pre-activations z [B*T][3d] float32 (zf | zc | zg: the y of
+ * mmf_bitlinear_train_fwd with the stacked [3d][K] latent weights and the
+ * bias), so that the backward ends in the gradient that mmf_bitlinear_bwd
+ * takes.  Forward, for token t of a sequence (s = sigmoid as above, fp32):
+ *   f = (1 - lb) s(zf) + lb,  c = zc s(zc),  g = zg
+ *   h_t = f h_{t-1} + (1 - f) c,   o'_t = g s(h_t)
+ * lb [d] or NULL (0); h0 [B][d] or NULL (0); o_prime [B*T][d]; h_last [B][d]
+ * (NULL: not stored; may be the same array as h0).  `states` (256-byte
+ * aligned, mmf_mlgru_train_states_bytes) receives the states entering chunks
+ * of tokens, which the backward starts from.
+ *
+ * Backward, from do_prime [B*T][d] (bf16 bits or float32, do_is_f32) and
+ * dh_last [B][d] (NULL: 0):
+ *   dh_t = do_t g_t s(h_t) (1 - s(h_t)) + f_{t+1} dh_{t+1}   (+ dh_last at the end)
+ *   dz_f = dh (h_{t-1} - c) (1 - lb) s(zf) (1 - s(zf))
+ *   dz_c = dh (1 - f) s(zc) (1 + zc (1 - s(zc)))
+ *   dz_g = do s(h)
+ *   dh0 = f_1 dh_1,  dlb = sum over all tokens of dh (h_{t-1} - c) (1 - s(zf))
+ * in fp32, dz [B*T][3d] rounded once to bf16 (the dO of mmf_bitlinear_bwd);
+ * dh0 [B][d] (NULL: not stored), dlb [d] (NULL: not computed; summed in fp64,
+ * in a fixed order) float32.  z, lb and states as the forward had and left
+ * them.  Inside both, the tokens are cut into chunks whose maps are joined.
+ * More than 2^22 workgroups (B ceil(T/64) ceil(d/128)) return MMF_ERR_SHAPE;
+ * B == 0 or T == 0 is a no-op.  Workspace as above; the backward's also
+ * serves the forward.
+ */
+size_t mmf_mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d);
+size_t mmf_mlgru_train_scan_workspace_bytes(int64_t B, int64_t T, int64_t d);
+int mmf_mlgru_train_scan(const float *z, const float *lb, const float *h0, float *o_prime,
+                         float *h_last, void *states, size_t states_bytes, int64_t B, int64_t T,
+                         int64_t d, void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t mmf_mlgru_scan_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d);
+int mmf_mlgru_scan_bwd(const float *z, const float *lb, const void *states, size_t states_bytes,
+                       const void *do_prime, int do_is_f32, const float *dh_last, uint16_t *dz,
+                       float *dh0, float *dlb, int64_t B, int64_t T, int64_t d, void *workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Training forward (Algorithm 1, forward_pass: the latent weights are
  * quantised on every call; the RMSNorm statistic r is kept for the
  * backward).  From latent float32 weights W [N][K]:
@@ -444,6 +483,26 @@ int mmf_bitlinear_bwd(const uint16_t *dO, const void *x, int x_is_f32, const flo
                       const uint32_t *Wpacked, const float *w_scale, float *dx, float *dW,
                       float *db, float *dgamma, int64_t M, int64_t K, int64_t N,
                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The norm over all elements of a set of gradients, and the set scaled to it:
+ *   norm = sqrt(sum_i sum g_i^2)            (squares and sums in fp64)
+ *   out_i = g_i min(max_norm / (norm + 1e-6), 1)    (fp32, rounded to g_i's type)
+ * `grads`, `outs`, `is_f32` and `counts` are HOST arrays of n entries, read
+ * before the call returns: device addresses of the gradients (16-byte
+ * aligned; any address where the count is 0), where the scaled ones go
+ * (outs[i] may be grads[i]; no other overlap), 0 for bf16 or 1 for float32, and
+ * numbers of elements (any from 0 to 2^36, MMF_ERR_SHAPE).  norm [1] float32
+ * is a device array: between the two calls the norms of other shards can be
+ * joined in it.  A norm of NaN makes every output NaN, an infinite one
+ * scales by 0.  max_norm must be a number of at least 0 (MMF_ERR_ARG).  The sums are added in a
+ * fixed order.  n == 0: norm = 0.  Workspace as above.
+ */
+size_t mmf_grad_norm_workspace_bytes(const int64_t *counts, int64_t n);
+int mmf_grad_norm(const void *const *grads, const int *is_f32, const int64_t *counts, int64_t n,
+                  float *norm, void *workspace, size_t workspace_bytes, hipStream_t stream);
+int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *counts, int64_t n,
+                  const float *norm, float max_norm, void *const *outs, hipStream_t stream);
 
 /*
  * Kernel selection for the contraction: MMF_PATH_AUTO (the fused decode, the

@@ -85,6 +85,15 @@ _SIGNATURES = {
     "mmf_bitlinear_bwd_workspace_bytes": ([_I64, _I64, _I64], _SZ),
     "mmf_bitlinear_bwd": ([_P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64,
                            _I64, _P, _SZ, _P], ctypes.c_int),
+    "mmf_mlgru_train_states_bytes": ([_I64, _I64, _I64], _SZ),
+    "mmf_mlgru_train_scan_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+    "mmf_mlgru_train_scan": ([_P, _P, _P, _P, _P, _P, _SZ, _I64, _I64, _I64, _P, _SZ, _P], ctypes.c_int),
+    "mmf_mlgru_scan_bwd_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+    "mmf_mlgru_scan_bwd": ([_P, _P, _P, _SZ, _P, ctypes.c_int, _P, _P, _P, _P, _I64, _I64, _I64, _P, _SZ, _P],
+                           ctypes.c_int),
+    "mmf_grad_norm_workspace_bytes": ([_P, _I64], _SZ),
+    "mmf_grad_norm": ([_P, _P, _P, _I64, _P, _P, _SZ, _P], ctypes.c_int),
+    "mmf_grad_clip": ([_P, _P, _P, _I64, _P, ctypes.c_float, _P, _P], ctypes.c_int),
     "mmf_mlgru_fwd": ([_P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                        _I64, _I64, _I64, _P, _SZ, _P], ctypes.c_int),
 }
@@ -561,6 +570,110 @@ def mmf_mlgru_fwd(x: torch.Tensor, B: int, T: int, gamma: torch.Tensor | None,
                               _ptr(bias), _ptr(lb), _ptr(h0), _ptr(h_last), _ptr(gamma_o),
                               _ptr(Wo), _ptr(w_scale_o), _ptr(b_o), _ptr(o), B, T, d, wp, wn,
                               _stream(stream)))
+
+
+def mmf_mlgru_train_states_bytes(B: int, T: int, d: int) -> int:
+    return int(_lib.mmf_mlgru_train_states_bytes(B, T, d))
+
+
+def mmf_mlgru_train_scan_workspace_bytes(B: int, T: int, d: int) -> int:
+    return int(_lib.mmf_mlgru_train_scan_workspace_bytes(B, T, d))
+
+
+def mmf_mlgru_scan_bwd_workspace_bytes(B: int, T: int, d: int) -> int:
+    return int(_lib.mmf_mlgru_scan_bwd_workspace_bytes(B, T, d))
+
+
+def mmf_mlgru_train_scan(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None, h0: torch.Tensor | None,
+                         o_prime: torch.Tensor, h_last: torch.Tensor | None, states: torch.Tensor,
+                         workspace: torch.Tensor | None = None, stream=None) -> None:
+    """The recurrence in training form: o_prime f32 [B*T][d] and h_last f32
+    [B][d] (or None; may be h0) from the gates' pre-activations z f32 [B*T][3d]
+    (f | c | g), lb f32 [d] or None and h0 f32 [B][d] or None; states uint8
+    (mmf_mlgru_train_states_bytes) keeps what mmf_mlgru_scan_bwd starts from."""
+    d = z.shape[1] // 3
+    _need_here(z, "z", torch.float32, (B * T, 3 * d))
+    if lb is not None:
+        _need_here(lb, "lb", torch.float32, (d,))
+    if h0 is not None:
+        _need_here(h0, "h0", torch.float32, (B, d))
+    _need_here(o_prime, "o_prime", torch.float32, (B * T, d))
+    if h_last is not None:
+        _need_here(h_last, "h_last", torch.float32, (B, d))
+    _need_here(states, "states", torch.uint8, (states.numel(),))
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_mlgru_train_scan(_ptr(z), _ptr(lb), _ptr(h0), _ptr(o_prime), _ptr(h_last), _ptr(states),
+                                     states.numel(), B, T, d, wp, wn, _stream(stream)))
+
+
+def mmf_mlgru_scan_bwd(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None, states: torch.Tensor,
+                       do_prime: torch.Tensor, dh_last: torch.Tensor | None, dz: torch.Tensor,
+                       dh0: torch.Tensor | None, dlb: torch.Tensor | None,
+                       workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Backward of mmf_mlgru_train_scan: dz bf16 [B*T][3d] (the dO of
+    mmf_bitlinear_bwd), dh0 f32 [B][d] (or None) and dlb f32 [d] (or None) from
+    do_prime bf16/f32 [B*T][d], dh_last f32 [B][d] (or None) and the forward's
+    z, lb and states."""
+    d = z.shape[1] // 3
+    do_f32 = _kind(do_prime, "do_prime")
+    _need_here(z, "z", torch.float32, (B * T, 3 * d))
+    if lb is not None:
+        _need_here(lb, "lb", torch.float32, (d,))
+    _need_here(states, "states", torch.uint8, (states.numel(),))
+    _need_here(do_prime, "do_prime", do_prime.dtype, (B * T, d))
+    if dh_last is not None:
+        _need_here(dh_last, "dh_last", torch.float32, (B, d))
+    _need_here(dz, "dz", torch.bfloat16, (B * T, 3 * d))
+    if dh0 is not None:
+        _need_here(dh0, "dh0", torch.float32, (B, d))
+    if dlb is not None:
+        _need_here(dlb, "dlb", torch.float32, (d,))
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_mlgru_scan_bwd(_ptr(z), _ptr(lb), _ptr(states), states.numel(), _ptr(do_prime), do_f32,
+                                   _ptr(dh_last), _ptr(dz), _ptr(dh0), _ptr(dlb), B, T, d, wp, wn, _stream(stream)))
+
+
+def _grad_set(tensors, name):
+    """Addresses, types and sizes of a list of tensors, as C arrays."""
+    n = len(tensors)
+    ptrs, kinds, counts = (ctypes.c_void_p * n)(), (ctypes.c_int * n)(), (_I64 * n)()
+    here = torch._C._cuda_getDevice() if n else 0
+    for i, t in enumerate(tensors):
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.get_device() == here
+                and (t.dtype is torch.float32 or t.dtype is torch.bfloat16)):
+            _kind(t, f"{name}[{i}]") if isinstance(t, torch.Tensor) else None
+            _need_here(t, f"{name}[{i}]", getattr(t, "dtype", None), getattr(t, "shape", ()))
+        ptrs[i], kinds[i], counts[i] = t.data_ptr(), t.dtype is torch.float32, t.numel()
+    return ptrs, kinds, counts, n
+
+
+def mmf_grad_norm_workspace_bytes(counts) -> int:
+    n = len(counts)
+    return int(_lib.mmf_grad_norm_workspace_bytes((_I64 * n)(*counts), n))
+
+
+def mmf_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """norm f32 [1] = the 2-norm over all elements of the tensors of `grads`
+    (each bf16 or f32, contiguous, of any shape)."""
+    _need_here(norm, "norm", torch.float32, (1,))
+    ptrs, kinds, counts, n = _grad_set(grads, "grads")
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_grad_norm(ptrs, kinds, counts, n, _ptr(norm), wp, wn, _stream(stream)))
+
+
+def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=None) -> None:
+    """outs[i] = grads[i] * min(max_norm / (norm + 1e-6), 1); outs None: in
+    place.  outs[i] has the type and shape of grads[i]."""
+    _need_here(norm, "norm", torch.float32, (1,))
+    ptrs, kinds, counts, n = _grad_set(grads, "grads")
+    dst = ptrs
+    if outs is not None:
+        if len(outs) != n:
+            raise ValueError(f"outs must have {n} tensors, got {len(outs)}")
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            _need_here(o, f"outs[{i}]", g.dtype, g.shape)
+        dst = (ctypes.c_void_p * n)(*[o.data_ptr() for o in outs])
+    _check(_lib.mmf_grad_clip(ptrs, kinds, counts, n, _ptr(norm), max_norm, dst, _stream(stream)))
 
 
 def mmf_bitlinear_train_workspace_bytes(M: int, K: int, N: int) -> int:

@@ -296,6 +296,21 @@ int glu_alloc(const void* x, bool x_is_f32, const float* gamma, const uint32_t* 
 
 bool aligned16_or_null(const void* p) { return p == nullptr || aligned16(p); }
 
+// ---- gradient norm ----
+int check_grads(const void* const* grads, const int* is_f32, const int64_t* counts, int64_t n, bool arrays) {
+  if (n < 0 || n > kMaxMN) return MMF_ERR_SHAPE;
+  if (n > 0 && (!counts || (arrays && (!grads || !is_f32)))) return MMF_ERR_NULL;
+  for (int64_t i = 0; i < n; ++i) {
+    if (counts[i] < 0 || counts[i] > mmf::kGradMaxCount) return MMF_ERR_SHAPE;
+    if (!arrays) continue;
+    if (int st = check_dtype(is_f32[i])) return st;
+    if (counts[i] == 0) continue;
+    if (!grads[i]) return MMF_ERR_NULL;
+    if (!aligned16(grads[i])) return MMF_ERR_ALIGN;
+  }
+  return MMF_OK;
+}
+
 // ---- residual addition + quantisation, backward ----
 size_t add_quant_bwd_bytes(int64_t M, int64_t K) {
   const int64_t parts = mmf::add_quant_bwd_parts(M, static_cast<int>(K));
@@ -351,6 +366,33 @@ MlgruScratch mlgru_scratch(int64_t B, int64_t T, int64_t d) {
   s.q_off = s.op_off + round_up(M * static_cast<size_t>(d) * 4, kScratchAlign);
   s.scan_off = s.q_off + fwd_scratch(static_cast<int64_t>(M), d).total;
   s.total = s.scan_off + scan_ws_bytes(B, T, d);
+  return s;
+}
+
+// ---- the recurrence in training form ----
+constexpr int64_t kMaxScanBlocks = int64_t(1) << 22;
+int check_mlgru_train(int64_t B, int64_t T, int64_t d) {
+  if (int st = check_mlgru_d(d)) return st;
+  if (B < 0 || T < 0 || B > kMaxMN || T > kMaxMN || (T > 0 && B > kMaxMN / T)) return MMF_ERR_SHAPE;
+  return mmf::mlgru_train_blocks(B, T, d) <= kMaxScanBlocks ? MMF_OK : MMF_ERR_SHAPE;
+}
+size_t mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d) {
+  return round_up(sizeof(float) * static_cast<size_t>(B * mmf::mlgru_train_chunks(T) * d), kScratchAlign);
+}
+bool states_fit(const void* states, size_t bytes, int64_t B, int64_t T, int64_t d) {
+  return (reinterpret_cast<uintptr_t>(states) & (kScratchAlign - 1)) == 0 && bytes >= mlgru_train_states_bytes(B, T, d);
+}
+// `arrays` of one value per chunk and channel (the chunks' maps, and the
+// backward's carries), then the partial sums of lb's gradient.
+struct MlgruTrainScratch {
+  size_t dlb_off, total;
+};
+MlgruTrainScratch mlgru_train_scratch(int64_t B, int64_t T, int64_t d, int arrays) {
+  const int64_t nchunk = mmf::mlgru_train_chunks(T);
+  const size_t n = static_cast<size_t>(B * nchunk * d);
+  MlgruTrainScratch s;
+  s.dlb_off = nchunk > 1 ? round_up(sizeof(float) * n * static_cast<size_t>(arrays), kScratchAlign) : 0;
+  s.total = s.dlb_off + round_up(sizeof(double) * n, kScratchAlign);
   return s;
 }
 
@@ -791,6 +833,61 @@ int mmf_mlgru_scan(const float* fcg, const float* h0, float* o_prime, float* h_l
   });
 }
 
+size_t mmf_mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d) {
+  if (check_mlgru_train(B, T, d) != MMF_OK) return 0;
+  return mlgru_train_states_bytes(B, T, d);
+}
+
+size_t mmf_mlgru_train_scan_workspace_bytes(int64_t B, int64_t T, int64_t d) {
+  if (check_mlgru_train(B, T, d) != MMF_OK) return 0;
+  return mlgru_train_scratch(B, T, d, 2).dlb_off;
+}
+
+int mmf_mlgru_train_scan(const float* z, const float* lb, const float* h0, float* o_prime, float* h_last,
+                         void* states, size_t states_bytes, int64_t B, int64_t T, int64_t d, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_mlgru_train(B, T, d)) return st;
+  if (B == 0 || T == 0) return MMF_OK;
+  if (!z || !o_prime || !states) return MMF_ERR_NULL;
+  if (!aligned16(z) || !aligned16_or_null(lb) || !aligned16_or_null(h0) || !aligned16(o_prime) ||
+      !aligned16_or_null(h_last))
+    return MMF_ERR_ALIGN;
+  if (!states_fit(states, states_bytes, B, T, d)) return MMF_ERR_WORKSPACE;
+  const size_t need = mlgru_train_scratch(B, T, d, 2).dlb_off;
+  return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
+    return hip_status(mmf::launch_mlgru_train_scan({z, lb, h0, B, T, d}, o_prime, h_last, static_cast<float*>(states),
+                                                   reinterpret_cast<float*>(scratch), stream));
+  });
+}
+
+size_t mmf_mlgru_scan_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d) {
+  if (check_mlgru_train(B, T, d) != MMF_OK) return 0;
+  return mlgru_train_scratch(B, T, d, 3).total;
+}
+
+int mmf_mlgru_scan_bwd(const float* z, const float* lb, const void* states, size_t states_bytes,
+                       const void* do_prime, int do_is_f32, const float* dh_last, uint16_t* dz, float* dh0,
+                       float* dlb, int64_t B, int64_t T, int64_t d, void* workspace, size_t workspace_bytes,
+                       hipStream_t stream) {
+  if (int st = check_dtype(do_is_f32)) return st;
+  if (int st = check_mlgru_train(B, T, d)) return st;
+  if (B == 0 || T == 0) return MMF_OK;
+  if (!z || !states || !do_prime || !dz) return MMF_ERR_NULL;
+  if (!aligned16(z) || !aligned16_or_null(lb) || !aligned16(do_prime) || !aligned16_or_null(dh_last) ||
+      !aligned16(dz) || !aligned16_or_null(dh0) || !aligned16_or_null(dlb))
+    return MMF_ERR_ALIGN;
+  if (!states_fit(states, states_bytes, B, T, d)) return MMF_ERR_WORKSPACE;
+  const MlgruTrainScratch s = mlgru_train_scratch(B, T, d, 3);
+  return with_workspace(workspace, workspace_bytes, dlb ? s.total : s.dlb_off, stream, [&](char* scratch) {
+    double* part = dlb ? reinterpret_cast<double*>(scratch + s.dlb_off) : nullptr;
+    if (mmf::launch_mlgru_scan_bwd({z, lb, nullptr, B, T, d}, static_cast<const float*>(states), do_prime,
+                                   do_is_f32 == 1, dh_last, dz, dh0, reinterpret_cast<float*>(scratch), part,
+                                   stream) != hipSuccess)
+      return MMF_ERR_HIP;
+    return hip_status(mmf::launch_col_final({part, B * mmf::mlgru_train_chunks(T), d, dlb}, {}, stream));
+  });
+}
+
 size_t mmf_mlgru_workspace_bytes(int64_t B, int64_t T, int64_t d) {
   if (check_mlgru_d(d) != MMF_OK || B < 0 || T < 0 || (T > 0 && B > kMaxMN / T)) return 0;
   return mlgru_scratch(B, T, d).total;
@@ -966,6 +1063,37 @@ int mmf_bitlinear_bwd(const uint16_t* dO, const void* x, int x_is_f32, const flo
       return MMF_ERR_HIP;
     return MMF_OK;
   });
+}
+
+size_t mmf_grad_norm_workspace_bytes(const int64_t* counts, int64_t n) {
+  if (check_grads(nullptr, nullptr, counts, n, false) != MMF_OK) return 0;
+  return round_up(sizeof(double) * static_cast<size_t>(mmf::grad_pieces(counts, n)), kScratchAlign);
+}
+
+int mmf_grad_norm(const void* const* grads, const int* is_f32, const int64_t* counts, int64_t n, float* norm,
+                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_grads(grads, is_f32, counts, n, true)) return st;
+  if (!norm) return MMF_ERR_NULL;
+  if (!aligned16(norm)) return MMF_ERR_ALIGN;
+  const size_t need = round_up(sizeof(double) * static_cast<size_t>(mmf::grad_pieces(counts, n)), kScratchAlign);
+  return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
+    return hip_status(
+        mmf::launch_grad_norm({grads, nullptr, is_f32, counts, n}, norm, reinterpret_cast<double*>(scratch), stream));
+  });
+}
+
+int mmf_grad_clip(const void* const* grads, const int* is_f32, const int64_t* counts, int64_t n, const float* norm,
+                  float max_norm, void* const* outs, hipStream_t stream) {
+  if (int st = check_grads(grads, is_f32, counts, n, true)) return st;
+  if (!(max_norm >= 0.0f)) return MMF_ERR_ARG;
+  if (!norm || (n > 0 && !outs)) return MMF_ERR_NULL;
+  if (!aligned16(norm)) return MMF_ERR_ALIGN;
+  for (int64_t i = 0; i < n; ++i) {
+    if (counts[i] == 0) continue;
+    if (!outs[i]) return MMF_ERR_NULL;
+    if (!aligned16(outs[i])) return MMF_ERR_ALIGN;
+  }
+  return hip_status(mmf::launch_grad_clip({grads, outs, is_f32, counts, n}, norm, max_norm, stream));
 }
 
 int mmf_set_path(int path) {

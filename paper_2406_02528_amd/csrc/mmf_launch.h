@@ -199,6 +199,46 @@ int64_t mlgru_scan_ws_floats(int64_t B, int64_t T, int64_t d);
 hipError_t launch_mlgru_scan(const float* fcg, const float* h0, float* o, float* h_last, int64_t B,
                              int64_t T, int64_t d, float* ws, hipStream_t stream);
 
+// The recurrence in training form (mlgru_train.hip), from the gates'
+// pre-activations z [B*T][3d] and the forget gate's lower bound lb (nullptr:
+// 0): o', the last state (h_last, nullptr: not stored; may be h0) and the
+// states entering the chunks of tokens, [B][mlgru_train_chunks(T)][d].
+// ws: 2 B nchunk d floats where nchunk > 1.  T >= 1, d % 16 == 0,
+// mlgru_train_blocks (workgroups) below 2^22.
+struct MlgruTrainArgs {
+  const float* z;
+  const float* lb;
+  const float* h0;
+  int64_t B, T, d;
+};
+int64_t mlgru_train_chunks(int64_t T);
+int64_t mlgru_train_blocks(int64_t B, int64_t T, int64_t d);
+hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_last, float* states, float* ws,
+                                   hipStream_t stream);
+// Its backward (h0 of `p` is not read): dz bf16 [B*T][3d], dh0 [B][d]
+// (nullptr: not stored) and the partial sums of lb's gradient
+// [B nchunk][d] (nullptr: not computed) from the gradient of o' and of the
+// last state (nullptr: 0).  ws: 3 B nchunk d floats where nchunk > 1.
+hipError_t launch_mlgru_scan_bwd(const MlgruTrainArgs& p, const float* states, const void* dout, bool dout_is_f32,
+                                 const float* dh_last, uint16_t* dz, float* dh0, float* ws, double* dlb_part,
+                                 hipStream_t stream);
+
+// The norm of a set of gradients and the set scaled to it (grad_norm.hip).
+// The arrays of addresses, types and sizes are host memory; partials holds
+// grad_pieces(counts, n) doubles; counts at most kGradMaxCount; dst for
+// launch_grad_clip only, dst[i] may be src[i].
+constexpr int64_t kGradMaxCount = int64_t(1) << 36;
+struct GradSetArgs {
+  const void* const* src;
+  void* const* dst;
+  const int* is_f32;
+  const int64_t* counts;
+  int64_t n;
+};
+int64_t grad_pieces(const int64_t* counts, int64_t n);
+hipError_t launch_grad_norm(const GradSetArgs& a, float* norm, double* partials, hipStream_t stream);
+hipError_t launch_grad_clip(const GradSetArgs& a, const float* norm, float max_norm, hipStream_t stream);
+
 // ---- backward (bwd.hip: final sums; bwd_gemm.hip: the two products) ----
 // out[c] = sum over p < nparts of partials[p * cols + c] (fp64, fixed order);
 // an array with a null `out` is left out.
