@@ -934,7 +934,7 @@ int64_t bwd_dy_row_slice(int64_t Np, int64_t K) {
   // one launch stay below 2^31 bytes; slices are whole row tiles
   const int64_t lim = (int64_t(1) << 31) - 1;
   if (((Np + 15) / 16) * K * 4 > lim) return 0;
-  int64_t rows = lim / (2 * Np);
+  int64_t rows = lim / (Np > 0 ? 2 * Np : 1);
   rows = rows / 128 * 128;
   return rows;
 }

@@ -440,12 +440,13 @@ BwdScratch bwd_scratch(int64_t M, int64_t K, int64_t N) {
 }
 
 // Shapes the backward's kernels address with 32-bit offsets: the n-major
-// codes and the dY launch's dO rows (bwd_dy_row_slice), dW [N][K] and the
-// token counts.
+// codes and the dY launch's dO rows (bwd_dy_row_slice), dW [N][K], the dO rows
+// of the smallest part of dW's token range (one row and two stages of 64) and
+// the token counts.
 int check_bwd_shape(int64_t M, int64_t K, int64_t N) {
   const int64_t lim = (int64_t(1) << 31) - 1;
   const int64_t Np = (N + 7) / 8 * 8;
-  if (mmf::bwd_dy_row_slice(Np, K) == 0 || N * K * 4 > lim || M > lim) return MMF_ERR_SHAPE;
+  if (mmf::bwd_dy_row_slice(Np, K) == 0 || 129 * 2 * Np > lim || N * K * 4 > lim || M > lim) return MMF_ERR_SHAPE;
   return MMF_OK;
 }
 
