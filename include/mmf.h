@@ -485,6 +485,51 @@ int mmf_bitlinear_bwd(const uint16_t *dO, const void *x, int x_is_f32, const flo
                       void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * The GLU channel mixer's training form: the gated up-projections p = SiLU(g)
+ * (.) u of two layers g, u that are trained together, their latent weights
+ * stacked in W [2L][K] float32 (gate rows, then up rows) and ternarised
+ * jointly (one w_scale).  L must be a multiple of 16.
+ *
+ * mmf_glu_train_fwd starts from quantised activations (q, a_scale, q_rowsum
+ * of mmf_act_quant_ex, or of mmf_add_act_quant, which also gives the rstd
+ * that the backward needs):
+ *   Wpacked [K/16][2L], w_scale [1]  as mmf_ternarize_weights(W)
+ *   p [M][L] float32                 as mmf_ternary_gemm_glu with them
+ *
+ * mmf_glu_gate_bwd is the stage between p and the two layers: both
+ * projections again from q and the packed weights, never stored, and in the
+ * same kernel, with s = sigmoid(g) (as for mmf_glu_fwd; fp32, rounded once),
+ *   du = dp g s,   dg = dp u s (1 + g (1 - s))
+ * into dgu [M][2L] bf16 (dg | du), the dO of mmf_bitlinear_bwd for the
+ * stacked layers.  dp [M][L] bf16 bits or float32 (dp_is_f32), the gradient of
+ * p (float32 as mmf_bitlinear_bwd of the down-projection leaves it);
+ * Wgu_packed [K/16][2L] interleaved by mmf_glu_pack, w_scales [2]: gate, up.
+ * Allocates nothing.
+ *
+ * mmf_glu_bwd is the whole backward: that stage, then mmf_bitlinear_bwd of the
+ * stacked layers with N = 2L (the same kernels, so the results of the two
+ * calls): dx [M][K], dW [2L][K] and dgamma [K] (or NULL) from dp, the layers'
+ * input x with gamma, rstd, q, a_scale and q_rowsum, and the forward's Wpacked
+ * and w_scale.  Shape limits of mmf_ternary_gemm_glu and of mmf_bitlinear_bwd.
+ * M == 0 or L == 0 is a no-op.  Workspace as for the latter.
+ */
+size_t mmf_glu_train_workspace_bytes(int64_t M, int64_t K, int64_t L);
+int mmf_glu_train_fwd(const int8_t *q, const float *a_scale, const int32_t *q_rowsum,
+                      const float *W, float *p, uint32_t *Wpacked, float *w_scale, int64_t M,
+                      int64_t K, int64_t L, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+int mmf_glu_gate_bwd(const int8_t *q, const float *a_scale, const int32_t *q_rowsum,
+                     const uint32_t *Wgu_packed, const float *w_scales, const void *dp,
+                     int dp_is_f32, uint16_t *dgu, int64_t M, int64_t K, int64_t L,
+                     hipStream_t stream);
+size_t mmf_glu_bwd_workspace_bytes(int64_t M, int64_t K, int64_t L);
+int mmf_glu_bwd(const void *dp, int dp_is_f32, const void *x, int x_is_f32, const float *gamma,
+                const float *rstd, const int8_t *q, const float *a_scale,
+                const int32_t *q_rowsum, const uint32_t *Wpacked, const float *w_scale,
+                float *dx, float *dW, float *dgamma, int64_t M, int64_t K, int64_t L,
+                void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * The norm over all elements of a set of gradients, and the set scaled to it:
  *   norm = sqrt(sum_i sum g_i^2)            (squares and sums in fp64)
  *   out_i = g_i min(max_norm / (norm + 1e-6), 1)    (fp32, rounded to g_i's type)

@@ -91,6 +91,12 @@ _SIGNATURES = {
     "mmf_mlgru_scan_bwd_workspace_bytes": ([_I64, _I64, _I64], _SZ),
     "mmf_mlgru_scan_bwd": ([_P, _P, _P, _SZ, _P, ctypes.c_int, _P, _P, _P, _P, _I64, _I64, _I64, _P, _SZ, _P],
                            ctypes.c_int),
+    "mmf_glu_train_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+    "mmf_glu_train_fwd": ([_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _P, _SZ, _P], ctypes.c_int),
+    "mmf_glu_gate_bwd": ([_P, _P, _P, _P, _P, _P, ctypes.c_int, _P, _I64, _I64, _I64, _P], ctypes.c_int),
+    "mmf_glu_bwd_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+    "mmf_glu_bwd": ([_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _P,
+                     _SZ, _P], ctypes.c_int),
     "mmf_grad_norm_workspace_bytes": ([_P, _I64], _SZ),
     "mmf_grad_norm": ([_P, _P, _P, _I64, _P, _P, _SZ, _P], ctypes.c_int),
     "mmf_grad_clip": ([_P, _P, _P, _I64, _P, ctypes.c_float, _P, _P], ctypes.c_int),
@@ -631,6 +637,84 @@ def mmf_mlgru_scan_bwd(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None,
     wp, wn = _ws_args(workspace)
     _check(_lib.mmf_mlgru_scan_bwd(_ptr(z), _ptr(lb), _ptr(states), states.numel(), _ptr(do_prime), do_f32,
                                    _ptr(dh_last), _ptr(dz), _ptr(dh0), _ptr(dlb), B, T, d, wp, wn, _stream(stream)))
+
+
+def mmf_glu_train_workspace_bytes(M: int, K: int, L: int) -> int:
+    return int(_lib.mmf_glu_train_workspace_bytes(M, K, L))
+
+
+def mmf_glu_bwd_workspace_bytes(M: int, K: int, L: int) -> int:
+    return int(_lib.mmf_glu_bwd_workspace_bytes(M, K, L))
+
+
+def mmf_glu_train_fwd(q: torch.Tensor, a_scale: torch.Tensor, q_rowsum: torch.Tensor, W: torch.Tensor,
+                      p: torch.Tensor, Wpacked: torch.Tensor, w_scale: torch.Tensor,
+                      workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Training forward of the GLU's gated up-projections from quantised
+    activations and the stacked latent weights W f32 [2L][K] (gate, up): p f32
+    [M][L], and Wpacked int32 [K/16][2L] and w_scale f32 [1] for the backward."""
+    M, K = q.shape
+    L = W.shape[0] // 2
+    _need_here(q, "q", torch.int8, (M, K))
+    _need_here(a_scale, "a_scale", torch.float32, (M,))
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
+    _need_here(W, "W", torch.float32, (2 * L, K))
+    _need_here(p, "p", torch.float32, (M, L))
+    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L))
+    _need_here(w_scale, "w_scale", torch.float32, (1,))
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_glu_train_fwd(_ptr(q), _ptr(a_scale), _ptr(q_rowsum), _ptr(W), _ptr(p), _ptr(Wpacked),
+                                  _ptr(w_scale), M, K, L, wp, wn, _stream(stream)))
+
+
+def mmf_glu_gate_bwd(q: torch.Tensor, a_scale: torch.Tensor, q_rowsum: torch.Tensor, Wgu_packed: torch.Tensor,
+                     w_scales: torch.Tensor, dp: torch.Tensor, dgu: torch.Tensor, stream=None) -> None:
+    """The GLU gate's gradients dgu bf16 [M][2L] (dg | du) from dp bf16/f32
+    [M][L], the projections recomputed from the quantised activations and the
+    interleaved packed weights [K/16][2L] with w_scales [gate, up]."""
+    M, K = q.shape
+    L = Wgu_packed.shape[1] // 2
+    dp_f32 = _kind(dp, "dp")
+    _need_here(q, "q", torch.int8, (M, K))
+    _need_here(a_scale, "a_scale", torch.float32, (M,))
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
+    _need_here(Wgu_packed, "Wgu_packed", torch.int32, (K // 16, 2 * L))
+    _need_here(w_scales, "w_scales", torch.float32, (2,))
+    _need_here(dp, "dp", dp.dtype, (M, L))
+    _need_here(dgu, "dgu", torch.bfloat16, (M, 2 * L))
+    _check(_lib.mmf_glu_gate_bwd(_ptr(q), _ptr(a_scale), _ptr(q_rowsum), _ptr(Wgu_packed), _ptr(w_scales), _ptr(dp),
+                                 dp_f32, _ptr(dgu), M, K, L, _stream(stream)))
+
+
+def mmf_glu_bwd(dp: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, rstd: torch.Tensor, q: torch.Tensor,
+                a_scale: torch.Tensor, q_rowsum: torch.Tensor, Wpacked: torch.Tensor, w_scale: torch.Tensor,
+                dx: torch.Tensor, dW: torch.Tensor, dgamma: torch.Tensor | None,
+                workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Backward of the GLU's gated up-projections: dx f32 [M][K], dW f32
+    [2L][K] (gate, up) and dgamma f32 [K] (or None) from dp bf16/f32 [M][L], the
+    input x bf16/f32 [M][K] with gamma, rstd, q, a_scale and q_rowsum, and
+    mmf_glu_train_fwd's Wpacked and w_scale."""
+    M, K = x.shape
+    L = Wpacked.shape[1] // 2
+    is_f32, dp_f32 = _x_kind(x), _kind(dp, "dp")
+    _need_here(dp, "dp", dp.dtype, (M, L))
+    _need_here(x, "x", x.dtype, (M, K))
+    if gamma is not None:
+        _need_here(gamma, "gamma", torch.float32, (K,))
+    _need_here(rstd, "rstd", torch.float32, (M,))
+    _need_here(q, "q", torch.int8, (M, K))
+    _need_here(a_scale, "a_scale", torch.float32, (M,))
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
+    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L))
+    _need_here(w_scale, "w_scale", torch.float32, (1,))
+    _need_here(dx, "dx", torch.float32, (M, K))
+    _need_here(dW, "dW", torch.float32, (2 * L, K))
+    if dgamma is not None:
+        _need_here(dgamma, "dgamma", torch.float32, (K,))
+    wp, wn = _ws_args(workspace)
+    _check(_lib.mmf_glu_bwd(_ptr(dp), dp_f32, _ptr(x), is_f32, _ptr(gamma), _ptr(rstd), _ptr(q), _ptr(a_scale),
+                            _ptr(q_rowsum), _ptr(Wpacked), _ptr(w_scale), _ptr(dx), _ptr(dW), _ptr(dgamma), M, K, L,
+                            wp, wn, _stream(stream)))
 
 
 def _grad_set(tensors, name):

@@ -57,6 +57,7 @@
 #include "gemm_common.h"
 #include "mmf_device.h"
 #include "mmf_launch.h"
+#include "row_vec.h"
 
 namespace mmf {
 namespace {
@@ -312,7 +313,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   // other workgroup's epilogue on the same SIMD (its SiLU arithmetic and
   // direct stores), which keeps the matrix cores fed (glu_gate 4-5 % faster;
   // the dequantising epilogue measured level and keeps the default).
-  constexpr bool kLoopPriority = T::kWaves == 4 && EP == Epilogue::kGluF32;
+  constexpr bool kLoopPriority =
+      T::kWaves == 4 && (EP == Epilogue::kGluF32 || EP == Epilogue::kGluGradF32 || EP == Epilogue::kGluGradBf16);
   if constexpr (kLoopPriority) __builtin_amdgcn_s_setprio(1);
   // Prologue: stages 0 .. S-2, wait for stage 0 (and the row factors).
 #pragma unroll
@@ -393,8 +395,9 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   const int el16 = elane & 15, eg = elane >> 4;
   const int* s_rsum = reinterpret_cast<const int*>(smem + S * T::kStageBytes);
   const float* s_scale = reinterpret_cast<const float*>(smem + S * T::kStageBytes + 4 * BM);
-  const float ws = (EP == Epilogue::kDequantF32 || EP == Epilogue::kGluF32) ? w_scale[0] : 0.0f;
-  const float ws_u = (EP == Epilogue::kGluF32) ? w_scale[1] : 0.0f;
+  constexpr bool kGluGrad = EP == Epilogue::kGluGradF32 || EP == Epilogue::kGluGradBf16;
+  const float ws = (EP == Epilogue::kDequantF32 || EP == Epilogue::kGluF32 || kGluGrad) ? w_scale[0] : 0.0f;
+  const float ws_u = (EP == Epilogue::kGluF32 || kGluGrad) ? w_scale[1] : 0.0f;
   __syncthreads();
   constexpr uint32_t kOut = kOutOfRange;
   // affine epilogue: bias, lower bound, scale and activation of the lane's
@@ -447,7 +450,60 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   constexpr bool kStaged = BX4 && (EP == Epilogue::kDequantF32 || EP == Epilogue::kRawI32);
   static_assert(!RAG || kStaged, "ragged rows leave through the staged stores");
   static_assert(!BIAS || (kStaged && !RAG && EP == Epilogue::kDequantF32), "the bias is added at the staged stores");
-  if constexpr (!kStaged) {
+  if constexpr (kGluGrad) {
+    // The gate's gradients.  With s = sigmoid(g) and dp the gradient of
+    // p = g s u:  du = dp g s,  dg = dp u s (1 + g (1 - s)),  fp32, each
+    // rounded once to bf16.  g and u carry the bits of the forward.
+    static_assert(BX4 && !RAG && !BIAS, "L % 16 == 0");
+    constexpr int kDp = EP == Epilogue::kGluGradF32 ? 4 : 2;  // bytes of a gradient
+    const uint32_t L = static_cast<uint32_t>(N) / 2;
+    const __amdgpu_buffer_rsrc_t grsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<void*>(aff.grad), 0, static_cast<int>(static_cast<uint32_t>(M) * L * kDp), kBufferFlags);
+    const __amdgpu_buffer_rsrc_t orsrc = __builtin_amdgcn_make_buffer_rsrc(
+        out, 0, static_cast<int>(static_cast<uint32_t>(M) * L * 4u), kBufferFlags);
+#pragma unroll
+    for (int fm = 0; fm < FM; ++fm) {
+      const int lr = wm * WM + fm * 16 + el16;
+      const bool row_ok = m0 + lr < M;
+      const uint32_t row = static_cast<uint32_t>(m0 + lr) * L;
+      const int rs = s_rsum[lr];
+      const float sg = s_scale[lr] * ws, su = s_scale[lr] * ws_u;
+#pragma unroll
+      for (int f = 0; f < FN / 2; ++f) {
+        const uint32_t ch = static_cast<uint32_t>((n0 + wn * WN) / 2 + f * 16 + 4 * eg);
+        const bool ok = row_ok && ch < L;
+        float dp[4];
+        if constexpr (kDp == 4) {
+          const v4f v = __builtin_bit_cast(
+              v4f, __builtin_amdgcn_raw_buffer_load_b128(grsrc, ok ? 4u * (row + ch) : kOut, 0, 0));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dp[r] = v[r];
+        } else {
+          const uint2 v = __builtin_bit_cast(
+              uint2, __builtin_amdgcn_raw_buffer_load_b64(grsrc, ok ? 2u * (row + ch) : kOut, 0, 0));
+          dp[0] = bf16_lo(v.x);
+          dp[1] = bf16_hi(v.x);
+          dp[2] = bf16_lo(v.y);
+          dp[3] = bf16_hi(v.y);
+        }
+        float dg[4], du[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float gv = static_cast<float>(acc[fm][2 * f][r] - rs) * sg;
+          const float uv = static_cast<float>(acc[fm][2 * f + 1][r] - rs) * su;
+          const float s = sigmoid_hw(gv);
+          du[r] = dp[r] * (gv * s);
+          dg[r] = dp[r] * uv * (s * (1.0f + gv * (1.0f - s)));
+        }
+        const uint32_t at = 2u * (2u * row + ch);
+        typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3])}, orsrc,
+                                              ok ? at : kOut, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3])}, orsrc,
+                                              ok ? at + 2u * L : kOut, 0, 0);
+      }
+    }
+  } else if constexpr (!kStaged) {
     const int ow = kGlu ? N / 2 : N;  // output row length
     const uint32_t out_bytes = static_cast<uint32_t>(M) * static_cast<uint32_t>(ow) * 4u;
     const __amdgpu_buffer_rsrc_t orsrc =
@@ -602,6 +658,21 @@ hipError_t launch_cfg(const ContractArgs& a, int64_t m_begin, int64_t m_rows, hi
                          static_cast<int>(m_rows), a.K, static_cast<int>(a.N), a.affine);
     else
       return hipErrorInvalidValue;
+  } else if (is_glu_grad(a.epilogue)) {
+    if constexpr (BX4) {
+      const bool f32 = a.epilogue == Epilogue::kGluGradF32;
+      Affine aff;
+      aff.grad = static_cast<const char*>(a.affine.grad) + m_begin * (a.N / 2) * (f32 ? 4 : 2);
+      void* out = static_cast<uint16_t*>(a.out) + m_begin * a.N;
+      if (f32)
+        hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, BK, S, true, Epilogue::kGluGradF32>), grid, block, 0, stream, q,
+                           as, rs, a.Wpacked, a.w_scale, out, static_cast<int>(m_rows), a.K, static_cast<int>(a.N), aff);
+      else
+        hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, BK, S, true, Epilogue::kGluGradBf16>), grid, block, 0, stream, q,
+                           as, rs, a.Wpacked, a.w_scale, out, static_cast<int>(m_rows), a.K, static_cast<int>(a.N), aff);
+    } else {
+      return hipErrorInvalidValue;
+    }
   } else
     hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, BK, S, BX4, Epilogue::kRawI32>), grid, block, 0,
                        stream, q, as, rs, a.Wpacked, a.w_scale,

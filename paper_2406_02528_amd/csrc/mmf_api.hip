@@ -450,6 +450,100 @@ int check_bwd_shape(int64_t M, int64_t K, int64_t N) {
   return MMF_OK;
 }
 
+// The backward on its scratch (laid out by bwd_scratch).
+struct BwdCall {
+  const uint16_t* dO;
+  const void* x;
+  bool x_is_f32;
+  const float* gamma;
+  const float* rstd;
+  const int8_t* q;
+  const float* a_scale;
+  const uint32_t* Wpacked;
+  const float* w_scale;
+  float *dx, *dW, *db, *dgamma;
+  int64_t M, K, N;
+};
+int run_bwd(const BwdCall& c, const BwdScratch& s, char* scratch, hipStream_t stream) {
+  const auto& [dO, x, x_f32, gamma, rstd, q, a_scale, Wpacked, w_scale, dx, dW, db, dgamma, M, K, N] = c;
+  uint32_t* Wn = reinterpret_cast<uint32_t*>(scratch + s.wn_off);
+  double* s_part = reinterpret_cast<double*>(scratch + s.spart_off);
+  double* dg_part = dgamma ? reinterpret_cast<double*>(scratch + s.dgpart_off) : nullptr;
+  const int Ki = static_cast<int>(K);
+  const bool f32 = x_f32;
+  // dO rows in 16-byte chunks: zero-padded copy when N % 8 != 0
+  const uint16_t* dOp = dO;
+  if (s.Np != N) {
+    uint16_t* pad = reinterpret_cast<uint16_t*>(scratch + s.dop_off);
+    if (mmf::launch_pad_rows(dO, M, N, s.Np, pad, stream) != hipSuccess) return MMF_ERR_HIP;
+    dOp = pad;
+  }
+  // dY = dO Wt^T with r gamma dY into dx and the row / column partials,
+  // then dx and dgamma finished
+  if (mmf::launch_pack_nmajor(Wpacked, N, s.Np, Ki, Wn, stream) != hipSuccess) return MMF_ERR_HIP;
+  double* db_part = db ? reinterpret_cast<double*>(scratch + s.dbpart_off) : nullptr;
+  const mmf::DyArgs dy{dOp, M, N, s.Np, Wn, w_scale, x, f32, gamma, rstd, Ki, dx, s_part, dg_part, db_part};
+  if (mmf::launch_dy(dy, s.dy, stream) != hipSuccess) return MMF_ERR_HIP;
+  if (mmf::launch_dx_finish(dx, x, f32, rstd, s_part, s.dy.col_tiles, M, Ki, stream) != hipSuccess)
+    return MMF_ERR_HIP;
+  // dW = dO^T Yq (token range split into parts when the output has few
+  // tiles; the last partial round of tiles spread over all CUs otherwise)
+  const int64_t S = s.plan.split_all;
+  float* dw_out = S > 1 ? reinterpret_cast<float*>(scratch + s.dw_off) : dW;
+  float* parts = s.plan.tail_units > 0 ? reinterpret_cast<float*>(scratch + s.parts_off) : nullptr;
+  if (mmf::launch_dw(dOp, q, a_scale, M, s.Np, N, Ki, dw_out, parts, s.plan, stream) != hipSuccess)
+    return MMF_ERR_HIP;
+  if (S > 1 && mmf::launch_sum_parts(dw_out, S, N * K, dW, stream) != hipSuccess) return MMF_ERR_HIP;
+  if (mmf::launch_col_final({dg_part, s.dy.row_tiles, K, dgamma}, {db_part, s.dy.row_tiles, N, db}, stream) !=
+      hipSuccess)
+    return MMF_ERR_HIP;
+  return MMF_OK;
+}
+
+// ---- the GLU channel mixer in training form ----
+int check_glu_train(int64_t M, int64_t K, int64_t L) {
+  if (L < 0 || L > kMaxMN / 2 || (L % 16) != 0) return MMF_ERR_SHAPE;
+  if (int st = check_shape(M, K, 2 * L)) return st;
+  return M == 0 || L == 0 ? MMF_OK : check_gemm(K, 2 * L);
+}
+// The gate's gradients from the recomputed projections.
+hipError_t glu_gate_bwd(const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wgu,
+                        const float* w_scales, const void* dp, bool dp_is_f32, uint16_t* dgu, int64_t M, int64_t K,
+                        int64_t L, hipStream_t stream) {
+  mmf::Affine aff;
+  aff.grad = dp;
+  return mmf::launch_gemm({q, a_scale, q_rowsum, Wgu, w_scales, dgu, M, static_cast<int>(K), 2 * L,
+                           dp_is_f32 ? mmf::Epilogue::kGluGradF32 : mmf::Epilogue::kGluGradBf16, aff},
+                          stream);
+}
+// Scratch: the interleaved weights and their two scales, then (forward) the
+// ternarisation's partial sums or (backward) the gate's gradients [M][2L] and
+// the layers' own backward's scratch.
+struct GluPacked {
+  size_t scales_off, end;
+};
+GluPacked glu_packed(int64_t K, int64_t L) {
+  GluPacked g;
+  g.scales_off = round_up(static_cast<size_t>(K / 16) * static_cast<size_t>(2 * L) * 4, kScratchAlign);
+  g.end = g.scales_off + kScratchAlign;
+  return g;
+}
+size_t glu_fwd_bytes(int64_t K, int64_t L) {
+  return glu_packed(K, L).end +
+         round_up(sizeof(double) * static_cast<size_t>(mmf::ternarize_partials_count(2 * L * K)), kScratchAlign);
+}
+struct GluBwdScratch {
+  BwdScratch bwd;
+  size_t bwd_off, total;
+};
+GluBwdScratch glu_bwd_scratch(int64_t M, int64_t K, int64_t L) {
+  GluBwdScratch s;
+  s.bwd = bwd_scratch(M, K, 2 * L);
+  s.bwd_off = glu_packed(K, L).end + round_up(static_cast<size_t>(M) * static_cast<size_t>(2 * L) * 2, kScratchAlign);
+  s.total = s.bwd_off + s.bwd.total;
+  return s;
+}
+
 // ---- the forward without allocation (mmf_bitlinear_fwd_noalloc) ----
 //
 // Its scratch (q, a_scale, q_rowsum: fwd_scratch) lives in a file-scope
@@ -704,7 +798,7 @@ int mmf_glu_pack(const uint32_t* Wg_packed, const uint32_t* Wu_packed, int64_t L
   if (L == 0) return MMF_OK;
   if (!Wg_packed || !Wu_packed || !Wgu_packed) return MMF_ERR_NULL;
   if (!aligned16(Wg_packed) || !aligned16(Wu_packed) || !aligned16(Wgu_packed)) return MMF_ERR_ALIGN;
-  return hip_status(mmf::launch_glu_pack(Wg_packed, Wu_packed, L, static_cast<int>(K), Wgu_packed, stream));
+  return hip_status(mmf::launch_glu_pack(Wg_packed, Wu_packed, L, L, static_cast<int>(K), Wgu_packed, nullptr, nullptr, stream));
 }
 
 int mmf_glu_fwd(const uint16_t* x, const float* gamma, const uint32_t* Wgu_packed,
@@ -1031,38 +1125,85 @@ int mmf_bitlinear_bwd(const uint16_t* dO, const void* x, int x_is_f32, const flo
     return MMF_ERR_ALIGN;
   const BwdScratch s = bwd_scratch(M, K, N);
   return with_workspace(workspace, workspace_bytes, s.total, stream, [&](char* scratch) {
-    uint32_t* Wn = reinterpret_cast<uint32_t*>(scratch + s.wn_off);
-    double* s_part = reinterpret_cast<double*>(scratch + s.spart_off);
-    double* dg_part = dgamma ? reinterpret_cast<double*>(scratch + s.dgpart_off) : nullptr;
+    return run_bwd({dO, x, x_is_f32 == 1, gamma, rstd, q, a_scale, Wpacked, w_scale, dx, dW, db, dgamma, M, K, N}, s,
+                   scratch, stream);
+  });
+}
+
+size_t mmf_glu_train_workspace_bytes(int64_t M, int64_t K, int64_t L) {
+  if (check_glu_train(M, K, L) != MMF_OK) return 0;
+  return glu_fwd_bytes(K, L);
+}
+
+int mmf_glu_train_fwd(const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const float* W, float* p,
+                      uint32_t* Wpacked, float* w_scale, int64_t M, int64_t K, int64_t L, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream) {
+  const int path = current_path();
+  if (int st = check_glu_train(M, K, L)) return st;
+  if (M == 0 || L == 0) return MMF_OK;
+  if (!q || !a_scale || !q_rowsum || !W || !p || !Wpacked || !w_scale) return MMF_ERR_NULL;
+  if (!aligned16(q) || !aligned16(a_scale) || !aligned16(q_rowsum) || !aligned16(W) || !aligned16(p) ||
+      !aligned16(Wpacked))
+    return MMF_ERR_ALIGN;
+  const GluPacked g = glu_packed(K, L);
+  return with_workspace(workspace, workspace_bytes, glu_fwd_bytes(K, L), stream, [&](char* scratch) {
     const int Ki = static_cast<int>(K);
-    const bool f32 = x_is_f32 == 1;
-    // dO rows in 16-byte chunks: zero-padded copy when N % 8 != 0
-    const uint16_t* dOp = dO;
-    if (s.Np != N) {
-      uint16_t* pad = reinterpret_cast<uint16_t*>(scratch + s.dop_off);
-      if (mmf::launch_pad_rows(dO, M, N, s.Np, pad, stream) != hipSuccess) return MMF_ERR_HIP;
-      dOp = pad;
-    }
-    // dY = dO Wt^T with r gamma dY into dx and the row / column partials,
-    // then dx and dgamma finished
-    if (mmf::launch_pack_nmajor(Wpacked, N, s.Np, Ki, Wn, stream) != hipSuccess) return MMF_ERR_HIP;
-    double* db_part = db ? reinterpret_cast<double*>(scratch + s.dbpart_off) : nullptr;
-    const mmf::DyArgs dy{dOp, M, N, s.Np, Wn, w_scale, x, f32, gamma, rstd, Ki, dx, s_part, dg_part, db_part};
-    if (mmf::launch_dy(dy, s.dy, stream) != hipSuccess) return MMF_ERR_HIP;
-    if (mmf::launch_dx_finish(dx, x, f32, rstd, s_part, s.dy.col_tiles, M, Ki, stream) != hipSuccess)
+    uint32_t* Wgu = reinterpret_cast<uint32_t*>(scratch);
+    float* scales = reinterpret_cast<float*>(scratch + g.scales_off);
+    if (mmf::launch_ternarize(W, 2 * L, Ki, Wpacked, w_scale, reinterpret_cast<double*>(scratch + g.end),
+                              stream) != hipSuccess ||
+        mmf::launch_glu_pack(Wpacked, Wpacked + L, 2 * L, L, Ki, Wgu, w_scale, scales, stream) != hipSuccess)
       return MMF_ERR_HIP;
-    // dW = dO^T Yq (token range split into parts when the output has few
-    // tiles; the last partial round of tiles spread over all CUs otherwise)
-    const int64_t S = s.plan.split_all;
-    float* dw_out = S > 1 ? reinterpret_cast<float*>(scratch + s.dw_off) : dW;
-    float* parts = s.plan.tail_units > 0 ? reinterpret_cast<float*>(scratch + s.parts_off) : nullptr;
-    if (mmf::launch_dw(dOp, q, a_scale, M, s.Np, N, Ki, dw_out, parts, s.plan, stream) != hipSuccess)
+    const mmf::ContractArgs a{q, a_scale, q_rowsum, Wgu, scales, p, M, Ki, 2 * L, mmf::Epilogue::kGluF32};
+    return hip_status(contract_mfma(path, a, stream));
+  });
+}
+
+int mmf_glu_gate_bwd(const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wgu_packed,
+                     const float* w_scales, const void* dp, int dp_is_f32, uint16_t* dgu, int64_t M, int64_t K,
+                     int64_t L, hipStream_t stream) {
+  if (int st = check_dtype(dp_is_f32)) return st;
+  if (int st = check_glu_train(M, K, L)) return st;
+  if (M == 0 || L == 0) return MMF_OK;
+  if (!q || !a_scale || !q_rowsum || !Wgu_packed || !w_scales || !dp || !dgu) return MMF_ERR_NULL;
+  if (!aligned16(q) || !aligned16(a_scale) || !aligned16(q_rowsum) || !aligned16(Wgu_packed) || !aligned16(dp) ||
+      !aligned16(dgu))
+    return MMF_ERR_ALIGN;
+  return hip_status(glu_gate_bwd(q, a_scale, q_rowsum, Wgu_packed, w_scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream));
+}
+
+size_t mmf_glu_bwd_workspace_bytes(int64_t M, int64_t K, int64_t L) {
+  if (check_glu_train(M, K, L) != MMF_OK || check_bwd_shape(M, K, 2 * L) != MMF_OK) return 0;
+  return glu_bwd_scratch(M, K, L).total;
+}
+
+int mmf_glu_bwd(const void* dp, int dp_is_f32, const void* x, int x_is_f32, const float* gamma, const float* rstd,
+                const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wpacked,
+                const float* w_scale, float* dx, float* dW, float* dgamma, int64_t M, int64_t K, int64_t L,
+                void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_dtype(dp_is_f32)) return st;
+  if (int st = check_dtype(x_is_f32)) return st;
+  if (int st = check_glu_train(M, K, L)) return st;
+  if (int st = check_bwd_shape(M, K, 2 * L)) return st;
+  if (M == 0 || L == 0) return MMF_OK;
+  if (!dp || !x || !rstd || !q || !a_scale || !q_rowsum || !Wpacked || !w_scale || !dx || !dW) return MMF_ERR_NULL;
+  if (!aligned16(dp) || !aligned16(x) || !aligned16_or_null(gamma) || !aligned16(rstd) || !aligned16(q) ||
+      !aligned16(a_scale) || !aligned16(q_rowsum) || !aligned16(Wpacked) || !aligned16(dx) || !aligned16(dW) ||
+      !aligned16_or_null(dgamma))
+    return MMF_ERR_ALIGN;
+  const GluPacked g = glu_packed(K, L);
+  const GluBwdScratch s = glu_bwd_scratch(M, K, L);
+  return with_workspace(workspace, workspace_bytes, s.total, stream, [&](char* scratch) {
+    uint32_t* Wgu = reinterpret_cast<uint32_t*>(scratch);
+    float* scales = reinterpret_cast<float*>(scratch + g.scales_off);
+    uint16_t* dgu = reinterpret_cast<uint16_t*>(scratch + g.end);
+    if (mmf::launch_glu_pack(Wpacked, Wpacked + L, 2 * L, L, static_cast<int>(K), Wgu, w_scale, scales, stream) !=
+            hipSuccess ||
+        glu_gate_bwd(q, a_scale, q_rowsum, Wgu, scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream) != hipSuccess)
       return MMF_ERR_HIP;
-    if (S > 1 && mmf::launch_sum_parts(dw_out, S, N * K, dW, stream) != hipSuccess) return MMF_ERR_HIP;
-    if (mmf::launch_col_final({dg_part, s.dy.row_tiles, K, dgamma}, {db_part, s.dy.row_tiles, N, db}, stream) !=
-        hipSuccess)
-      return MMF_ERR_HIP;
-    return MMF_OK;
+    return run_bwd({dgu, x, x_is_f32 == 1, gamma, rstd, q, a_scale, Wpacked, w_scale, dx, dW, nullptr, dgamma, M, K,
+                    2 * L},
+                   s.bwd, scratch + s.bwd_off, stream);
   });
 }
 

@@ -74,7 +74,11 @@ hipError_t launch_ternarize(const float* W, int64_t N, int K, uint32_t* Wpacked,
 // the two up-projections of a GLU interleaved in blocks of 16 (gate, up,
 // gate, ...), w_scale holds [gate, up], and the output is the gated
 // representation SiLU(g) * u, N / 2 columns wide.
-enum class Epilogue { kDequantF32, kRawI32, kGluF32, kAffineF32 };
+// kGluGradF32 / kGluGradBf16 (launch_gemm only): the columns of kGluF32, and
+// the output is [dg | du], the gradients of g and u in bf16 [M][N], from the
+// gradient of the gated representation (Affine::grad, [M][N/2] fp32 or bf16).
+enum class Epilogue { kDequantF32, kRawI32, kGluF32, kAffineF32, kGluGradF32, kGluGradBf16 };
+inline bool is_glu_grad(Epilogue e) { return e == Epilogue::kGluGradF32 || e == Epilogue::kGluGradBf16; }
 
 // kAffineF32: y = act_s(acc * a_scale * w_scale[s] + bias[n]) with the columns
 // in segments of `seg` (s = n / seg, seg % 16 == 0) and one activation per
@@ -89,6 +93,7 @@ struct Affine {
   const float* lb = nullptr;    // [seg]
   int64_t seg = 0;
   uint32_t acts = 0;
+  const void* grad = nullptr;   // kGluGrad*: [M][N / 2]
 };
 
 struct ContractArgs {
@@ -304,7 +309,9 @@ size_t bwd_dw_parts_bytes(const DwPlan& plan);
 hipError_t launch_dw(const uint16_t* dO, const int8_t* q, const float* a_scale, int64_t M, int64_t Np, int64_t N,
                      int K, float* out, float* parts, const DwPlan& plan, hipStream_t stream);
 
-hipError_t launch_glu_pack(const uint32_t* Wg, const uint32_t* Wu, int64_t L, int K, uint32_t* Wgu,
-                           hipStream_t stream);
+// `ld` words from one row of Wg and of Wu to the next; w_scales [2] (nullptr:
+// not stored) receives w_scale[0] twice.
+hipError_t launch_glu_pack(const uint32_t* Wg, const uint32_t* Wu, int64_t ld, int64_t L, int K, uint32_t* Wgu,
+                           const float* w_scale, float* w_scales, hipStream_t stream);
 
 }  // namespace mmf
