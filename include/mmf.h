@@ -416,7 +416,7 @@ int mmf_mlgru_fwd(const void *x, int x_is_f32, const float *gamma, const uint32_
  * dh0 [B][d] (NULL: not stored), dlb [d] (NULL: not computed; summed in fp64,
  * in a fixed order) float32.  z, lb and states as the forward had and left
  * them.  Inside both, the tokens are cut into chunks whose maps are joined.
- * More than 2^22 workgroups (B ceil(T/64) ceil(d/128)) return MMF_ERR_SHAPE;
+ * d above 2^20 or more than 2^22 workgroups (B ceil(T/128) ceil(d/64)) return MMF_ERR_SHAPE;
  * B == 0 or T == 0 is a no-op.  Workspace as above; the backward's also
  * serves the forward.
  */

@@ -373,6 +373,7 @@ MlgruScratch mlgru_scratch(int64_t B, int64_t T, int64_t d) {
 constexpr int64_t kMaxScanBlocks = int64_t(1) << 22;
 int check_mlgru_train(int64_t B, int64_t T, int64_t d) {
   if (int st = check_mlgru_d(d)) return st;
+  if (d > kMaxK) return MMF_ERR_SHAPE;
   if (B < 0 || T < 0 || B > kMaxMN || T > kMaxMN || (T > 0 && B > kMaxMN / T)) return MMF_ERR_SHAPE;
   return mmf::mlgru_train_blocks(B, T, d) <= kMaxScanBlocks ? MMF_OK : MMF_ERR_SHAPE;
 }
@@ -382,16 +383,17 @@ size_t mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d) {
 bool states_fit(const void* states, size_t bytes, int64_t B, int64_t T, int64_t d) {
   return (reinterpret_cast<uintptr_t>(states) & (kScratchAlign - 1)) == 0 && bytes >= mlgru_train_states_bytes(B, T, d);
 }
-// `arrays` of one value per chunk and channel (the chunks' maps, and the
-// backward's carries), then the partial sums of lb's gradient.
+// Where a sequence has several chunks, the words that they exchange and the
+// ticket counter; then the partial sums of lb's gradient (backward).
 struct MlgruTrainScratch {
-  size_t dlb_off, total;
+  size_t ticket_off, dlb_off, total;
 };
-MlgruTrainScratch mlgru_train_scratch(int64_t B, int64_t T, int64_t d, int arrays) {
+MlgruTrainScratch mlgru_train_scratch(int64_t B, int64_t T, int64_t d) {
   const int64_t nchunk = mmf::mlgru_train_chunks(T);
   const size_t n = static_cast<size_t>(B * nchunk * d);
   MlgruTrainScratch s;
-  s.dlb_off = nchunk > 1 ? round_up(sizeof(float) * n * static_cast<size_t>(arrays), kScratchAlign) : 0;
+  s.ticket_off = nchunk > 1 ? round_up(sizeof(uint64_t) * n, kScratchAlign) : 0;
+  s.dlb_off = s.ticket_off + (nchunk > 1 ? kScratchAlign : 0);
   s.total = s.dlb_off + round_up(sizeof(double) * n, kScratchAlign);
   return s;
 }
@@ -935,7 +937,7 @@ size_t mmf_mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d) {
 
 size_t mmf_mlgru_train_scan_workspace_bytes(int64_t B, int64_t T, int64_t d) {
   if (check_mlgru_train(B, T, d) != MMF_OK) return 0;
-  return mlgru_train_scratch(B, T, d, 2).dlb_off;
+  return mlgru_train_scratch(B, T, d).dlb_off;
 }
 
 int mmf_mlgru_train_scan(const float* z, const float* lb, const float* h0, float* o_prime, float* h_last,
@@ -948,16 +950,17 @@ int mmf_mlgru_train_scan(const float* z, const float* lb, const float* h0, float
       !aligned16_or_null(h_last))
     return MMF_ERR_ALIGN;
   if (!states_fit(states, states_bytes, B, T, d)) return MMF_ERR_WORKSPACE;
-  const size_t need = mlgru_train_scratch(B, T, d, 2).dlb_off;
-  return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
+  const MlgruTrainScratch s = mlgru_train_scratch(B, T, d);
+  return with_workspace(workspace, workspace_bytes, s.dlb_off, stream, [&](char* scratch) {
     return hip_status(mmf::launch_mlgru_train_scan({z, lb, h0, B, T, d}, o_prime, h_last, static_cast<float*>(states),
-                                                   reinterpret_cast<float*>(scratch), stream));
+                                                   reinterpret_cast<uint64_t*>(scratch),
+                                                   reinterpret_cast<uint32_t*>(scratch + s.ticket_off), stream));
   });
 }
 
 size_t mmf_mlgru_scan_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d) {
   if (check_mlgru_train(B, T, d) != MMF_OK) return 0;
-  return mlgru_train_scratch(B, T, d, 3).total;
+  return mlgru_train_scratch(B, T, d).total;
 }
 
 int mmf_mlgru_scan_bwd(const float* z, const float* lb, const void* states, size_t states_bytes,
@@ -972,12 +975,12 @@ int mmf_mlgru_scan_bwd(const float* z, const float* lb, const void* states, size
       !aligned16(dz) || !aligned16_or_null(dh0) || !aligned16_or_null(dlb))
     return MMF_ERR_ALIGN;
   if (!states_fit(states, states_bytes, B, T, d)) return MMF_ERR_WORKSPACE;
-  const MlgruTrainScratch s = mlgru_train_scratch(B, T, d, 3);
+  const MlgruTrainScratch s = mlgru_train_scratch(B, T, d);
   return with_workspace(workspace, workspace_bytes, dlb ? s.total : s.dlb_off, stream, [&](char* scratch) {
     double* part = dlb ? reinterpret_cast<double*>(scratch + s.dlb_off) : nullptr;
     if (mmf::launch_mlgru_scan_bwd({z, lb, nullptr, B, T, d}, static_cast<const float*>(states), do_prime,
-                                   do_is_f32 == 1, dh_last, dz, dh0, reinterpret_cast<float*>(scratch), part,
-                                   stream) != hipSuccess)
+                                   do_is_f32 == 1, dh_last, dz, dh0, reinterpret_cast<uint64_t*>(scratch),
+                                   reinterpret_cast<uint32_t*>(scratch + s.ticket_off), part, stream) != hipSuccess)
       return MMF_ERR_HIP;
     return hip_status(mmf::launch_col_final({part, B * mmf::mlgru_train_chunks(T), d, dlb}, {}, stream));
   });

@@ -208,8 +208,9 @@ hipError_t launch_mlgru_scan(const float* fcg, const float* h0, float* o, float*
 // pre-activations z [B*T][3d] and the forget gate's lower bound lb (nullptr:
 // 0): o', the last state (h_last, nullptr: not stored; may be h0) and the
 // states entering the chunks of tokens, [B][mlgru_train_chunks(T)][d].
-// ws: 2 B nchunk d floats where nchunk > 1.  T >= 1, d % 16 == 0,
-// mlgru_train_blocks (workgroups) below 2^22.
+// Where nchunk > 1, words holds B nchunk d of them (16-byte aligned) and
+// tickets one; the call clears them.  T >= 1, d % 16 == 0, mlgru_train_blocks
+// (workgroups) at most 2^22.
 struct MlgruTrainArgs {
   const float* z;
   const float* lb;
@@ -218,15 +219,15 @@ struct MlgruTrainArgs {
 };
 int64_t mlgru_train_chunks(int64_t T);
 int64_t mlgru_train_blocks(int64_t B, int64_t T, int64_t d);
-hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_last, float* states, float* ws,
-                                   hipStream_t stream);
+hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_last, float* states, uint64_t* words,
+                                   uint32_t* tickets, hipStream_t stream);
 // Its backward (h0 of `p` is not read): dz bf16 [B*T][3d], dh0 [B][d]
 // (nullptr: not stored) and the partial sums of lb's gradient
 // [B nchunk][d] (nullptr: not computed) from the gradient of o' and of the
-// last state (nullptr: 0).  ws: 3 B nchunk d floats where nchunk > 1.
+// last state (nullptr: 0).  words, tickets as above.
 hipError_t launch_mlgru_scan_bwd(const MlgruTrainArgs& p, const float* states, const void* dout, bool dout_is_f32,
-                                 const float* dh_last, uint16_t* dz, float* dh0, float* ws, double* dlb_part,
-                                 hipStream_t stream);
+                                 const float* dh_last, uint16_t* dz, float* dh0, uint64_t* words, uint32_t* tickets,
+                                 double* dlb_part, hipStream_t stream);
 
 // The norm of a set of gradients and the set scaled to it (grad_norm.hip).
 // The arrays of addresses, types and sizes are host memory; partials holds

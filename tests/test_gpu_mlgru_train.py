@@ -133,8 +133,9 @@ def check(mmf, v, B, T, **kw):
     return got
 
 
-SIZES = [(1, 1, 16), (3, 1, 2048), (2, 7, 16), (1, 8, 48), (1, 9, 128), (2, 63, 144), (2, 64, 256), (2, 65, 256),
-         (1, 129, 272), (3, 357, 1040), (5, 700, 32), (1, 5000, 16), (1, 18433, 16)]
+# around 8 tokens (a half wave's), 128 (a chunk) and 16 chunks (a run)
+SIZES = [(1, 1, 16), (3, 1, 2048), (2, 7, 16), (1, 8, 48), (1, 9, 128), (2, 63, 144), (2, 127, 80), (2, 128, 256),
+         (2, 129, 256), (3, 357, 1040), (5, 700, 32), (1, 2048, 64), (2, 2049, 48), (1, 18433, 16)]
 
 
 @pytest.mark.gpu
@@ -249,21 +250,22 @@ A, BAD, S = 0x100000, 0x100004, None
 
 def test_refusals(mmf):
     lib = mmf._lib
-    sb = mmf.mmf_mlgru_train_states_bytes(2, 100, 32)
-    wf, wb = mmf.mmf_mlgru_train_scan_workspace_bytes(2, 100, 32), mmf.mmf_mlgru_scan_bwd_workspace_bytes(2, 100, 32)
+    sb = mmf.mmf_mlgru_train_states_bytes(2, 200, 32)
+    wf, wb = mmf.mmf_mlgru_train_scan_workspace_bytes(2, 200, 32), mmf.mmf_mlgru_scan_bwd_workspace_bytes(2, 200, 32)
     assert sb == 2 * 2 * 32 * 4 and 0 < wf < wb and wb % 256 == 0
 
-    def fwd(z=A, lb=A, h0=A, o=A, h=A, st=A, n=sb, B=2, T=100, d=32, ws=A, wn=wf):
+    def fwd(z=A, lb=A, h0=A, o=A, h=A, st=A, n=sb, B=2, T=200, d=32, ws=A, wn=wf):
         return lib.mmf_mlgru_train_scan(z, lb, h0, o, h, st, n, B, T, d, ws, wn, S)
 
-    def bwd(z=A, lb=A, st=A, n=sb, do=A, k=1, dh=A, dz=A, dh0=A, dlb=A, B=2, T=100, d=32, ws=A, wn=wb):
+    def bwd(z=A, lb=A, st=A, n=sb, do=A, k=1, dh=A, dz=A, dh0=A, dlb=A, B=2, T=200, d=32, ws=A, wn=wb):
         return lib.mmf_mlgru_scan_bwd(z, lb, st, n, do, k, dh, dz, dh0, dlb, B, T, d, ws, wn, S)
 
     for f in (fwd, bwd):
         for d in (0, -16, 24):
             assert f(d=d) == 2
         assert f(B=-1) == 2 and f(T=-1) == 2 and f(B=1 << 20, T=1 << 12) == 2
-        assert f(B=1 << 22, T=65, d=16) == 2          # 2^23 workgroups
+        assert f(B=1 << 22, T=129, d=16) == 2          # 2^23 workgroups
+        assert f(d=(1 << 20) + 16) == 2
         assert f(n=sb - 1) == 6 and f(st=A + 16) == 6 and f(ws=A + 16) == 6
         assert f(z=None) == 1 and f(st=None) == 1
         assert f(z=None, B=0) == 0 and f(z=None, T=0) == 0
@@ -274,7 +276,7 @@ def test_refusals(mmf):
     for name in ("z", "lb", "do", "dh", "dz", "dh0", "dlb"):
         assert bwd(**{name: BAD}) == 3
     assert mmf.mmf_mlgru_train_states_bytes(2, 100, 24) == 0
-    assert mmf.mmf_mlgru_train_scan_workspace_bytes(7, 64, 32) == 0   # one chunk: no maps
+    assert mmf.mmf_mlgru_train_scan_workspace_bytes(7, 128, 32) == 0   # one chunk: no maps
 
 
 def test_workspace_of_a_batch_serves_smaller_ones(mmf):
