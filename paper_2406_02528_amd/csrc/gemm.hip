@@ -461,39 +461,44 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
         const_cast<void*>(aff.grad), 0, static_cast<int>(static_cast<uint32_t>(M) * L * kDp), kBufferFlags);
     const __amdgpu_buffer_rsrc_t orsrc = __builtin_amdgcn_make_buffer_rsrc(
         out, 0, static_cast<int>(static_cast<uint32_t>(M) * L * 4u), kBufferFlags);
+    // every load of the wave's gradients in flight before the first is used
+    // (the k loop's fragments are free by now)
+    auto place = [&](int fm, int f, uint32_t& row, uint32_t& ch) -> bool {
+      const int m = m0 + wm * WM + fm * 16 + el16;
+      row = static_cast<uint32_t>(m) * L;
+      ch = static_cast<uint32_t>((n0 + wn * WN) / 2 + f * 16 + 4 * eg);
+      return m < M && ch < L;
+    };
+    constexpr int kDpWords = kDp == 4 ? 4 : 2;
+    Words<kDpWords> dpw[FM][FN / 2];
+#pragma unroll
+    for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+      for (int f = 0; f < FN / 2; ++f) {
+        uint32_t row, ch;
+        const bool ok = place(fm, f, row, ch);
+        dpw[fm][f] = load_words<kDpWords>(grsrc, ok ? kDp * (row + ch) : kOut, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int fm = 0; fm < FM; ++fm) {
       const int lr = wm * WM + fm * 16 + el16;
-      const bool row_ok = m0 + lr < M;
-      const uint32_t row = static_cast<uint32_t>(m0 + lr) * L;
       const int rs = s_rsum[lr];
       const float sg = s_scale[lr] * ws, su = s_scale[lr] * ws_u;
 #pragma unroll
       for (int f = 0; f < FN / 2; ++f) {
-        const uint32_t ch = static_cast<uint32_t>((n0 + wn * WN) / 2 + f * 16 + 4 * eg);
-        const bool ok = row_ok && ch < L;
-        float dp[4];
-        if constexpr (kDp == 4) {
-          const v4f v = __builtin_bit_cast(
-              v4f, __builtin_amdgcn_raw_buffer_load_b128(grsrc, ok ? 4u * (row + ch) : kOut, 0, 0));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) dp[r] = v[r];
-        } else {
-          const uint2 v = __builtin_bit_cast(
-              uint2, __builtin_amdgcn_raw_buffer_load_b64(grsrc, ok ? 2u * (row + ch) : kOut, 0, 0));
-          dp[0] = bf16_lo(v.x);
-          dp[1] = bf16_hi(v.x);
-          dp[2] = bf16_lo(v.y);
-          dp[3] = bf16_hi(v.y);
-        }
+        uint32_t row, ch;
+        const bool ok = place(fm, f, row, ch);
         float dg[4], du[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+          const float dp = kDp == 4 ? __uint_as_float(dpw[fm][f].w[r % kDpWords])
+                                    : (r & 1 ? bf16_hi(dpw[fm][f].w[r / 2]) : bf16_lo(dpw[fm][f].w[r / 2]));
           const float gv = static_cast<float>(acc[fm][2 * f][r] - rs) * sg;
           const float uv = static_cast<float>(acc[fm][2 * f + 1][r] - rs) * su;
           const float s = sigmoid_hw(gv);
-          du[r] = dp[r] * (gv * s);
-          dg[r] = dp[r] * uv * (s * (1.0f + gv * (1.0f - s)));
+          du[r] = dp * (gv * s);
+          dg[r] = dp * uv * (s * (1.0f + gv * (1.0f - s)));
         }
         const uint32_t at = 2u * (2u * row + ch);
         typedef unsigned int v2u __attribute__((ext_vector_type(2)));
