@@ -37,8 +37,9 @@ struct FwdArgs {
 
 // One row per W waves, VPL vectors of E values per lane (VPL == 0: any K, the
 // stored sum read again for each further pass).  x and s may be the same
-// array: every element is read and written by one lane.
-template <typename XT, typename BT, int E, int W, int VPL>
+// array: every element is read and written by one lane.  NT: x, branch and s
+// as streams (q stays for the contraction).
+template <typename XT, typename BT, int E, int W, int VPL, bool NT>
 __global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const FwdArgs a) {
   constexpr int kBlockWaves = W > 4 ? W : 4;
   constexpr int kRows = kBlockWaves / W;
@@ -80,9 +81,9 @@ __global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const 
       RowVec<BT, E> bv[VPL];
       RowVec<float, E> gv[VPL];
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) xv[i].load(xrsrc, rl + W * kWave * i);
+      for (int i = 0; i < VPL; ++i) xv[i].template load<NT>(xrsrc, rl + W * kWave * i);
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) bv[i].load(brsrc, rl + W * kWave * i);
+      for (int i = 0; i < VPL; ++i) bv[i].template load<NT>(brsrc, rl + W * kWave * i);
 #pragma unroll
       for (int i = 0; i < VPL; ++i) gv[i].load(grsrc, rl + W * kWave * i);
       __builtin_amdgcn_sched_barrier(0);  // all loads before the first wait
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const 
 #pragma unroll
         for (int e = 0; e < E; ++e) f[i][e] = xv[i].get(e) + bv[i].get(e);
         xv[i].set(f[i]);
-        if (sum != nullptr && live && v < nvec) xv[i].store(sum + at, v);
+        if (sum != nullptr && live && v < nvec) xv[i].template store<NT>(sum + at, v);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           f[i][e] = xv[i].get(e);  // the stored value
@@ -178,7 +179,10 @@ hipError_t launch_fwd_one(const FwdArgs& a, hipStream_t stream) {
   constexpr int kRows = kBlockWaves / W;
   const int64_t blocks = (a.M + kRows - 1) / kRows;
   const dim3 grid(static_cast<unsigned>(blocks < kMaxBlocks ? blocks : kMaxBlocks));
-  hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
+  if (VPL > 0 && a.M * a.K * static_cast<int64_t>(2 * sizeof(XT) + sizeof(BT) + 1) >= kLastLevelBytes)
+    hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL, (VPL > 0)>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL, false>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -239,8 +243,8 @@ struct BwdArgs {
 // dgamma sums (fp64) in registers.  The next row's loads are in flight while
 // a row is reduced and written (not with 16 waves, whose 128 registers hold
 // one row only).  VPL == 0: any K; the row is read twice and the column sums
-// are kept in dg_part.
-template <typename ST, typename DT, int E, int W, int VPL>
+// are kept in dg_part.  NT: every array but gamma and the sums as streams.
+template <typename ST, typename DT, int E, int W, int VPL, bool NT>
 __global__ __launch_bounds__(kWave* W) void add_quant_bwd_kernel(const BwdArgs a) {
   __shared__ double s_t[2][W];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -258,11 +262,11 @@ __global__ __launch_bounds__(kWave* W) void add_quant_bwd_kernel(const BwdArgs a
   auto emit = [&](int64_t at, int v, const float* o) {
     RowVec<float, E> ov;
     ov.set(o);
-    ov.store(a.ds + at, v);
+    ov.template store<NT>(a.ds + at, v);
     if (a.ds_bf16 != nullptr) {
       RowVec<uint16_t, E> hv;
       hv.set(o);
-      hv.store(a.ds_bf16 + at, v);
+      hv.template store<NT>(a.ds_bf16 + at, v);
     }
   };
   int parity = 0;
@@ -280,11 +284,11 @@ __global__ __launch_bounds__(kWave* W) void add_quant_bwd_kernel(const BwdArgs a
       const __amdgpu_buffer_rsrc_t orsrc =
           row_rsrc(a.ds_out == nullptr ? a.ds_out : a.ds_out + at, K, live && a.ds_out != nullptr);
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) w.dy[i].load(drsrc, rl + W * kWave * i);
+      for (int i = 0; i < VPL; ++i) w.dy[i].template load<NT>(drsrc, rl + W * kWave * i);
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) w.s[i].load(srsrc, rl + W * kWave * i);
+      for (int i = 0; i < VPL; ++i) w.s[i].template load<NT>(srsrc, rl + W * kWave * i);
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) w.res[i].load(orsrc, rl + W * kWave * i);
+      for (int i = 0; i < VPL; ++i) w.res[i].template load<NT>(orsrc, rl + W * kWave * i);
       w.r = a.rstd[live ? row : 0];
     };
     RowVec<float, E> gv[VPL];
@@ -393,7 +397,15 @@ __global__ __launch_bounds__(kWave* W) void add_quant_bwd_kernel(const BwdArgs a
 template <typename ST, typename DT, int E, int W>
 hipError_t launch_bwd_w(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
   const int vpl = (a.K / E + W * kWave - 1) / (W * kWave);
-#define MMF_LAUNCH(V) hipLaunchKernelGGL((add_quant_bwd_kernel<ST, DT, E, W, V>), dim3(blocks), dim3(kWave * W), 0, stream, a)
+  const int64_t bytes = sizeof(ST) + sizeof(DT) + (a.ds_out ? 4 : 0) + 4 + (a.ds_bf16 ? 2 : 0);
+  const bool nt = a.M * a.K * bytes >= kLastLevelBytes;
+#define MMF_LAUNCH(V)                                                                                                \
+  do {                                                                                                               \
+    if (nt)                                                                                                          \
+      hipLaunchKernelGGL((add_quant_bwd_kernel<ST, DT, E, W, V, true>), dim3(blocks), dim3(kWave * W), 0, stream, a); \
+    else                                                                                                             \
+      hipLaunchKernelGGL((add_quant_bwd_kernel<ST, DT, E, W, V, false>), dim3(blocks), dim3(kWave * W), 0, stream, a); \
+  } while (0)
   switch (vpl) {
     case 1: MMF_LAUNCH(1); break;
     case 2: MMF_LAUNCH(2); break;

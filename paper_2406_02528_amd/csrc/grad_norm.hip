@@ -7,6 +7,13 @@
 // array shorter), one workgroup each.  Every piece's sum of squares is a
 // partial of its own, and one workgroup adds them in a fixed order: the same
 // bits on every call, with no atomics.
+//
+// Bound by HBM: 4 bytes read for the norm, 4 read and 4 written for the
+// scaling.  All of it passes the caches as streams (nontemporal): a set of 800
+// MB then takes 433 us where cached accesses take 461, and one of 192 MB behind
+// other work 106 instead of 141, since a cached read pushes out lines that
+// others wrote, which go to memory first.  Only a set of 64 to 128 MB that was
+// just read or written is faster cached (128 MB: 65 instead of 73 us).
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "row_vec.h"
@@ -29,14 +36,12 @@ struct Set {
   int n;
 };
 
-// The array and the piece of it that workgroup `blk` takes (REV: an array's
-// pieces from its last to its first).
+// The array and the piece of it that workgroup `blk` takes.
 struct Piece {
   int i;
   int64_t begin, end;
   bool f32;
 };
-template <bool REV>
 __device__ __forceinline__ Piece piece_of(const Set& s, uint32_t blk) {
   int lo = 0, hi = s.n - 1;  // the last array whose first piece is at most blk
   while (lo < hi) {
@@ -44,22 +49,43 @@ __device__ __forceinline__ Piece piece_of(const Set& s, uint32_t blk) {
     if (s.first[mid] <= blk) lo = mid;
     else hi = mid - 1;
   }
-  int64_t p = blk - s.first[lo];
-  if constexpr (REV) p = (s.count[lo] - 1) / kPiece - p;
-  const int64_t begin = p * kPiece;
+  const int64_t begin = static_cast<int64_t>(blk - s.first[lo]) * kPiece;
   const int64_t end = begin + kPiece < s.count[lo] ? begin + kPiece : s.count[lo];
   return {lo, begin, end, ((s.f32[lo / 32] >> (lo % 32)) & 1u) != 0};
 }
 
-// Elements [begin, end) of an array: whole vectors of E, then the rest one by
-// one (arrays and pieces start on 16 bytes).
+// Elements [begin, end) of an array: vec(raw, i) for whole vectors of 16 bytes,
+// kAhead of a thread's loads in flight together, then one(i) for the rest
+// (arrays and pieces start on 16 bytes).
+constexpr int kAhead = 8;
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ v4u load16(const void* p) { return __builtin_nontemporal_load(static_cast<const v4u*>(p)); }
+__device__ __forceinline__ void store16(void* p, v4u w) { __builtin_nontemporal_store(w, static_cast<v4u*>(p)); }
 template <typename T, typename F, typename G>
-__device__ __forceinline__ void each(int64_t begin, int64_t end, F&& vec, G&& one) {
+__device__ __forceinline__ void each(const T* g, int64_t begin, int64_t end, F&& vec, G&& one) {
   constexpr int E = 16 / sizeof(T);
-  const int64_t whole = begin + (end - begin) / E * E;
-  for (int64_t i = begin + E * threadIdx.x; i < whole; i += E * kBlock) vec(i);
-  const int64_t i = whole + threadIdx.x;
-  if (i < end) one(i);
+  const int n = static_cast<int>(end - begin);  // at most kPiece
+  const T* const p = g + begin;
+  const int whole = n / E;
+  int v = threadIdx.x;
+  for (; v + (kAhead - 1) * kBlock < whole; v += kAhead * kBlock) {
+    v4u w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) w[u] = load16(p + static_cast<int64_t>(v + u * kBlock) * E);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) vec(w[u], begin + static_cast<int64_t>(v + u * kBlock) * E);
+  }
+  for (; v < whole; v += kBlock) vec(load16(p + static_cast<int64_t>(v) * E), begin + static_cast<int64_t>(v) * E);
+  const int i = whole * E + threadIdx.x;
+  if (i < n) one(begin + i);
+}
+
+template <typename T>
+__device__ __forceinline__ RowVec<T, 16 / sizeof(T)> row_vec(v4u w) {
+  RowVec<T, 16 / sizeof(T)> v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.w[i] = w[i];
+  return v;
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -74,12 +100,10 @@ template <typename T>
 __device__ __forceinline__ double sum_squares(const T* g, int64_t begin, int64_t end) {
   constexpr int E = 16 / sizeof(T);
   double ss = 0.0;
-  each<T>(
-      begin, end,
-      [&](int64_t i) {
-        RowVec<T, E> v;
-        const uint4 w = *reinterpret_cast<const uint4*>(g + i);
-        v.w[0] = w.x; v.w[1] = w.y; v.w[2] = w.z; v.w[3] = w.w;
+  each(
+      g, begin, end,
+      [&](v4u w, int64_t) {
+        const auto v = row_vec<T>(w);
 #pragma unroll
         for (int e = 0; e < E; ++e) ss = sum_sq(ss, v.get(e));
       },
@@ -91,7 +115,7 @@ __device__ __forceinline__ double sum_squares(const T* g, int64_t begin, int64_t
 }
 
 __global__ __launch_bounds__(kBlock) void grad_sumsq_kernel(const Set s, double* __restrict__ partials) {
-  const Piece p = piece_of<false>(s, blockIdx.x);
+  const Piece p = piece_of(s, blockIdx.x);
   const double ss = p.f32 ? sum_squares(static_cast<const float*>(s.src[p.i]), p.begin, p.end)
                           : sum_squares(static_cast<const uint16_t*>(s.src[p.i]), p.begin, p.end);
   const double t = block_sum(ss);
@@ -100,9 +124,15 @@ __global__ __launch_bounds__(kBlock) void grad_sumsq_kernel(const Set s, double*
 
 __global__ __launch_bounds__(kBlock) void grad_norm_kernel(const double* __restrict__ partials, int64_t n,
                                                            float* __restrict__ norm) {
+  constexpr int kLoads = 16;
   double v = 0.0;
-#pragma unroll 8
-  for (int64_t i = threadIdx.x; i < n; i += kBlock) v += partials[i];
+  for (int64_t i = threadIdx.x; i < n; i += kLoads * kBlock) {
+    double p[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) p[u] = i + u * kBlock < n ? partials[i + u * kBlock] : 0.0;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) v += p[u];
+  }
   const double t = block_sum(v);
   if (threadIdx.x == 0) norm[0] = static_cast<float>(__builtin_sqrt(t));
 }
@@ -110,17 +140,15 @@ __global__ __launch_bounds__(kBlock) void grad_norm_kernel(const double* __restr
 template <typename T>
 __device__ __forceinline__ void scale(const T* g, T* o, int64_t begin, int64_t end, float c) {
   constexpr int E = 16 / sizeof(T);
-  each<T>(
-      begin, end,
-      [&](int64_t i) {
-        RowVec<T, E> v;
-        const uint4 w = *reinterpret_cast<const uint4*>(g + i);
-        v.w[0] = w.x; v.w[1] = w.y; v.w[2] = w.z; v.w[3] = w.w;
+  each(
+      g, begin, end,
+      [&](v4u w, int64_t i) {
+        auto v = row_vec<T>(w);
         float f[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) f[e] = v.get(e) * c;
         v.set(f);
-        *reinterpret_cast<uint4*>(o + i) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+        store16(o + i, v4u{v.w[0], v.w[1], v.w[2], v.w[3]});
       },
       [&](int64_t i) {
         if constexpr (sizeof(T) == 4) o[i] = g[i] * c;
@@ -128,30 +156,27 @@ __device__ __forceinline__ void scale(const T* g, T* o, int64_t begin, int64_t e
       });
 }
 
-// The arrays and their pieces from the last to the first: the sums of squares
-// read them in the other order, so what they read last is still in the
-// last-level cache.
 __global__ __launch_bounds__(kBlock) void grad_scale_kernel(const Set s, const float* __restrict__ norm,
                                                             float max_norm) {
   float c = max_norm / (norm[0] + 1e-6f);
   if (c > 1.0f) c = 1.0f;  // a NaN stays
-  const Piece p = piece_of<true>(s, blockIdx.x);
+  const Piece p = piece_of(s, blockIdx.x);
   if (c == 1.0f && s.src[p.i] == s.dst[p.i]) return;  // nothing changes
   if (p.f32) scale(static_cast<const float*>(s.src[p.i]), static_cast<float*>(s.dst[p.i]), p.begin, p.end, c);
   else scale(static_cast<const uint16_t*>(s.src[p.i]), static_cast<uint16_t*>(s.dst[p.i]), p.begin, p.end, c);
 }
 
-// Calls launch(set, pieces) for every launch's worth of arrays, from the first
-// to the last or (reverse) from the last to the first.  An array's pieces fit
-// a launch (counts are at most kGradMaxCount), so every round takes one.
+// Calls launch(set, pieces) for every launch's worth of arrays.  An array's
+// pieces fit a launch (counts are at most kGradMaxCount), so every round takes
+// one.
 template <typename F>
-hipError_t for_sets(const GradSetArgs& a, bool reverse, F&& launch) {
+hipError_t for_sets(const GradSetArgs& a, F&& launch) {
   int64_t done = 0;
   while (done < a.n) {
     Set s{};
     int64_t pieces = 0;
     for (; done < a.n; ++done) {
-      const int64_t i = reverse ? a.n - 1 - done : done;
+      const int64_t i = done;
       const int64_t p = (a.counts[i] + kPiece - 1) / kPiece;
       if (p == 0) continue;
       if (s.n == kSet || pieces + p > kMaxPieces) break;
@@ -180,7 +205,7 @@ int64_t grad_pieces(const int64_t* counts, int64_t n) {
 
 hipError_t launch_grad_norm(const GradSetArgs& a, float* norm, double* partials, hipStream_t stream) {
   int64_t done = 0;
-  const hipError_t e = for_sets(a, false, [&](const Set& s, uint32_t pieces) {
+  const hipError_t e = for_sets(a, [&](const Set& s, uint32_t pieces) {
     hipLaunchKernelGGL(grad_sumsq_kernel, dim3(pieces), dim3(kBlock), 0, stream, s, partials + done);
     done += pieces;
     return hipGetLastError();
@@ -191,7 +216,7 @@ hipError_t launch_grad_norm(const GradSetArgs& a, float* norm, double* partials,
 }
 
 hipError_t launch_grad_clip(const GradSetArgs& a, const float* norm, float max_norm, hipStream_t stream) {
-  return for_sets(a, true, [&](const Set& s, uint32_t pieces) {
+  return for_sets(a, [&](const Set& s, uint32_t pieces) {
     hipLaunchKernelGGL(grad_scale_kernel, dim3(pieces), dim3(kBlock), 0, stream, s, norm, max_norm);
     return hipGetLastError();
   });

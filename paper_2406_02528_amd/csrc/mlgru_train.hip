@@ -81,8 +81,10 @@ struct Place {
 
 // A chunk's rows of `width` elements of `size` bytes: loads past the
 // sequence's end or (off) past d read as zero and stores there go nowhere.
-// Offsets stay below 2^31 (d <= 2^20: 128 rows of 3 d floats).
+// Offsets stay below 2^31 (d <= 2^20: 128 rows of 3 d floats).  NT: as streams.
+template <bool NT>
 struct Rows {
+  static constexpr int kPolicy = NT ? kNontemporal : 0;
   __amdgpu_buffer_rsrc_t r;
   uint32_t row_bytes, at;   // of a row; the lane's channel in its first token
   template <typename T>
@@ -93,19 +95,20 @@ struct Rows {
     at = p.col ? static_cast<uint32_t>(p.u0) * row_bytes + static_cast<uint32_t>(p.c) * size : 0x80000000u;
   }
   __device__ __forceinline__ V2 f32(int u, uint32_t off) const {
-    const float2 v = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, at + u * row_bytes + off, 0, 0));
+    const float2 v = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, at + u * row_bytes + off, 0, kPolicy));
     return {v.x, v.y};
   }
   __device__ __forceinline__ V2 bf16(int u) const {
-    const uint32_t w = __builtin_amdgcn_raw_buffer_load_b32(r, at + u * row_bytes, 0, 0);
+    const uint32_t w = __builtin_amdgcn_raw_buffer_load_b32(r, at + u * row_bytes, 0, kPolicy);
     return {bf16_lo(w), bf16_hi(w)};
   }
   __device__ __forceinline__ void store(int u, V2 v) const {
     typedef unsigned int v2u __attribute__((ext_vector_type(2)));
-    __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(v.x), __float_as_uint(v.y)}, r, at + u * row_bytes, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(v.x), __float_as_uint(v.y)}, r, at + u * row_bytes, 0,
+                                          kPolicy);
   }
   __device__ __forceinline__ void store_bf16(int u, uint32_t off, float x, float y) const {
-    __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(x, y), r, at + u * row_bytes + off, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(x, y), r, at + u * row_bytes + off, 0, kPolicy);
   }
 };
 
@@ -200,12 +203,12 @@ struct FwdArgs {
   int64_t B, T, d, nchunk;
 };
 
-template <bool MANY>
+template <bool MANY, bool NT>
 __global__ __launch_bounds__(kThreads) void mlgru_train_fwd_kernel(const FwdArgs a) {
   __shared__ Map2 maps[kSubs][kLanes], look[MANY ? kSubs : 1][kLanes];
   const int64_t d = a.d;
   const Place p = place<MANY>(a.T, d, a.B, a.nchunk, false, a.tickets);
-  const Rows z(a.z, p, 3 * d, 4), o(a.o, p, d, 4);
+  const Rows<NT> z(a.z, p, 3 * d, 4), o(a.o, p, d, 4);
   const uint32_t gate = static_cast<uint32_t>(d) * 4u;
   V2 f[kTok], c[kTok], g[kTok];
 #pragma unroll
@@ -276,14 +279,14 @@ struct BwdArgs {
   int64_t B, T, d, nchunk;
 };
 
-template <typename DT, bool MANY>
+template <typename DT, bool MANY, bool NT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void mlgru_train_bwd_kernel(const BwdArgs a) {
   __shared__ Map2 maps[kSubs][kLanes], back[kSubs][kLanes];
   __shared__ V2 s_dlb[kSubs][kLanes];
   const int64_t d = a.d;
   const Place p = place<MANY>(a.T, d, a.B, a.nchunk, true, a.tickets);
-  const Rows z(a.z, p, 3 * d, 4), dz(a.dz, p, 3 * d, 2);
-  const Rows dout(static_cast<const DT*>(a.dout), p, d, sizeof(DT));
+  const Rows<NT> z(a.z, p, 3 * d, 4), dz(a.dz, p, 3 * d, 2);
+  const Rows<NT> dout(static_cast<const DT*>(a.dout), p, d, sizeof(DT));
   const uint32_t gate = static_cast<uint32_t>(d) * 4u, dgate = static_cast<uint32_t>(d) * 2u;
   V2 zf[kTok], zc[kTok], zg[kTok], go[kTok];
 #pragma unroll
@@ -422,29 +425,40 @@ hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_l
   const dim3 grid(static_cast<unsigned>(mlgru_train_blocks(p.B, p.T, p.d)));
   if (nchunk > 1) {
     if (const hipError_t e = clear(words, p.B * nchunk * p.d, tickets, stream); e != hipSuccess) return e;
-    hipLaunchKernelGGL(mlgru_train_fwd_kernel<true>, grid, dim3(kThreads), 0, stream, a);
+    if (p.B * p.T * p.d * 16 >= kLastLevelBytes)  // z and o'
+      hipLaunchKernelGGL((mlgru_train_fwd_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((mlgru_train_fwd_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
   } else {
-    hipLaunchKernelGGL(mlgru_train_fwd_kernel<false>, grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((mlgru_train_fwd_kernel<false, false>), grid, dim3(kThreads), 0, stream, a);
   }
   return hipGetLastError();
 }
+
+namespace {
+template <typename DT>
+hipError_t launch_bwd(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
+  const dim3 grid(blocks), block(kThreads);
+  if (a.nchunk == 1)
+    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, false, false>), grid, block, 0, stream, a);
+  else if (a.B * a.T * a.d * static_cast<int64_t>(18 + sizeof(DT)) >= kLastLevelBytes)  // z, do and dz
+    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, true>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, false>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+}  // namespace
 
 hipError_t launch_mlgru_scan_bwd(const MlgruTrainArgs& p, const float* states, const void* dout, bool dout_is_f32,
                                  const float* dh_last, uint16_t* dz, float* dh0, uint64_t* words, uint32_t* tickets,
                                  double* dlb_part, hipStream_t stream) {
   const int64_t nchunk = mlgru_train_chunks(p.T);
   const BwdArgs a{p.z, p.lb, states, dout, dh_last, words, tickets, dz, dh0, dlb_part, p.B, p.T, p.d, nchunk};
-  const dim3 grid(static_cast<unsigned>(mlgru_train_blocks(p.B, p.T, p.d))), block(kThreads);
   if (nchunk > 1) {
     if (const hipError_t e = clear(words, p.B * nchunk * p.d, tickets, stream); e != hipSuccess) return e;
-    if (dout_is_f32) hipLaunchKernelGGL((mlgru_train_bwd_kernel<float, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((mlgru_train_bwd_kernel<uint16_t, true>), grid, block, 0, stream, a);
-  } else if (dout_is_f32) {
-    hipLaunchKernelGGL((mlgru_train_bwd_kernel<float, false>), grid, block, 0, stream, a);
-  } else {
-    hipLaunchKernelGGL((mlgru_train_bwd_kernel<uint16_t, false>), grid, block, 0, stream, a);
   }
-  return hipGetLastError();
+  const unsigned blocks = static_cast<unsigned>(mlgru_train_blocks(p.B, p.T, p.d));
+  return dout_is_f32 ? launch_bwd<float>(a, blocks, stream) : launch_bwd<uint16_t>(a, blocks, stream);
 }
 
 }  // namespace mmf

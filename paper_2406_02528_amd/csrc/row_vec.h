@@ -28,6 +28,34 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_rsrc(const T* row, int K, 
                                            kBufferWord3);
 }
 
+// Streams.  A call whose arrays together fill the last-level cache (256 MB)
+// reads and writes them without leaving them there (nontemporal: nothing of
+// them would still be there for their next reader, and taking a line in pushes
+// another out, which goes to memory first if it was written).  Smaller ones
+// stay for their next reader.
+constexpr int64_t kLastLevelBytes = int64_t(256) << 20;
+constexpr int kNontemporal = 2;  // buffer cache policy: the nt bit
+
+// load_words with the stream's cache policy.
+template <int F, bool NT>
+__device__ __forceinline__ Words<F> load_stream(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  constexpr int kPolicy = NT ? kNontemporal : 0;
+  Words<F> p;
+  if constexpr (F == 2) {
+    const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kPolicy));
+    p.w[0] = v.x;
+    p.w[1] = v.y;
+  } else {
+    static_assert(F == 4, "two or four words");
+    const uint4 v = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kPolicy));
+    p.w[0] = v.x;
+    p.w[1] = v.y;
+    p.w[2] = v.z;
+    p.w[3] = v.w;
+  }
+  return p;
+}
+
 // E values of T (uint16_t: bf16 bits, or float) of a row, from value E v.
 template <typename T, int E>
 struct RowVec {
@@ -36,10 +64,11 @@ struct RowVec {
   static constexpr int kLoad = kWords < 4 ? kWords : 4;  // dwords per load
   uint32_t w[kWords];
 
+  template <bool NT = false>
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int v) {
 #pragma unroll
     for (int i = 0; i < kWords; i += kLoad) {
-      const Words<kLoad> p = load_words<kLoad>(r, static_cast<uint32_t>(v) * (4u * kWords) + 4u * i, 0);
+      const Words<kLoad> p = load_stream<kLoad, NT>(r, static_cast<uint32_t>(v) * (4u * kWords) + 4u * i);
 #pragma unroll
       for (int j = 0; j < kLoad; ++j) w[i + j] = p.w[j];
     }
@@ -56,14 +85,17 @@ struct RowVec {
       else w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
     }
   }
+  template <bool NT = false>
   __device__ __forceinline__ void store(T* row, int v) const {
-    uint32_t* p = reinterpret_cast<uint32_t*>(row + static_cast<int64_t>(v) * E);
-    if constexpr (kWords == 2) {
-      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    } else {
+    typedef unsigned int vec __attribute__((ext_vector_type(kLoad)));
+    vec* const p = reinterpret_cast<vec*>(row + static_cast<int64_t>(v) * E);
 #pragma unroll
-      for (int i = 0; i < kWords; i += 4)
-        *reinterpret_cast<uint4*>(p + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    for (int i = 0; i < kWords / kLoad; ++i) {
+      vec x;
+#pragma unroll
+      for (int j = 0; j < kLoad; ++j) x[j] = w[i * kLoad + j];
+      if constexpr (NT) __builtin_nontemporal_store(x, p + i);
+      else p[i] = x;
     }
   }
 };

@@ -112,6 +112,20 @@ def test_forward_more_rows_than_a_grid(mmf):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("xt,bt", [(BF, F32), (F32, F32), (BF, BF)])
+def test_forward_past_the_last_level_cache(mmf, xt, bt):
+    """More than 256 MB: read and written as streams."""
+    check_fwd(mmf, 9001, 8000, xt, bt)
+    check_fwd(mmf, 40001, 1040, xt, bt, in_place=True)
+
+
+@pytest.mark.gpu
+def test_backward_past_the_last_level_cache(mmf):
+    check_bwd(mmf, 8001, 2288, BF, F32)
+    check_bwd(mmf, 30001, 1040, F32, BF, in_place=True)
+
+
+@pytest.mark.gpu
 def test_forward_without_the_optional_outputs(mmf):
     g = gen(5)
     x, b = rand(g, 9, 256), rand(g, 9, 256)

@@ -158,6 +158,28 @@ def test_optional_inputs(mmf, B, T, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+def test_past_the_last_level_cache(mmf, dt):
+    """Four sequences that together exceed 256 MB, and so pass as streams:
+    each as in a call of its own."""
+    B, T, d = 4, 2100, 2064
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(s, generator=g, device=dev())  # noqa: E731
+    v = {"z": rand(B * T, 3 * d), "lb": torch.rand(d, generator=g, device=dev()) * 0.9, "h0": rand(B, d),
+         "do": rand(B * T, d).to(dt), "dh": rand(B, d)}
+    a = run(mmf, v, B, T)
+    total = torch.zeros(d, device=dev(), dtype=torch.float64)
+    for b in range(B):
+        s, r = slice(b * T, (b + 1) * T), slice(b, b + 1)
+        one = run(mmf, {"z": v["z"][s], "lb": v["lb"], "h0": v["h0"][r], "do": v["do"][s], "dh": v["dh"][r]}, 1, T)
+        assert torch.equal(a["o"][s], one["o"]) and torch.equal(a["dz"][s], one["dz"])
+        assert torch.equal(a["h"][r], one["h"]) and torch.equal(a["dh0"][r], one["dh0"])
+        total += one["dlb"].double()
+    # the same fp64 sums, rounded once, or once per sequence
+    assert ((a["dlb"].double() - total).abs() <= U * (total.abs() + B * 2 ** 11)).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [60, 300])
 def test_saturated_gates(mmf, T):
     """Forget gates of exactly 0 and 1 (long memories), candidates far out."""
