@@ -463,32 +463,34 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
         out, 0, static_cast<int>(static_cast<uint32_t>(M) * L * 4u), kBufferFlags);
     // every load of the wave's gradients in flight before the first is used
     // (the k loop's fragments are free by now)
-    auto place = [&](int fm, int f, uint32_t& row, uint32_t& ch) -> bool {
-      const int m = m0 + wm * WM + fm * 16 + el16;
-      row = static_cast<uint32_t>(m) * L;
-      ch = static_cast<uint32_t>((n0 + wn * WN) / 2 + f * 16 + 4 * eg);
-      return m < M && ch < L;
-    };
     constexpr int kDpWords = kDp == 4 ? 4 : 2;
+    const uint32_t cw = static_cast<uint32_t>((n0 + wn * WN) / 2);  // the wave's first channel
     Words<kDpWords> dpw[FM][FN / 2];
 #pragma unroll
     for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
       for (int f = 0; f < FN / 2; ++f) {
-        uint32_t row, ch;
-        const bool ok = place(fm, f, row, ch);
-        dpw[fm][f] = load_words<kDpWords>(grsrc, ok ? kDp * (row + ch) : kOut, 0);
+        const int m = m0 + wm * WM + fm * 16 + el16;
+        const uint32_t ch = cw + f * 16 + 4 * eg;
+        dpw[fm][f] = load_words<kDpWords>(
+            grsrc, m < M && ch < L ? kDp * (static_cast<uint32_t>(m) * L + ch) : kOut, 0);
       }
     __builtin_amdgcn_sched_barrier(0);
+    // A lane ends up with four channels of either 16-channel block; lanes 16
+    // apart exchange halves (row eg of 16 lanes even: eight of the first
+    // block, odd: of the second), so that a wave stores 64 contiguous bytes
+    // of dg and of du per row with one 16-byte store each.
+    static_assert(FN == 4, "two blocks of channels per wave");
+    const uint32_t ch8 = cw + (eg & 1) * 16 + (eg >> 1) * 8;
 #pragma unroll
     for (int fm = 0; fm < FM; ++fm) {
       const int lr = wm * WM + fm * 16 + el16;
+      const int m = m0 + lr;
       const int rs = s_rsum[lr];
       const float sg = s_scale[lr] * ws, su = s_scale[lr] * ws_u;
+      uint32_t g2[2][2], u2[2][2];  // [block][pair of channels]
 #pragma unroll
-      for (int f = 0; f < FN / 2; ++f) {
-        uint32_t row, ch;
-        const bool ok = place(fm, f, row, ch);
+      for (int f = 0; f < 2; ++f) {
         float dg[4], du[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -500,13 +502,20 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
           du[r] = dp * (gv * s);
           dg[r] = dp * uv * (s * (1.0f + gv * (1.0f - s)));
         }
-        const uint32_t at = 2u * (2u * row + ch);
-        typedef unsigned int v2u __attribute__((ext_vector_type(2)));
-        __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3])}, orsrc,
-                                              ok ? at : kOut, 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3])}, orsrc,
-                                              ok ? at + 2u * L : kOut, 0, 0);
+        g2[f][0] = pack_bf16(dg[0], dg[1]);
+        g2[f][1] = pack_bf16(dg[2], dg[3]);
+        u2[f][0] = pack_bf16(du[0], du[1]);
+        u2[f][1] = pack_bf16(du[2], du[3]);
       }
+      auto pieces = [](const uint32_t (&v)[2][2]) -> v4i {
+        const auto a = __builtin_amdgcn_permlane16_swap(v[0][0], v[1][0], false, false);
+        const auto b = __builtin_amdgcn_permlane16_swap(v[0][1], v[1][1], false, false);
+        return v4i{static_cast<int>(a[0]), static_cast<int>(b[0]), static_cast<int>(a[1]), static_cast<int>(b[1])};
+      };
+      const bool ok = m < M && ch8 < L;
+      const uint32_t at = 2u * (2u * static_cast<uint32_t>(m) * L + ch8);
+      __builtin_amdgcn_raw_buffer_store_b128(pieces(g2), orsrc, ok ? at : kOut, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(pieces(u2), orsrc, ok ? at + 2u * L : kOut, 0, 0);
     }
   } else if constexpr (!kStaged) {
     const int ow = kGlu ? N / 2 : N;  // output row length
