@@ -231,6 +231,9 @@ __global__ __launch_bounds__(kThreads) void mlgru_train_fwd_kernel(const FwdArgs
     m = {m.ax * f[u].x, fmaf(f[u].x, m.bx, c[u].x), m.ay * f[u].y, fmaf(f[u].y, m.by, c[u].y)};
   }
   maps[p.sub][p.lane] = m;
+  // h0 is read before the chunk's map is published: h_last, which may be the
+  // same array, is written by a chunk that has read the maps before it
+  asm volatile("" : "+v"(H.x), "+v"(H.y) : : "memory");
   __syncthreads();
   const int64_t at = (p.b * a.nchunk + p.k) * d + p.c;
   Map2 whole = kSame;

@@ -120,6 +120,24 @@ def test_forward_past_the_last_level_cache(mmf, xt, bt):
 
 
 @pytest.mark.gpu
+def test_offsets_past_32_bits(mmf):
+    """Arrays of 4.9 GB: the last rows as in calls of their own."""
+    M, K, n = 600_000, 2048, 37
+    g = gen(11)
+    x, b = rand(g, M, K), rand(g, M, K, dtype=BF)
+    s, q, a, rs, r = mmf.add_act_quant(x, b, None)
+    tail = slice(M - n, M)
+    s2, q2, a2, rs2, r2 = mmf.add_act_quant(x[tail], b[tail], None)
+    for u, v in ((s, s2), (q, q2), (a, a2), (rs, rs2), (r, r2)):
+        assert torch.equal(u[tail], v)
+    ds, dh = torch.empty_like(s), torch.empty((M, K), dtype=BF, device=dev())
+    mmf.mmf_add_act_quant_bwd(b, x, s, None, r, ds, dh, None)
+    ds2, dh2 = torch.empty_like(s2), torch.empty((n, K), dtype=BF, device=dev())
+    mmf.mmf_add_act_quant_bwd(b[tail], x[tail], s2, None, r2, ds2, dh2, None)
+    assert torch.equal(ds[tail], ds2) and torch.equal(dh[tail], dh2)
+
+
+@pytest.mark.gpu
 def test_backward_past_the_last_level_cache(mmf):
     check_bwd(mmf, 8001, 2288, BF, F32)
     check_bwd(mmf, 30001, 1040, F32, BF, in_place=True)

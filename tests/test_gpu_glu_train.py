@@ -94,6 +94,23 @@ def test_gate_gradients(mmf, M, K, L, tile, dt):
 
 
 @pytest.mark.gpu
+def test_row_slices(mmf):
+    """q of more than 2^31 bytes: the rows of the second launch as in a call
+    of their own."""
+    M, K, L, n = 1_060_000, 2048, 32, 300
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q = torch.randint(-127, 128, (M, K), generator=g, dtype=torch.int8, device=dev())
+    a, rs = torch.rand(M, generator=g, device=dev()) * 0.01, q.sum(1, dtype=torch.int32)
+    Wp, s = mmf.ternarize(torch.randn((2 * L, K), generator=g, device=dev()))
+    dp = torch.randn((M, L), generator=g, device=dev())
+    ws, tail = torch.tensor([0.5, 2.0], device=dev()), slice(M - n, M)
+    dgu, one = (torch.empty((m, 2 * L), dtype=BF, device=dev()) for m in (M, n))
+    mmf.mmf_glu_gate_bwd(q, a, rs, Wp, ws, dp, dgu)
+    mmf.mmf_glu_gate_bwd(q[tail], a[tail].clone(), rs[tail].clone(), Wp, ws, dp[tail], one)
+    assert torch.equal(dgu[tail], one)
+
+
+@pytest.mark.gpu
 def test_gate_gradients_far_out(mmf):
     """Gates where the sigmoid saturates, gradients of 0."""
     M, K, L = 70, 64, 48

@@ -100,6 +100,19 @@ def test_one_large_tensor(mmf):
 
 
 @pytest.mark.gpu
+def test_offsets_past_32_bits(mmf):
+    """One array of 4.4 GB: ones, whose squares sum up exactly."""
+    n = 1_100_000_003
+    g = torch.ones(n, device=dev())
+    norm = torch.zeros(1, device=dev())
+    mmf.mmf_grad_norm([g], norm)
+    assert abs(float(norm) - n ** 0.5) <= U * n ** 0.5
+    mmf.mmf_grad_clip([g], norm, 1.0)
+    c = float(factor(float(norm), 1.0))
+    assert float(g.min()) == c and float(g.max()) == c
+
+
+@pytest.mark.gpu
 def test_small_and_large_values(mmf):
     """Squares that fp32 could not hold."""
     check(mmf, [1000, 33], 1.0, scale=1e-25)

@@ -158,6 +158,12 @@ def test_optional_inputs(mmf, B, T, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [129, 1500, 2500])
+def test_state_in_place_over_several_chunks(mmf, T):
+    check(mmf, make(6, 2, T, 80, F32), 2, T, h_last_is_h0=True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
 def test_past_the_last_level_cache(mmf, dt):
     """Four sequences that together exceed 256 MB, and so pass as streams:
@@ -177,6 +183,22 @@ def test_past_the_last_level_cache(mmf, dt):
         total += one["dlb"].double()
     # the same fp64 sums, rounded once, or once per sequence
     assert ((a["dlb"].double() - total).abs() <= U * (total.abs() + B * 2 ** 11)).all()
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits(mmf):
+    """z of 4.4 GB: the last sequence as in a call of its own."""
+    B, T, d = 44, 4096, 2048
+    g = torch.Generator(device="cuda").manual_seed(10)
+    v = {"z": torch.randn((B * T, 3 * d), generator=g, device=dev()), "lb": None,
+         "h0": torch.randn((B, d), generator=g, device=dev()),
+         "do": torch.randn((B * T, d), generator=g, device=dev()), "dh": None}
+    assert v["z"].numel() * 4 > 1 << 32
+    a = run(mmf, v, B, T)
+    s, r = slice((B - 1) * T, B * T), slice(B - 1, B)
+    one = run(mmf, {"z": v["z"][s], "lb": None, "h0": v["h0"][r], "do": v["do"][s], "dh": None}, 1, T)
+    assert torch.equal(a["o"][s], one["o"]) and torch.equal(a["dz"][s], one["dz"])
+    assert torch.equal(a["h"][r], one["h"]) and torch.equal(a["dh0"][r], one["dh0"])
 
 
 @pytest.mark.gpu
