@@ -153,16 +153,36 @@ def _need(t: torch.Tensor, name: str, dtype, shape) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
-def _need_here(t: torch.Tensor, name: str, dtype, shape) -> None:
-    """_need, and on the current device: the call is enqueued there."""
+# The current device, asked once per call (0.13 us each), or one that no tensor
+# is on where there is none.
+def _here() -> int:
     try:
-        if (t.dtype is dtype and t.get_device() == torch._C._cuda_getDevice() and t.shape == shape
-                and t.is_contiguous()):
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -2
+
+
+def _need_here(t: torch.Tensor, name: str, dtype, shape, here: int) -> None:
+    """_need, and on the current device `here`: the call is enqueued there."""
+    try:
+        if t.dtype is dtype and t.get_device() == here and t.shape == shape and t.is_contiguous():
             return
-    except (AttributeError, RuntimeError):  # not a tensor, no device: the check below says so
+    except AttributeError:  # not a tensor: the check below says so
         pass
     _need(t, name, dtype, shape)
     raise ValueError(f"{name} must be on the current device, cuda:{torch.cuda.current_device()}")
+
+
+def _ws_here(workspace: torch.Tensor | None, here: int):
+    if workspace is None:
+        return None, 0
+    n = workspace.numel()
+    _need_here(workspace, "workspace", torch.uint8, (n,), here)
+    return workspace.data_ptr(), n
+
+
+def _stream_here(stream, here: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
 
 
 def _x_kind(x: torch.Tensor) -> bool:
@@ -258,25 +278,26 @@ def mmf_add_act_quant(x: torch.Tensor, branch: torch.Tensor | None, gamma: torch
     quantisation as mmf_act_quant gives it: q int8 [M][K], a_scale f32 [M],
     q_rowsum i32 [M], rstd f32 [M].  branch bf16/f32 [M][K], or None: s = x,
     which may be None."""
+    here = _here()
     M, K = x.shape
     is_f32 = _x_kind(x)
-    _need_here(x, "x", x.dtype, (M, K))
+    _need_here(x, "x", x.dtype, (M, K), here)
     branch_f32 = False
     if branch is not None:
         branch_f32 = _kind(branch, "branch")
-        _need_here(branch, "branch", branch.dtype, (M, K))
+        _need_here(branch, "branch", branch.dtype, (M, K), here)
     if gamma is not None:
-        _need_here(gamma, "gamma", torch.float32, (K,))
+        _need_here(gamma, "gamma", torch.float32, (K,), here)
     if s is not None or branch is not None:
-        _need_here(s, "s", x.dtype, (M, K))
-    _need_here(q, "q", torch.int8, (M, K))
-    _need_here(a_scale, "a_scale", torch.float32, (M,))
+        _need_here(s, "s", x.dtype, (M, K), here)
+    _need_here(q, "q", torch.int8, (M, K), here)
+    _need_here(a_scale, "a_scale", torch.float32, (M,), here)
     if q_rowsum is not None:
-        _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
+        _need_here(q_rowsum, "q_rowsum", torch.int32, (M,), here)
     if rstd is not None:
-        _need_here(rstd, "rstd", torch.float32, (M,))
+        _need_here(rstd, "rstd", torch.float32, (M,), here)
     _check(_lib.mmf_add_act_quant(_ptr(x), is_f32, _ptr(branch), branch_f32, _ptr(gamma), _ptr(s), _ptr(q),
-                                  _ptr(a_scale), _ptr(q_rowsum), _ptr(rstd), M, K, _stream(stream)))
+                                  _ptr(a_scale), _ptr(q_rowsum), _ptr(rstd), M, K, _stream_here(stream, here)))
 
 
 def mmf_add_act_quant_bwd_workspace_bytes(M: int, K: int) -> int:
@@ -290,23 +311,24 @@ def mmf_add_act_quant_bwd(dY: torch.Tensor, ds_out: torch.Tensor | None, s: torc
     """Backward: ds f32 [M][K] (may be ds_out), the same in bf16 (or None) and
     dgamma f32 [K] (or None) from dY bf16/f32 [M][K], the residual stream's
     gradient ds_out f32 [M][K] (or None) and the forward's s and rstd."""
+    here = _here()
     M, K = s.shape
     s_f32, dy_f32 = _kind(s, "s"), _kind(dY, "dY")
-    _need_here(dY, "dY", dY.dtype, (M, K))
+    _need_here(dY, "dY", dY.dtype, (M, K), here)
     if ds_out is not None:
-        _need_here(ds_out, "ds_out", torch.float32, (M, K))
-    _need_here(s, "s", s.dtype, (M, K))
+        _need_here(ds_out, "ds_out", torch.float32, (M, K), here)
+    _need_here(s, "s", s.dtype, (M, K), here)
     if gamma is not None:
-        _need_here(gamma, "gamma", torch.float32, (K,))
-    _need_here(rstd, "rstd", torch.float32, (M,))
-    _need_here(ds, "ds", torch.float32, (M, K))
+        _need_here(gamma, "gamma", torch.float32, (K,), here)
+    _need_here(rstd, "rstd", torch.float32, (M,), here)
+    _need_here(ds, "ds", torch.float32, (M, K), here)
     if ds_bf16 is not None:
-        _need_here(ds_bf16, "ds_bf16", torch.bfloat16, (M, K))
+        _need_here(ds_bf16, "ds_bf16", torch.bfloat16, (M, K), here)
     if dgamma is not None:
-        _need_here(dgamma, "dgamma", torch.float32, (K,))
-    wp, wn = _ws_args(workspace)
+        _need_here(dgamma, "dgamma", torch.float32, (K,), here)
+    wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_add_act_quant_bwd(_ptr(dY), dy_f32, _ptr(ds_out), _ptr(s), s_f32, _ptr(gamma), _ptr(rstd),
-                                      _ptr(ds), _ptr(ds_bf16), _ptr(dgamma), M, K, wp, wn, _stream(stream)))
+                                      _ptr(ds), _ptr(ds_bf16), _ptr(dgamma), M, K, wp, wn, _stream_here(stream, here)))
 
 
 def mmf_bitlinear_fwd(x: torch.Tensor, gamma: torch.Tensor | None, Wpacked: torch.Tensor,
@@ -604,19 +626,20 @@ def mmf_mlgru_train_scan(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | Non
     [B][d] (or None; may be h0) from the gates' pre-activations z f32 [B*T][3d]
     (f | c | g), lb f32 [d] or None and h0 f32 [B][d] or None; states uint8
     (mmf_mlgru_train_states_bytes) keeps what mmf_mlgru_scan_bwd starts from."""
+    here = _here()
     d = z.shape[1] // 3
-    _need_here(z, "z", torch.float32, (B * T, 3 * d))
+    _need_here(z, "z", torch.float32, (B * T, 3 * d), here)
     if lb is not None:
-        _need_here(lb, "lb", torch.float32, (d,))
+        _need_here(lb, "lb", torch.float32, (d,), here)
     if h0 is not None:
-        _need_here(h0, "h0", torch.float32, (B, d))
-    _need_here(o_prime, "o_prime", torch.float32, (B * T, d))
+        _need_here(h0, "h0", torch.float32, (B, d), here)
+    _need_here(o_prime, "o_prime", torch.float32, (B * T, d), here)
     if h_last is not None:
-        _need_here(h_last, "h_last", torch.float32, (B, d))
-    _need_here(states, "states", torch.uint8, (states.numel(),))
-    wp, wn = _ws_args(workspace)
+        _need_here(h_last, "h_last", torch.float32, (B, d), here)
+    _need_here(states, "states", torch.uint8, (states.numel(),), here)
+    wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_mlgru_train_scan(_ptr(z), _ptr(lb), _ptr(h0), _ptr(o_prime), _ptr(h_last), _ptr(states),
-                                     states.numel(), B, T, d, wp, wn, _stream(stream)))
+                                     states.numel(), B, T, d, wp, wn, _stream_here(stream, here)))
 
 
 def mmf_mlgru_scan_bwd(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None, states: torch.Tensor,
@@ -627,23 +650,25 @@ def mmf_mlgru_scan_bwd(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None,
     mmf_bitlinear_bwd), dh0 f32 [B][d] (or None) and dlb f32 [d] (or None) from
     do_prime bf16/f32 [B*T][d], dh_last f32 [B][d] (or None) and the forward's
     z, lb and states."""
+    here = _here()
     d = z.shape[1] // 3
     do_f32 = _kind(do_prime, "do_prime")
-    _need_here(z, "z", torch.float32, (B * T, 3 * d))
+    _need_here(z, "z", torch.float32, (B * T, 3 * d), here)
     if lb is not None:
-        _need_here(lb, "lb", torch.float32, (d,))
-    _need_here(states, "states", torch.uint8, (states.numel(),))
-    _need_here(do_prime, "do_prime", do_prime.dtype, (B * T, d))
+        _need_here(lb, "lb", torch.float32, (d,), here)
+    _need_here(states, "states", torch.uint8, (states.numel(),), here)
+    _need_here(do_prime, "do_prime", do_prime.dtype, (B * T, d), here)
     if dh_last is not None:
-        _need_here(dh_last, "dh_last", torch.float32, (B, d))
-    _need_here(dz, "dz", torch.bfloat16, (B * T, 3 * d))
+        _need_here(dh_last, "dh_last", torch.float32, (B, d), here)
+    _need_here(dz, "dz", torch.bfloat16, (B * T, 3 * d), here)
     if dh0 is not None:
-        _need_here(dh0, "dh0", torch.float32, (B, d))
+        _need_here(dh0, "dh0", torch.float32, (B, d), here)
     if dlb is not None:
-        _need_here(dlb, "dlb", torch.float32, (d,))
-    wp, wn = _ws_args(workspace)
+        _need_here(dlb, "dlb", torch.float32, (d,), here)
+    wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_mlgru_scan_bwd(_ptr(z), _ptr(lb), _ptr(states), states.numel(), _ptr(do_prime), do_f32,
-                                   _ptr(dh_last), _ptr(dz), _ptr(dh0), _ptr(dlb), B, T, d, wp, wn, _stream(stream)))
+                                   _ptr(dh_last), _ptr(dz), _ptr(dh0), _ptr(dlb), B, T, d, wp, wn,
+                                   _stream_here(stream, here)))
 
 
 def mmf_glu_train_workspace_bytes(M: int, K: int, L: int) -> int:
@@ -660,18 +685,19 @@ def mmf_glu_train_fwd(q: torch.Tensor, a_scale: torch.Tensor, q_rowsum: torch.Te
     """Training forward of the GLU's gated up-projections from quantised
     activations and the stacked latent weights W f32 [2L][K] (gate, up): p f32
     [M][L], and Wpacked int32 [K/16][2L] and w_scale f32 [1] for the backward."""
+    here = _here()
     M, K = q.shape
     L = W.shape[0] // 2
-    _need_here(q, "q", torch.int8, (M, K))
-    _need_here(a_scale, "a_scale", torch.float32, (M,))
-    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
-    _need_here(W, "W", torch.float32, (2 * L, K))
-    _need_here(p, "p", torch.float32, (M, L))
-    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L))
-    _need_here(w_scale, "w_scale", torch.float32, (1,))
-    wp, wn = _ws_args(workspace)
+    _need_here(q, "q", torch.int8, (M, K), here)
+    _need_here(a_scale, "a_scale", torch.float32, (M,), here)
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,), here)
+    _need_here(W, "W", torch.float32, (2 * L, K), here)
+    _need_here(p, "p", torch.float32, (M, L), here)
+    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L), here)
+    _need_here(w_scale, "w_scale", torch.float32, (1,), here)
+    wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_glu_train_fwd(_ptr(q), _ptr(a_scale), _ptr(q_rowsum), _ptr(W), _ptr(p), _ptr(Wpacked),
-                                  _ptr(w_scale), M, K, L, wp, wn, _stream(stream)))
+                                  _ptr(w_scale), M, K, L, wp, wn, _stream_here(stream, here)))
 
 
 def mmf_glu_gate_bwd(q: torch.Tensor, a_scale: torch.Tensor, q_rowsum: torch.Tensor, Wgu_packed: torch.Tensor,
@@ -679,18 +705,19 @@ def mmf_glu_gate_bwd(q: torch.Tensor, a_scale: torch.Tensor, q_rowsum: torch.Ten
     """The GLU gate's gradients dgu bf16 [M][2L] (dg | du) from dp bf16/f32
     [M][L], the projections recomputed from the quantised activations and the
     interleaved packed weights [K/16][2L] with w_scales [gate, up]."""
+    here = _here()
     M, K = q.shape
     L = Wgu_packed.shape[1] // 2
     dp_f32 = _kind(dp, "dp")
-    _need_here(q, "q", torch.int8, (M, K))
-    _need_here(a_scale, "a_scale", torch.float32, (M,))
-    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
-    _need_here(Wgu_packed, "Wgu_packed", torch.int32, (K // 16, 2 * L))
-    _need_here(w_scales, "w_scales", torch.float32, (2,))
-    _need_here(dp, "dp", dp.dtype, (M, L))
-    _need_here(dgu, "dgu", torch.bfloat16, (M, 2 * L))
+    _need_here(q, "q", torch.int8, (M, K), here)
+    _need_here(a_scale, "a_scale", torch.float32, (M,), here)
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,), here)
+    _need_here(Wgu_packed, "Wgu_packed", torch.int32, (K // 16, 2 * L), here)
+    _need_here(w_scales, "w_scales", torch.float32, (2,), here)
+    _need_here(dp, "dp", dp.dtype, (M, L), here)
+    _need_here(dgu, "dgu", torch.bfloat16, (M, 2 * L), here)
     _check(_lib.mmf_glu_gate_bwd(_ptr(q), _ptr(a_scale), _ptr(q_rowsum), _ptr(Wgu_packed), _ptr(w_scales), _ptr(dp),
-                                 dp_f32, _ptr(dgu), M, K, L, _stream(stream)))
+                                 dp_f32, _ptr(dgu), M, K, L, _stream_here(stream, here)))
 
 
 def mmf_glu_bwd(dp: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, rstd: torch.Tensor, q: torch.Tensor,
@@ -701,27 +728,28 @@ def mmf_glu_bwd(dp: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, r
     [2L][K] (gate, up) and dgamma f32 [K] (or None) from dp bf16/f32 [M][L], the
     input x bf16/f32 [M][K] with gamma, rstd, q, a_scale and q_rowsum, and
     mmf_glu_train_fwd's Wpacked and w_scale."""
+    here = _here()
     M, K = x.shape
     L = Wpacked.shape[1] // 2
     is_f32, dp_f32 = _x_kind(x), _kind(dp, "dp")
-    _need_here(dp, "dp", dp.dtype, (M, L))
-    _need_here(x, "x", x.dtype, (M, K))
+    _need_here(dp, "dp", dp.dtype, (M, L), here)
+    _need_here(x, "x", x.dtype, (M, K), here)
     if gamma is not None:
-        _need_here(gamma, "gamma", torch.float32, (K,))
-    _need_here(rstd, "rstd", torch.float32, (M,))
-    _need_here(q, "q", torch.int8, (M, K))
-    _need_here(a_scale, "a_scale", torch.float32, (M,))
-    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,))
-    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L))
-    _need_here(w_scale, "w_scale", torch.float32, (1,))
-    _need_here(dx, "dx", torch.float32, (M, K))
-    _need_here(dW, "dW", torch.float32, (2 * L, K))
+        _need_here(gamma, "gamma", torch.float32, (K,), here)
+    _need_here(rstd, "rstd", torch.float32, (M,), here)
+    _need_here(q, "q", torch.int8, (M, K), here)
+    _need_here(a_scale, "a_scale", torch.float32, (M,), here)
+    _need_here(q_rowsum, "q_rowsum", torch.int32, (M,), here)
+    _need_here(Wpacked, "Wpacked", torch.int32, (K // 16, 2 * L), here)
+    _need_here(w_scale, "w_scale", torch.float32, (1,), here)
+    _need_here(dx, "dx", torch.float32, (M, K), here)
+    _need_here(dW, "dW", torch.float32, (2 * L, K), here)
     if dgamma is not None:
-        _need_here(dgamma, "dgamma", torch.float32, (K,))
-    wp, wn = _ws_args(workspace)
+        _need_here(dgamma, "dgamma", torch.float32, (K,), here)
+    wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_glu_bwd(_ptr(dp), dp_f32, _ptr(x), is_f32, _ptr(gamma), _ptr(rstd), _ptr(q), _ptr(a_scale),
                             _ptr(q_rowsum), _ptr(Wpacked), _ptr(w_scale), _ptr(dx), _ptr(dW), _ptr(dgamma), M, K, L,
-                            wp, wn, _stream(stream)))
+                            wp, wn, _stream_here(stream, here)))
 
 
 # Lists of tensors: checked and converted by map over whole lists, and passed
@@ -731,11 +759,11 @@ _T = torch.Tensor
 _dtype_of = operator.attrgetter("dtype")
 
 
-def _grad_ptrs(tensors, name):
+def _grad_ptrs(tensors, name, here):
     """Addresses of a list of contiguous bf16 or f32 tensors on the current device, and their types."""
     try:
         kinds = list(map(_dtype_of, tensors))
-        if (all(map(_T.is_contiguous, tensors)) and not set(map(_T.get_device, tensors)) - {torch._C._cuda_getDevice()}
+        if (all(map(_T.is_contiguous, tensors)) and not set(map(_T.get_device, tensors)) - {here}
                 and not set(kinds) - {torch.float32, torch.bfloat16}):
             return list(map(_T.data_ptr, tensors)), kinds
     except (AttributeError, TypeError, RuntimeError):
@@ -744,13 +772,13 @@ def _grad_ptrs(tensors, name):
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name}[{i}] must be a torch.Tensor")
         _kind(t, f"{name}[{i}]")
-        _need_here(t, f"{name}[{i}]", t.dtype, t.shape)
+        _need_here(t, f"{name}[{i}]", t.dtype, t.shape, here)
     raise ValueError(f"{name} must be tensors on the current device")
 
 
-def _grad_set(tensors):
+def _grad_set(tensors, here):
     """What the C calls take: arrays of addresses, kinds and sizes, and the types."""
-    ptrs, types = _grad_ptrs(tensors, "grads")
+    ptrs, types = _grad_ptrs(tensors, "grads", here)
     return (array.array("Q", ptrs), array.array("i", [k is torch.float32 for k in types]),
             array.array("q", map(_T.numel, tensors)), types)
 
@@ -767,25 +795,28 @@ def mmf_grad_norm_workspace_bytes(counts) -> int:
 def mmf_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
     """norm f32 [1] = the 2-norm over all elements of the tensors of the list
     `grads` (each bf16 or f32, contiguous, of any shape)."""
-    _need_here(norm, "norm", torch.float32, (1,))
-    ptrs, kinds, counts, _ = _grad_set(grads)
-    wp, wn = _ws_args(workspace)
-    _check(_lib.mmf_grad_norm(_at(ptrs), _at(kinds), _at(counts), len(ptrs), _ptr(norm), wp, wn, _stream(stream)))
+    here = _here()
+    _need_here(norm, "norm", torch.float32, (1,), here)
+    ptrs, kinds, counts, _ = _grad_set(grads, here)
+    wp, wn = _ws_here(workspace, here)
+    _check(_lib.mmf_grad_norm(_at(ptrs), _at(kinds), _at(counts), len(ptrs), _ptr(norm), wp, wn,
+                              _stream_here(stream, here)))
 
 
 def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=None) -> None:
     """outs[i] = grads[i] * min(max_norm / (norm + 1e-6), 1); outs None: in
     place.  outs[i] has the type and the number of elements of grads[i]."""
-    _need_here(norm, "norm", torch.float32, (1,))
-    ptrs, kinds, counts, types = _grad_set(grads)
+    here = _here()
+    _need_here(norm, "norm", torch.float32, (1,), here)
+    ptrs, kinds, counts, types = _grad_set(grads, here)
     dst = ptrs
     if outs is not None:
-        optrs, otypes = _grad_ptrs(outs, "outs")
+        optrs, otypes = _grad_ptrs(outs, "outs", here)
         if otypes != types or list(map(_T.numel, outs)) != counts.tolist():
             raise ValueError("outs must have the types and numbers of elements of grads")
         dst = array.array("Q", optrs)
     _check(_lib.mmf_grad_clip(_at(ptrs), _at(kinds), _at(counts), len(ptrs), _ptr(norm), max_norm, _at(dst),
-                              _stream(stream)))
+                              _stream_here(stream, here)))
 
 
 def mmf_bitlinear_train_workspace_bytes(M: int, K: int, N: int) -> int:
