@@ -504,7 +504,8 @@ int mmf_bitlinear_bwd(const uint16_t *dO, const void *x, int x_is_f32, const flo
  * stacked layers.  dp [M][L] bf16 bits or float32 (dp_is_f32), the gradient of
  * p (float32 as mmf_bitlinear_bwd of the down-projection leaves it);
  * Wgu_packed [K/16][2L] interleaved by mmf_glu_pack, w_scales [2]: gate, up.
- * Allocates nothing.
+ * The kernels of mmf_ternary_gemm_glu (the same bits from each).  Allocates
+ * nothing.
  *
  * mmf_glu_bwd is the whole backward: that stage, then mmf_bitlinear_bwd of the
  * stacked layers with N = 2L (the same kernels, so the results of the two

@@ -309,12 +309,12 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
                  : "s"(dst), "v"(off), "s"(desc)
                  : "memory", "m0");
   }
-  // Paired tiles with the GLU epilogue: the k loop's waves issue ahead of the
+  // Paired tiles with the GLU epilogues: the k loop's waves issue ahead of the
   // other workgroup's epilogue on the same SIMD (its SiLU arithmetic and
-  // direct stores), which keeps the matrix cores fed (glu_gate 4-5 % faster;
+  // direct stores), which keeps the matrix cores fed (glu_gate 4-5 % faster,
+  // the gate's gradients 1.5 %;
   // the dequantising epilogue measured level and keeps the default).
-  constexpr bool kLoopPriority =
-      T::kWaves == 4 && (EP == Epilogue::kGluF32 || EP == Epilogue::kGluGradF32 || EP == Epilogue::kGluGradBf16);
+  constexpr bool kLoopPriority = T::kWaves == 4 && is_glu(EP);
   if constexpr (kLoopPriority) __builtin_amdgcn_s_setprio(1);
   // Prologue: stages 0 .. S-2, wait for stage 0 (and the row factors).
 #pragma unroll
@@ -395,7 +395,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   const int el16 = elane & 15, eg = elane >> 4;
   const int* s_rsum = reinterpret_cast<const int*>(smem + S * T::kStageBytes);
   const float* s_scale = reinterpret_cast<const float*>(smem + S * T::kStageBytes + 4 * BM);
-  constexpr bool kGluGrad = EP == Epilogue::kGluGradF32 || EP == Epilogue::kGluGradBf16;
+  constexpr bool kGluGrad = is_glu_grad(EP);
   const float ws = (EP == Epilogue::kDequantF32 || EP == Epilogue::kGluF32 || kGluGrad) ? w_scale[0] : 0.0f;
   const float ws_u = (EP == Epilogue::kGluF32 || kGluGrad) ? w_scale[1] : 0.0f;
   __syncthreads();
@@ -451,9 +451,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   static_assert(!RAG || kStaged, "ragged rows leave through the staged stores");
   static_assert(!BIAS || (kStaged && !RAG && EP == Epilogue::kDequantF32), "the bias is added at the staged stores");
   if constexpr (kGluGrad) {
-    // The gate's gradients.  With s = sigmoid(g) and dp the gradient of
-    // p = g s u:  du = dp g s,  dg = dp u s (1 + g (1 - s)),  fp32, each
-    // rounded once to bf16.  g and u carry the bits of the forward.
+    // The gate's gradients (glu_grad), each rounded once to bf16.  g and u
+    // carry the bits of the forward.
     static_assert(BX4 && !RAG && !BIAS, "L % 16 == 0");
     constexpr int kDp = EP == Epilogue::kGluGradF32 ? 4 : 2;  // bytes of a gradient
     const uint32_t L = static_cast<uint32_t>(N) / 2;
@@ -498,9 +497,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
                                     : (r & 1 ? bf16_hi(dpw[fm][f].w[r / 2]) : bf16_lo(dpw[fm][f].w[r / 2]));
           const float gv = static_cast<float>(acc[fm][2 * f][r] - rs) * sg;
           const float uv = static_cast<float>(acc[fm][2 * f + 1][r] - rs) * su;
-          const float s = sigmoid_hw(gv);
-          du[r] = dp * (gv * s);
-          dg[r] = dp * uv * (s * (1.0f + gv * (1.0f - s)));
+          glu_grad(gv, uv, dp, dg[r], du[r]);
         }
         g2[f][0] = pack_bf16(dg[0], dg[1]);
         g2[f][1] = pack_bf16(dg[2], dg[3]);

@@ -509,14 +509,15 @@ int check_glu_train(int64_t M, int64_t K, int64_t L) {
   return M == 0 || L == 0 ? MMF_OK : check_gemm(K, 2 * L);
 }
 // The gate's gradients from the recomputed projections.
-hipError_t glu_gate_bwd(const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wgu,
+hipError_t glu_gate_bwd(int path, const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wgu,
                         const float* w_scales, const void* dp, bool dp_is_f32, uint16_t* dgu, int64_t M, int64_t K,
                         int64_t L, hipStream_t stream) {
   mmf::Affine aff;
   aff.grad = dp;
-  return mmf::launch_gemm({q, a_scale, q_rowsum, Wgu, w_scales, dgu, M, static_cast<int>(K), 2 * L,
-                           dp_is_f32 ? mmf::Epilogue::kGluGradF32 : mmf::Epilogue::kGluGradBf16, aff},
-                          stream);
+  return contract_mfma(path,
+                       {q, a_scale, q_rowsum, Wgu, w_scales, dgu, M, static_cast<int>(K), 2 * L,
+                        dp_is_f32 ? mmf::Epilogue::kGluGradF32 : mmf::Epilogue::kGluGradBf16, aff},
+                       stream);
 }
 // Scratch: the interleaved weights and their two scales, then (forward) the
 // ternarisation's partial sums or (backward) the gate's gradients [M][2L] and
@@ -1165,6 +1166,7 @@ int mmf_glu_train_fwd(const int8_t* q, const float* a_scale, const int32_t* q_ro
 int mmf_glu_gate_bwd(const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wgu_packed,
                      const float* w_scales, const void* dp, int dp_is_f32, uint16_t* dgu, int64_t M, int64_t K,
                      int64_t L, hipStream_t stream) {
+  const int path = current_path();
   if (int st = check_dtype(dp_is_f32)) return st;
   if (int st = check_glu_train(M, K, L)) return st;
   if (M == 0 || L == 0) return MMF_OK;
@@ -1172,7 +1174,7 @@ int mmf_glu_gate_bwd(const int8_t* q, const float* a_scale, const int32_t* q_row
   if (!aligned16(q) || !aligned16(a_scale) || !aligned16(q_rowsum) || !aligned16(Wgu_packed) || !aligned16(dp) ||
       !aligned16(dgu))
     return MMF_ERR_ALIGN;
-  return hip_status(glu_gate_bwd(q, a_scale, q_rowsum, Wgu_packed, w_scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream));
+  return hip_status(glu_gate_bwd(path, q, a_scale, q_rowsum, Wgu_packed, w_scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream));
 }
 
 size_t mmf_glu_bwd_workspace_bytes(int64_t M, int64_t K, int64_t L) {
@@ -1184,6 +1186,7 @@ int mmf_glu_bwd(const void* dp, int dp_is_f32, const void* x, int x_is_f32, cons
                 const int8_t* q, const float* a_scale, const int32_t* q_rowsum, const uint32_t* Wpacked,
                 const float* w_scale, float* dx, float* dW, float* dgamma, int64_t M, int64_t K, int64_t L,
                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int path = current_path();
   if (int st = check_dtype(dp_is_f32)) return st;
   if (int st = check_dtype(x_is_f32)) return st;
   if (int st = check_glu_train(M, K, L)) return st;
@@ -1202,7 +1205,7 @@ int mmf_glu_bwd(const void* dp, int dp_is_f32, const void* x, int x_is_f32, cons
     uint16_t* dgu = reinterpret_cast<uint16_t*>(scratch + g.end);
     if (mmf::launch_glu_pack(Wpacked, Wpacked + L, 2 * L, L, static_cast<int>(K), Wgu, w_scale, scales, stream) !=
             hipSuccess ||
-        glu_gate_bwd(q, a_scale, q_rowsum, Wgu, scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream) != hipSuccess)
+        glu_gate_bwd(path, q, a_scale, q_rowsum, Wgu, scales, dp, dp_is_f32 == 1, dgu, M, K, L, stream) != hipSuccess)
       return MMF_ERR_HIP;
     return run_bwd({dgu, x, x_is_f32 == 1, gamma, rstd, q, a_scale, Wpacked, w_scale, dx, dW, nullptr, dgamma, M, K,
                     2 * L},

@@ -216,6 +216,16 @@ __device__ __forceinline__ float mlgru_step(float h, float f, float c) { return 
 __device__ __forceinline__ float mlgru_out_gate(float g, float h) { return g * sigmoid_hw(h); }
 
 // ---------------------------------------------------------------------------
+// Gradients of the GLU's gate, p = g s u with s = sigmoid(g), from dp, fp32:
+//   du = dp g s,   dg = dp u s (1 + g (1 - s))
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void glu_grad(float g, float u, float dp, float& dg, float& du) {
+  const float s = sigmoid_hw(g);
+  du = dp * (g * s);
+  dg = dp * u * (s * (1.0f + g * (1.0f - s)));
+}
+
+// ---------------------------------------------------------------------------
 // Affine epilogue.  z = (float)acc * (a_scale * w_scale[s]) + bias[n] in
 // fp32, one rounding per operation, then the activation of segment s:
 // identity, (1 - lb) sigmoid(z) + lb (sigmoid with a lower bound) or

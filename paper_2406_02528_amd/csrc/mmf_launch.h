@@ -74,11 +74,13 @@ hipError_t launch_ternarize(const float* W, int64_t N, int K, uint32_t* Wpacked,
 // the two up-projections of a GLU interleaved in blocks of 16 (gate, up,
 // gate, ...), w_scale holds [gate, up], and the output is the gated
 // representation SiLU(g) * u, N / 2 columns wide.
-// kGluGradF32 / kGluGradBf16 (launch_gemm only): the columns of kGluF32, and
+// kGluGradF32 / kGluGradBf16 (the MFMA kernels): the columns of kGluF32, and
 // the output is [dg | du], the gradients of g and u in bf16 [M][N], from the
 // gradient of the gated representation (Affine::grad, [M][N/2] fp32 or bf16).
 enum class Epilogue { kDequantF32, kRawI32, kGluF32, kAffineF32, kGluGradF32, kGluGradBf16 };
-inline bool is_glu_grad(Epilogue e) { return e == Epilogue::kGluGradF32 || e == Epilogue::kGluGradBf16; }
+constexpr bool is_glu_grad(Epilogue e) { return e == Epilogue::kGluGradF32 || e == Epilogue::kGluGradBf16; }
+// Whether the packed columns are blocks of gate and up in turn.
+constexpr bool is_glu(Epilogue e) { return e == Epilogue::kGluF32 || is_glu_grad(e); }
 
 // kAffineF32: y = act_s(acc * a_scale * w_scale[s] + bias[n]) with the columns
 // in segments of `seg` (s = n / seg, seg % 16 == 0) and one activation per

@@ -22,7 +22,7 @@ SkinnyPlan skinny_plan(int64_t M, int K, int64_t N, Epilogue ep, int cus) {
   const double c = cus > 0 ? cus : 256;
   SkinnyPlan best;
   for (int fn = 1; fn <= 16; fn *= 2) {
-    if (ep == Epilogue::kGluF32 && fn < 2) continue;
+    if (is_glu(ep) && fn < 2) continue;
     for (int fm = 1; fm <= 4; ++fm) {
       if (fn == 16 && fm != 4) continue;  // the one form built: smaller ones never measured best
       const int64_t mb = (M + 16 * fm - 1) / (16 * fm), nb = (N + 16 * fn - 1) / (16 * fn);
@@ -55,7 +55,7 @@ static double skinny_us(const SkinnyPlan& p, int K, int64_t N, bool tiled) {
 bool skinny_fits(int64_t M, int K, int64_t N, Epilogue ep) {
   // 32-bit offsets: the packed weights
   if (M < 1 || N < 1 || static_cast<int64_t>(K / 16) * N * 4 >= (int64_t(1) << 31)) return false;
-  return ep == Epilogue::kGluF32 ? N % 32 == 0 : ep == Epilogue::kAffineF32 ? N % 4 == 0 : true;
+  return is_glu(ep) ? N % 32 == 0 : ep == Epilogue::kAffineF32 ? N % 4 == 0 : true;
 }
 
 bool skinny_beats_gemm(int64_t M, int K, int64_t N, Epilogue ep, bool tiled, int cus) {
@@ -85,6 +85,8 @@ hipError_t launch_skinny(const ContractArgs& a, bool tiled, hipStream_t stream) 
     case Epilogue::kRawI32: return launch_skinny_raw(a, p.fm, p.fn, tiled, stream);
     case Epilogue::kGluF32: return launch_skinny_glu(a, p.fm, p.fn, tiled, stream);
     case Epilogue::kAffineF32: return launch_skinny_affine(a, p.fm, p.fn, tiled, stream);
+    case Epilogue::kGluGradF32:
+    case Epilogue::kGluGradBf16: return launch_skinny_glu_grad(a, p.fm, p.fn, tiled, stream);
   }
   return hipErrorInvalidValue;
 }

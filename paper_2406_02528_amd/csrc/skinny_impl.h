@@ -40,6 +40,7 @@
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "q_layout.h"
+#include "row_vec.h"
 
 namespace mmf {
 namespace skinny {
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   constexpr int R = rows_per_round(FM, FN);
   constexpr int kStride = BN + 4;  // padded row of a partial tile: conflict-free 16-byte writes of 16 rows
   constexpr int kPart = 16 * R * kStride;
-  static_assert(EP != Epilogue::kGluF32 || (FN >= 2 && VEC), "whole gate/up block pairs per workgroup");
+  static_assert(!is_glu(EP) || (FN >= 2 && VEC), "whole gate/up block pairs per workgroup");
   static_assert(EP != Epilogue::kAffineF32 || VEC, "affine output needs N % 4 == 0");
   __shared__ __attribute__((aligned(16))) int part[kSplit * kPart];
   __shared__ float s_scale[16 * FM];
@@ -180,8 +181,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     my_rsum = p.q_rowsum[m0 + tid];
     if constexpr (EP != Epilogue::kRawI32) my_scale = p.a_scale[m0 + tid];
   }
-  const float ws = (EP == Epilogue::kDequantF32 || EP == Epilogue::kGluF32) ? p.w_scale[0] : 0.0f;
-  const float ws_u = EP == Epilogue::kGluF32 ? p.w_scale[1] : 0.0f;
+  const float ws = (EP == Epilogue::kDequantF32 || is_glu(EP)) ? p.w_scale[0] : 0.0f;
+  const float ws_u = is_glu(EP) ? p.w_scale[1] : 0.0f;
   ColAffine4 col{};
   if constexpr (EP == Epilogue::kAffineF32) {
     static_assert(kThreads % (BN / 4) == 0, "a thread keeps its column quad over the epilogue");
@@ -234,10 +235,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
     }
     lds_barrier();
-    constexpr int kW = EP == Epilogue::kGluF32 ? BN / 2 : BN;  // output columns of the tile
+    constexpr int kW = is_glu(EP) ? BN / 2 : BN;  // output columns of the tile
     constexpr int kQuads = kW / 4;
     const int live = (FM - f0 < R ? FM - f0 : R) * 16 * kQuads;
-    const int64_t ow = EP == Epilogue::kGluF32 ? N / 2 : N;
+    const int64_t ow = is_glu(EP) ? N / 2 : N;
     auto total = [&](int row, int c) -> v4i {
       v4i t = v4i{0, 0, 0, 0};
 #pragma unroll
@@ -251,7 +252,34 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int rs = s_rsum[tr];
       const float as = s_scale[tr];
       v4i v;
-      if constexpr (EP == Epilogue::kGluF32) {
+      if constexpr (is_glu_grad(EP)) {
+        // four channels' gradients of the gate and of the up projection
+        const int64_t at = (m0 + tr) * ow + n0 / 2 + 4 * cq;
+        const bool ok = tr < rows && n0 / 2 + 4 * cq < ow;
+        float dp[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (EP == Epilogue::kGluGradF32) {
+          if (ok) {
+            const float4 w = *reinterpret_cast<const float4*>(static_cast<const float*>(p.affine.grad) + at);
+            dp[0] = w.x; dp[1] = w.y; dp[2] = w.z; dp[3] = w.w;
+          }
+        } else if (ok) {
+          const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.affine.grad) + at);
+          dp[0] = bf16_lo(w.x); dp[1] = bf16_hi(w.x); dp[2] = bf16_lo(w.y); dp[3] = bf16_hi(w.y);
+        }
+        const int cg = (cq / 4) * 32 + 4 * (cq % 4);  // gate columns; the up columns follow 16 later
+        const v4i tg = total(lr, cg), tu = total(lr, cg + 16);
+        const float sg = as * ws, su = as * ws_u;
+        float dg[4], du[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          glu_grad(static_cast<float>(tg[r] - rs) * sg, static_cast<float>(tu[r] - rs) * su, dp[r], dg[r], du[r]);
+        if (ok) {
+          uint16_t* dst = static_cast<uint16_t*>(p.out) + (m0 + tr) * N + n0 / 2 + 4 * cq;
+          *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]));
+          *reinterpret_cast<uint2*>(dst + ow) = make_uint2(pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]));
+        }
+        continue;
+      } else if constexpr (EP == Epilogue::kGluF32) {
         const int cg = (cq / 4) * 32 + 4 * (cq % 4);  // gate columns; the up columns follow 16 later
         const v4i tg = total(lr, cg), tu = total(lr, cg + 16);
         const float sg = as * ws, su = as * ws_u;
@@ -332,7 +360,7 @@ hipError_t dispatch_fn(const ContractArgs& a, int fn, bool tiled, hipStream_t st
   if (a.N % 4 != 0) return hipErrorInvalidValue;
   switch (fn) {
     case 1:
-      if constexpr (EP != Epilogue::kGluF32) return dispatch_d<FM, 1, 1, true, EP>(a, tiled, stream);
+      if constexpr (!is_glu(EP)) return dispatch_d<FM, 1, 1, true, EP>(a, tiled, stream);
       return hipErrorInvalidValue;
     case 2: return dispatch_d<FM, 1, 2, true, EP>(a, tiled, stream);
     case 4: return dispatch_d<FM, 1, 4, true, EP>(a, tiled, stream);
@@ -362,5 +390,6 @@ hipError_t launch_skinny_dequant(const ContractArgs& a, int fm, int fn, bool til
 hipError_t launch_skinny_raw(const ContractArgs& a, int fm, int fn, bool tiled, hipStream_t stream);
 hipError_t launch_skinny_glu(const ContractArgs& a, int fm, int fn, bool tiled, hipStream_t stream);
 hipError_t launch_skinny_affine(const ContractArgs& a, int fm, int fn, bool tiled, hipStream_t stream);
+hipError_t launch_skinny_glu_grad(const ContractArgs& a, int fm, int fn, bool tiled, hipStream_t stream);
 
 }  // namespace mmf

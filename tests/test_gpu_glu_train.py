@@ -64,22 +64,28 @@ def guarded(M, N, dtype):
     return whole, whole[1:M + 1]
 
 
-def check_gate(mmf, M, K, L, dt, seed=0):
-    log(f"[glu_gate_bwd] M={M} K={K} L={L} dp={dt}")
+def check_gate(mmf, M, K, L, dt, path, seed=0):
+    log(f"[glu_gate_bwd] M={M} K={K} L={L} dp={dt} path={path}")
     v = inputs(mmf, seed + M + K + L, M, K, L, dt)
     Wg, sg = mmf.ternarize(v["W"][:L].contiguous())
     Wu, su = mmf.ternarize(v["W"][L:].contiguous() * 3.0)  # another scale
     ws = torch.cat([sg, su])
     whole, dgu = guarded(M, 2 * L, BF)
-    mmf.mmf_glu_gate_bwd(v["q"], v["a"], v["rs"], mmf.glu_pack(Wg, Wu), ws, v["dp"], dgu)
+    prev = mmf.mmf_set_path(path)
+    try:
+        mmf.mmf_glu_gate_bwd(v["q"], v["a"], v["rs"], mmf.glu_pack(Wg, Wu), ws, v["dp"], dgu)
+    finally:
+        mmf.mmf_set_path(prev)
     torch.cuda.synchronize()
     want, tol = gate64(v["q"], v["a"], unpack(Wg, L), unpack(Wu, L), ws, v["dp"])
     err = (dgu.double() - want).abs()
     assert (err <= tol).all(), float((err / tol).max())
     assert (whole[0] == 33).all() and (whole[-1] == 33).all()
+    return dgu
 
 
-# M, K, L and the tile that the planner takes for them
+# M, K, L and the tile that the planner takes for them on the tiled kernel;
+# fewer rows take the K-split kernel on the automatic path
 SIZES = [(1, 16, 16, "64x256"), (5, 48, 32, "64x256"), (37, 272, 304, "64x256"), (357, 1040, 2832, "64x256"),
          (1000, 336, 3008, "64x512"), (1100, 528, 4000, "128x512"), (3000, 400, 4112, "128x256_paired"),
          (129, 4112, 48, "64x256")]
@@ -90,7 +96,19 @@ SIZES = [(1, 16, 16, "64x256"), (5, 48, 32, "64x256"), (37, 272, 304, "64x256"),
 @pytest.mark.parametrize("M,K,L,tile", SIZES)
 def test_gate_gradients(mmf, M, K, L, tile, dt):
     assert mmf.mmf_prefill_tile_plan(M, K, 2 * L, mmf.MMF_EPILOGUE_GLU) == tile
-    check_gate(mmf, M, K, L, dt)
+    tiled = check_gate(mmf, M, K, L, dt, mmf.MMF_PATH_GEMM)
+    assert torch.equal(check_gate(mmf, M, K, L, dt, mmf.MMF_PATH_AUTO), tiled)
+
+
+# every row and column block count of the K-split kernel's tiles, K of less
+# than one step per wave to more than two
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,K,L", [(1, 2048, 5632), (16, 64, 2048), (17, 2048, 48), (33, 1040, 2832), (48, 528, 16),
+                                   (64, 2048, 5632), (100, 2064, 1040), (128, 4112, 3008), (300, 272, 5632)])
+def test_gate_gradients_of_few_rows(mmf, M, K, L, dt):
+    few = check_gate(mmf, M, K, L, dt, mmf.MMF_PATH_AUTO)
+    assert torch.equal(check_gate(mmf, M, K, L, dt, mmf.MMF_PATH_GEMM), few)
 
 
 @pytest.mark.gpu

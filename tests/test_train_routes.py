@@ -2,7 +2,7 @@
 tests/record.py records the launches of the built library)."""
 import pytest
 
-from record import call, kernels, record
+from record import GEMM, call, kernels, record
 
 A = 0x100000000  # made-up 256-byte aligned device address, never dereferenced
 BIG = 1 << 60
@@ -63,12 +63,25 @@ def test_recurrence_at_its_limits_launches():
 
 
 def test_glu_backward_joins_its_stages():
-    M, K, L = 300, 2048, 5632
+    M, K, L = 1000, 2048, 5632
     (r,) = record([call("mmf_glu_bwd", A, 1, A, 0, A, A, A, A, A, A, A, A, A, A, M, K, L, A, BIG, None)])
     names = kernels(r)
     assert r["status"] == 0 and names[:2] == ["glu_pack_kernel", "gemm_kernel"]
     (b,) = record([call("mmf_bitlinear_bwd", A, A, 0, A, A, A, A, A, A, A, A, None, A, M, K, 2 * L, A, BIG, None)])
     assert names[2:] == kernels(b)
+
+
+def test_gate_gradients_of_few_rows_split_k():
+    """On the kernels that the forward's contraction takes."""
+    for M, K, L in ((1, 2048, 5632), (16, 64, 2048), (17, 2048, 48), (64, 2048, 5632), (300, 2048, 5632),
+                    (1000, 2048, 5632), (300, 512, 512)):
+        for dp in (0, 1):
+            fwd, bwd, tiled = record([
+                call("mmf_ternary_gemm_glu", A, A, A, A, A, A, M, K, L, None),
+                call("mmf_glu_gate_bwd", A, A, A, A, A, A, dp, A, M, K, L, None),
+                call("mmf_glu_gate_bwd", A, A, A, A, A, A, dp, A, M, K, L, None, path=GEMM)])
+            assert kernels(fwd) == kernels(bwd) and bwd["status"] == 0 and kernels(tiled) == ["gemm_kernel"]
+            assert fwd["launches"][0]["grid"] == bwd["launches"][0]["grid"]
 
 
 def test_failing_allocations_are_reported():
