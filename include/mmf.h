@@ -537,8 +537,9 @@ int mmf_glu_bwd(const void *dp, int dp_is_f32, const void *x, int x_is_f32, cons
  * `grads`, `outs`, `is_f32` and `counts` are HOST arrays of n entries, read
  * before the call returns: device addresses of the gradients (16-byte
  * aligned; any address where the count is 0), where the scaled ones go
- * (outs[i] may be grads[i]; no other overlap), 0 for bf16 or 1 for float32, and
- * numbers of elements (any from 0 to 2^36, MMF_ERR_SHAPE).  norm [1] float32
+ * (outs[i] may be grads[i]; no other overlap, and none of two outputs), 0 for
+ * bf16 or 1 for float32, and numbers of elements (any from 0 to 2^36,
+ * MMF_ERR_SHAPE).  norm [1] float32
  * is a device array: between the two calls the norms of other shards can be
  * joined in it.  A norm of NaN makes every output NaN, an infinite one
  * scales by 0.  max_norm must be a number of at least 0 (MMF_ERR_ARG).  The sums are added in a

@@ -805,7 +805,8 @@ def mmf_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor | None = No
 
 def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=None) -> None:
     """outs[i] = grads[i] * min(max_norm / (norm + 1e-6), 1); outs None: in
-    place.  outs[i] has the type and the number of elements of grads[i]."""
+    place.  outs[i] has the type and the number of elements of grads[i]; no
+    two of them may overlap."""
     here = _here()
     _need_here(norm, "norm", torch.float32, (1,), here)
     ptrs, kinds, counts, types = _grad_set(grads, here)
@@ -815,6 +816,10 @@ def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=
         if otypes != types or list(map(_T.numel, outs)) != counts.tolist():
             raise ValueError("outs must have the types and numbers of elements of grads")
         dst = array.array("Q", optrs)
+    if len(set(dst)) != len(dst):  # empty tensors may share an address
+        full = [p for p, c in zip(dst, counts) if c]
+        if len(set(full)) != len(full):
+            raise ValueError("a tensor to write is in the list twice")
     _check(_lib.mmf_grad_clip(_at(ptrs), _at(kinds), _at(counts), len(ptrs), _ptr(norm), max_norm, _at(dst),
                               _stream_here(stream, here)))
 

@@ -32,6 +32,14 @@
 // forget gates from the chunk's start to t, the gradient that leaves at the
 // chunk's start is P_end G + sum_t P_t e_t (G the gradient entering at its
 // end), summed in the forward direction together with h.
+//
+// Bound by HBM: 16 bytes per token and channel forward, 22 backward (fp32 do).
+// One sequence of 16384 tokens x 2048: forward 103 us (5.2 TB/s), backward 148
+// us (5.0 TB/s); as two sweeps (the chunks' maps first, z read again for the
+// values) 155 and 300 us.  What waiting for other chunks costs of that: 5 and
+// 10 % (measured with the waits left out).  The backward takes 128 registers
+// of four waves per SIMD; three waves with 164 measured 9 % slower for both
+// directions together, as did 4 tokens per half wave with five (11 %).
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "row_vec.h"

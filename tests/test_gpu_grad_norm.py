@@ -211,6 +211,24 @@ def test_refusals(mmf):
 
 
 @pytest.mark.gpu
+def test_a_tensor_in_the_list_twice(mmf):
+    """It counts twice in the norm, and is refused where it would be written
+    twice; empty tensors may share an address."""
+    g, e = torch.ones(100, device=dev()), torch.empty(0, device=dev())
+    norm = torch.zeros(1, device=dev())
+    mmf.mmf_grad_norm([g, e, g, e], norm)
+    assert abs(float(norm) - 200 ** 0.5) <= 2 * U * 200 ** 0.5
+    with pytest.raises(ValueError, match="twice"):
+        mmf.mmf_grad_clip([g, e, g], norm, 1.0)
+    o = torch.empty_like(g)
+    with pytest.raises(ValueError, match="twice"):
+        mmf.mmf_grad_clip([g, g], norm, 1.0, [o, o])
+    p = torch.empty_like(g)
+    mmf.mmf_grad_clip([g, e, g, e], norm, 1.0, [o, e, p, e])
+    assert torch.equal(o, p) and float(o[0]) == float(factor(float(norm), 1.0))
+
+
+@pytest.mark.gpu
 def test_binding_refuses(mmf):
     g = torch.zeros((4, 8), device=dev())
     norm = torch.zeros(1, device=dev())
