@@ -413,9 +413,10 @@ int mmf_mlgru_fwd(const void *x, int x_is_f32, const float *gamma, const uint32_
  *   dz_g = do s(h)
  *   dh0 = f_1 dh_1,  dlb = sum over all tokens of dh (h_{t-1} - c) (1 - s(zf))
  * in fp32, dz [B*T][3d] rounded once to bf16 (the dO of mmf_bitlinear_bwd);
- * dh0 [B][d] (NULL: not stored), dlb [d] (NULL: not computed; summed in fp64,
- * in a fixed order) float32.  z, lb and states as the forward had and left
- * them.  Inside both, the tokens are cut into chunks whose maps are joined.
+ * dh0 [B][d] (NULL: not stored; may be the same array as dh_last), dlb [d]
+ * (NULL: not computed; summed in fp64, in a fixed order) float32.  z, lb and
+ * states as the forward had and left them.  No other overlap is allowed in
+ * either.  Inside both, the tokens are cut into chunks whose maps are joined.
  * d above 2^20 or more than 2^22 workgroups (B ceil(T/128) ceil(d/64)) return MMF_ERR_SHAPE;
  * B == 0 or T == 0 is a no-op.  Workspace as above; the backward's also
  * serves the forward.

@@ -354,6 +354,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     m.by = fmaf(m.ay, zg[u].y, m.by);
   }
   back[p.sub][p.lane] = m;
+  asm volatile("" : "+v"(G.x), "+v"(G.y) : : "memory");  // dh_last is read by here, as h0 above: it may be dh0
   __syncthreads();
   Map2 whole = kSame;
   if constexpr (MANY) {

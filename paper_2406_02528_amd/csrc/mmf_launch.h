@@ -224,7 +224,7 @@ int64_t mlgru_train_blocks(int64_t B, int64_t T, int64_t d);
 hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_last, float* states, uint64_t* words,
                                    uint32_t* tickets, hipStream_t stream);
 // Its backward (h0 of `p` is not read): dz bf16 [B*T][3d], dh0 [B][d]
-// (nullptr: not stored) and the partial sums of lb's gradient
+// (nullptr: not stored; may be dh_last) and the partial sums of lb's gradient
 // [B nchunk][d] (nullptr: not computed) from the gradient of o' and of the
 // last state (nullptr: 0).  words, tickets as above.
 hipError_t launch_mlgru_scan_bwd(const MlgruTrainArgs& p, const float* states, const void* dout, bool dout_is_f32,

@@ -103,13 +103,13 @@ def guarded(rows, cols, dtype):
     return whole, whole[1:rows + 1]
 
 
-def run(mmf, v, B, T, h_last_is_h0=False):
+def run(mmf, v, B, T, h_last_is_h0=False, dh0_is_dh_last=False):
     d = v["z"].shape[1] // 3
     t = {k: None if x is None else x.to(dev()) for k, x in v.items()}
     wo, o = guarded(B * T, d, F32)
     wz, dz = guarded(B * T, 3 * d, BF)
     h = t["h0"] if h_last_is_h0 else torch.full((B, d), float("nan"), device=dev())
-    dh0 = torch.full((B, d), float("nan"), device=dev())
+    dh0 = t["dh"] if dh0_is_dh_last else torch.full((B, d), float("nan"), device=dev())
     dlb = torch.full((d,), float("nan"), device=dev())
     n, m = mmf.mmf_mlgru_train_states_bytes(B, T, d), mmf.mmf_mlgru_scan_bwd_workspace_bytes(B, T, d)
     assert m >= mmf.mmf_mlgru_train_scan_workspace_bytes(B, T, d)
@@ -161,6 +161,13 @@ def test_optional_inputs(mmf, B, T, d):
 @pytest.mark.parametrize("T", [129, 1500, 2500])
 def test_state_in_place_over_several_chunks(mmf, T):
     check(mmf, make(6, 2, T, 80, F32), 2, T, h_last_is_h0=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 128, 129, 1500, 2500])
+def test_gradient_of_the_state_in_place(mmf, T):
+    """As for sequences that are passed segment by segment, the last first."""
+    check(mmf, make(7, 2, T, 80, F32), 2, T, dh0_is_dh_last=True)
 
 
 @pytest.mark.gpu
