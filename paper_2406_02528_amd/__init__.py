@@ -647,8 +647,8 @@ def mmf_mlgru_scan_bwd(z: torch.Tensor, B: int, T: int, lb: torch.Tensor | None,
                        dh0: torch.Tensor | None, dlb: torch.Tensor | None,
                        workspace: torch.Tensor | None = None, stream=None) -> None:
     """Backward of mmf_mlgru_train_scan: dz bf16 [B*T][3d] (the dO of
-    mmf_bitlinear_bwd), dh0 f32 [B][d] (or None) and dlb f32 [d] (or None) from
-    do_prime bf16/f32 [B*T][d], dh_last f32 [B][d] (or None) and the forward's
+    mmf_bitlinear_bwd), dh0 f32 [B][d] (or None; may be dh_last) and dlb f32
+    [d] (or None) from do_prime bf16/f32 [B*T][d], dh_last f32 [B][d] (or None) and the forward's
     z, lb and states."""
     here = _here()
     d = z.shape[1] // 3
@@ -776,8 +776,16 @@ def _grad_ptrs(tensors, name, here):
     raise ValueError(f"{name} must be tensors on the current device")
 
 
+def _listed(tensors, name):
+    """The tensors as a list or tuple (a generator could be passed over only once)."""
+    if isinstance(tensors, torch.Tensor):
+        raise TypeError(f"{name} must be a list of tensors")
+    return tensors if isinstance(tensors, (list, tuple)) else list(tensors)
+
+
 def _grad_set(tensors, here):
     """What the C calls take: arrays of addresses, kinds and sizes, and the types."""
+    tensors = _listed(tensors, "grads")
     ptrs, types = _grad_ptrs(tensors, "grads", here)
     return (array.array("Q", ptrs), array.array("i", [k is torch.float32 for k in types]),
             array.array("q", map(_T.numel, tensors)), types)
@@ -812,6 +820,7 @@ def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=
     ptrs, kinds, counts, types = _grad_set(grads, here)
     dst = ptrs
     if outs is not None:
+        outs = _listed(outs, "outs")
         optrs, otypes = _grad_ptrs(outs, "outs", here)
         if otypes != types or list(map(_T.numel, outs)) != counts.tolist():
             raise ValueError("outs must have the types and numbers of elements of grads")

@@ -229,6 +229,24 @@ def test_a_tensor_in_the_list_twice(mmf):
 
 
 @pytest.mark.gpu
+def test_a_generator_of_tensors(mmf):
+    gs = [torch.full((30,), 2.0, device=dev()), torch.full((7,), 1.0, device=dev()).bfloat16()]
+    outs = [torch.empty_like(g) for g in gs]
+    norm, want = torch.zeros(1, device=dev()), (30 * 4 + 7) ** 0.5
+    mmf.mmf_grad_norm((g for g in gs), norm)
+    assert abs(float(norm) - want) <= 2 * U * want
+    mmf.mmf_grad_clip((g for g in gs), norm, 1.0, (o for o in outs))
+    mmf.mmf_grad_clip(dict(enumerate(gs)).values(), norm, 1.0)
+    c = factor(float(norm), 1.0)
+    assert float(outs[0][29]) == float(gs[0][29]) == float(torch.tensor(2.0) * c)
+    assert float(outs[1][6]) == float(gs[1][6]) == float((torch.tensor(1.0) * c).bfloat16())
+    for one in (lambda: mmf.mmf_grad_norm(gs[0], norm), lambda: mmf.mmf_grad_clip(gs[0], norm, 1.0),
+                lambda: mmf.mmf_grad_clip([gs[0]], norm, 1.0, outs[0])):
+        with pytest.raises(TypeError, match="list"):
+            one()
+
+
+@pytest.mark.gpu
 def test_binding_refuses(mmf):
     g = torch.zeros((4, 8), device=dev())
     norm = torch.zeros(1, device=dev())
