@@ -10,7 +10,10 @@ PyTorch is used for device memory and streams only.
 
 Also the GLU channel mixer's gated up-projection, the MLGRU token mixer
 (input projections with gate activations, the recurrence, the whole mixer),
-and the training forward and backward of the layer.
+the training forward and backward of the layer, and what a block's training
+step needs around it: the residual addition fused into the quantiser, the GLU
+mixer's and the recurrence's training forms, and the global gradient norm with
+clipping.
 
 Functions carry the names of the C entry points.  There is no fallback: if
 the library is not built, importing this package raises ``ImportError``.
