@@ -766,9 +766,9 @@ def _grad_ptrs(tensors, name, here):
     """Addresses of a list of contiguous bf16 or f32 tensors on the current device, and their types."""
     try:
         kinds = list(map(_dtype_of, tensors))
-        if (all(map(_T.is_contiguous, tensors)) and not set(map(_T.get_device, tensors)) - {here}
-                and not set(kinds) - {torch.float32, torch.bfloat16}):
-            return list(map(_T.data_ptr, tensors)), kinds
+        if (all(map(_T.is_contiguous, tensors)) and set(map(_T.get_device, tensors)) <= {here}
+                and kinds.count(torch.float32) + kinds.count(torch.bfloat16) == len(kinds)):
+            return array.array("Q", list(map(_T.data_ptr, tensors))), kinds
     except (AttributeError, TypeError, RuntimeError):
         pass
     for i, t in enumerate(tensors):
@@ -790,8 +790,12 @@ def _grad_set(tensors, here):
     """What the C calls take: arrays of addresses, kinds and sizes, and the types."""
     tensors = _listed(tensors, "grads")
     ptrs, types = _grad_ptrs(tensors, "grads", here)
-    return (array.array("Q", ptrs), array.array("i", [k is torch.float32 for k in types]),
-            array.array("q", map(_T.numel, tensors)), types)
+    n, n32 = len(types), types.count(torch.float32)
+    if n32 == n or n32 == 0:
+        is_f32 = array.array("i", (n32 > 0,)) * n
+    else:
+        is_f32 = array.array("i", [k is torch.float32 for k in types])
+    return ptrs, is_f32, array.array("q", list(map(_T.numel, tensors))), types
 
 
 def _at(a: array.array) -> int:
@@ -824,10 +828,9 @@ def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=
     dst = ptrs
     if outs is not None:
         outs = _listed(outs, "outs")
-        optrs, otypes = _grad_ptrs(outs, "outs", here)
-        if otypes != types or list(map(_T.numel, outs)) != counts.tolist():
+        dst, otypes = _grad_ptrs(outs, "outs", here)
+        if otypes != types or array.array("q", list(map(_T.numel, outs))) != counts:
             raise ValueError("outs must have the types and numbers of elements of grads")
-        dst = array.array("Q", optrs)
     if len(set(dst)) != len(dst):  # empty tensors may share an address
         full = [p for p, c in zip(dst, counts) if c]
         if len(set(full)) != len(full):
