@@ -272,6 +272,75 @@ def test_on_another_stream_and_captured(mmf, T):
         assert same()
 
 
+class Held:
+    """Device arrays of a problem and its two calls; `ws` may be another's."""
+
+    def __init__(self, mmf, seed, B, T, d, ws=None):
+        self.v = make(seed, B, T, d, F32)
+        self.t = {k: x.to(dev()) for k, x in self.v.items()}
+        self.size = B, T
+        self.out = {"o": torch.zeros((B * T, d), device=dev()), "h": torch.zeros((B, d), device=dev()),
+                    "dz": torch.zeros((B * T, 3 * d), dtype=BF, device=dev()),
+                    "dh0": torch.zeros((B, d), device=dev()), "dlb": torch.zeros(d, device=dev())}
+        self.states = torch.empty(mmf.mmf_mlgru_train_states_bytes(B, T, d), dtype=torch.uint8, device=dev())
+        n = mmf.mmf_mlgru_scan_bwd_workspace_bytes(B, T, d)
+        self.ws = torch.empty(n, dtype=torch.uint8, device=dev()) if ws is None else ws
+        assert self.ws.numel() >= n
+        self.want = run(mmf, self.v, B, T)
+
+    def step(self, mmf, stream=None):
+        t, w, (B, T) = self.t, self.out, self.size
+        mmf.mmf_mlgru_train_scan(t["z"], B, T, t["lb"], t["h0"], w["o"], w["h"], self.states, self.ws, stream)
+        mmf.mmf_mlgru_scan_bwd(t["z"], B, T, t["lb"], self.states, t["do"], t["dh"], w["dz"], w["dh0"], w["dlb"],
+                               self.ws, stream)
+
+    def same(self):
+        return all(torch.equal(x, self.want[k]) for k, x in self.out.items())
+
+    def clear(self):
+        for x in self.out.values():
+            x.zero_()
+
+
+@pytest.mark.gpu
+def test_two_graphs_share_a_workspace(mmf):
+    """Replayed in turn on one stream, of different sizes."""
+    a = Held(mmf, 11, 2, 2500, 144)
+    b = Held(mmf, 12, 3, 300, 80, a.ws)
+    graphs = []
+    for x in (a, b):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            x.step(mmf)
+    for _ in range(3):
+        for x in (a, b):
+            x.clear()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert a.same() and b.same()
+        b.clear()
+        b.step(mmf)
+        torch.cuda.synchronize()
+        assert b.same()
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once(mmf):
+    """Calls side by side, each with more chunks than fit the chip at once."""
+    both = [Held(mmf, 13, 1, 6000, 2048), Held(mmf, 14, 2, 4000, 1040)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x in both:
+            x.clear()
+        torch.cuda.synchronize()
+        for x, s in zip(both, streams):
+            x.step(mmf, s)
+        torch.cuda.synchronize()
+        assert both[0].same() and both[1].same()
+
+
 def test_equations_against_differences():
     """The gradients are those of sum(do o') + sum(dh_last h_T)."""
     B, T, d = 2, 5, 2
