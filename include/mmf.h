@@ -474,7 +474,7 @@ int mmf_bitlinear_train_fwd(const void *x, int x_is_f32, const float *gamma, con
  * and forms Yq while staging them.  s, db and dgamma are summed in fp64;
  * when the dW output has few tiles its contraction over tokens is split into
  * parts added in fp64.  Shapes whose dO rows, re-packed codes or dW exceed
- * 32-bit offsets ((N + 7) / 8 * 16 * 128 bytes of dO per 128 rows, K * 4 *
+ * 32-bit offsets ((N + 7) / 8 * 16 * 129 bytes for 129 rows of dO, K * 4 *
  * ceil(N / 16) bytes of codes, N * K * 4 bytes of dW, each below 2^31)
  * return MMF_ERR_SHAPE.  M == 0 or N == 0 is a no-op.  Workspace as above.
  */
