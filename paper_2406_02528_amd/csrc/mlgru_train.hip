@@ -293,7 +293,7 @@ struct BwdArgs {
 template <typename DT, bool MANY, bool NT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void mlgru_train_bwd_kernel(const BwdArgs a) {
   __shared__ Map2 maps[kSubs][kLanes], back[kSubs][kLanes];
-  __shared__ V2 s_dlb[kSubs][kLanes];
+  __shared__ double2 s_dlb[kSubs][kLanes];
   const int64_t d = a.d;
   const Place p = place<MANY>(a.T, d, a.B, a.nchunk, true, a.tickets);
   const Rows<NT> z(a.z, p, 3 * d, 4), dz(a.dz, p, 3 * d, 2);
@@ -370,17 +370,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
   }
 #pragma unroll 2
   for (int i = kSubs - 1; i > p.sub; --i) G = back[i][p.lane](G);
-  float dlx = 0.0f, dly = 0.0f;
+  double dlx = 0.0, dly = 0.0;
 #pragma unroll
   for (int u = kTok - 1; u >= 0; --u) {
     const bool in = p.u0 + u < p.rows;
     // one channel: its gradients, and G carried to the token before
     auto one = [in, &forget](float sf, float c, float q, float e, float hp, float lb, float& G, float& df, float& dc,
-                             float& dl) {
+                             double& dl) {
       const float f = forget(sf, lb, in), dh = G + e, w = dh * (hp - c), k = w * (1.0f - sf);
       df = k * ((1.0f - lb) * sf);
       dc = dh * (1.0f - f) * q;
-      dl += in ? k : 0.0f;
+      dl += static_cast<double>(in ? k : 0.0f);
       G = f * dh;
     };
     float dfx, dfy, dcx, dcy;
@@ -391,15 +391,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     dz.store_bf16(u, dgate, dcx, dcy);
   }
   if (p.k == 0 && p.sub == 0 && p.col && a.dh0 != nullptr) st2(a.dh0 + p.b * d + p.c, G);
-  if (a.dlb_part != nullptr) {  // eight tokens each in fp32, from there in fp64
-    s_dlb[p.sub][p.lane] = {dlx, dly};
+  if (a.dlb_part != nullptr) {
+    s_dlb[p.sub][p.lane] = make_double2(dlx, dly);
     __syncthreads();
     if (p.sub == 0 && p.col) {
       double x = 0.0, y = 0.0;
 #pragma unroll
       for (int i = 0; i < kSubs; ++i) {
-        x += static_cast<double>(s_dlb[i][p.lane].x);
-        y += static_cast<double>(s_dlb[i][p.lane].y);
+        x += s_dlb[i][p.lane].x;
+        y += s_dlb[i][p.lane].y;
       }
       *reinterpret_cast<double2*>(a.dlb_part + at) = make_double2(x, y);
     }
