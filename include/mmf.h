@@ -542,9 +542,11 @@ int mmf_glu_bwd(const void *dp, int dp_is_f32, const void *x, int x_is_f32, cons
  * bf16 or 1 for float32, and numbers of elements (any from 0 to 2^36,
  * MMF_ERR_SHAPE).  norm [1] float32
  * is a device array: between the two calls the norms of other shards can be
- * joined in it.  A norm of NaN makes every output NaN, an infinite one
- * scales by 0.  max_norm must be a number of at least 0 (MMF_ERR_ARG).  The sums are added in a
- * fixed order.  n == 0: norm = 0.  Workspace as above.
+ * joined in it.  max_norm must be a number of at least 0 (MMF_ERR_ARG); an
+ * infinite one sets no limit (the factor is 1).  A norm of NaN makes every
+ * output NaN; an infinite norm under a finite max_norm scales by 0, which
+ * leaves NaN where a gradient is infinite.  The sums are added in a fixed
+ * order.  n == 0: norm = 0.  Workspace as above.
  */
 size_t mmf_grad_norm_workspace_bytes(const int64_t *counts, int64_t n);
 int mmf_grad_norm(const void *const *grads, const int *is_f32, const int64_t *counts, int64_t n,

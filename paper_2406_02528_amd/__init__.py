@@ -820,8 +820,8 @@ def mmf_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor | None = No
 
 def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=None) -> None:
     """outs[i] = grads[i] * min(max_norm / (norm + 1e-6), 1); outs None: in
-    place.  outs[i] has the type and the number of elements of grads[i]; no
-    two of them may overlap."""
+    place; max_norm infinite: no limit.  outs[i] has the type and the number of
+    elements of grads[i]; no two of them may overlap."""
     here = _here()
     _need_here(norm, "norm", torch.float32, (1,), here)
     ptrs, kinds, counts, types = _grad_set(grads, here)

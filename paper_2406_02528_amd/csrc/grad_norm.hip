@@ -1,6 +1,7 @@
 // The norm over all elements of a set of gradients, and the set scaled to it:
 //   norm = sqrt(sum over the arrays of sum g^2)   (squares and sums in fp64)
-//   c = max_norm / (norm + 1e-6),  out = g min(c, 1)   (fp32)
+//   c = max_norm / (norm + 1e-6),  out = g min(c, 1)   (fp32; c = 1 where
+//   max_norm is infinite and norm is a number)
 //
 // A launch covers up to kSet arrays, whose addresses and sizes travel in its
 // arguments; their elements are cut into pieces of kPiece (the last of an
@@ -160,6 +161,7 @@ __global__ __launch_bounds__(kBlock) void grad_scale_kernel(const Set s, const f
                                                             float max_norm) {
   float c = max_norm / (norm[0] + 1e-6f);
   if (c > 1.0f) c = 1.0f;  // a NaN stays
+  if (max_norm == __builtin_inff() && norm[0] == norm[0]) c = 1.0f;  // no limit, also for an infinite norm
   const Piece p = piece_of(s, blockIdx.x);
   if (c == 1.0f && s.src[p.i] == s.dst[p.i]) return;  // nothing changes
   if (p.f32) scale(static_cast<const float*>(s.src[p.i]), static_cast<float*>(s.dst[p.i]), p.begin, p.end, c);
