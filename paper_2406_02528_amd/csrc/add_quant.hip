@@ -92,6 +92,10 @@ __global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const 
 #pragma unroll
       for (int i = 0; i < VPL; ++i) gv[i].load(grsrc, rl + W * kWave * i);
       __builtin_amdgcn_sched_barrier(0);  // all loads before the first wait
+      if (branch == nullptr) {  // uniform
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) bv[i].set_negative_zero();
+      }
       double ss = 0.0;
       float f[VPL][E];
 #pragma unroll
@@ -133,6 +137,7 @@ __global__ __launch_bounds__(kWave*(W > 4 ? W : 4)) void add_quant_kernel(const 
         RowVec<BT, E> bv;
         xv.load(xrsrc, v);
         bv.load(brsrc, v);
+        if (branch == nullptr) bv.set_negative_zero();
         float f[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) f[e] = xv.get(e) + bv.get(e);

@@ -85,6 +85,11 @@ struct RowVec {
       else w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
     }
   }
+  // Values of -0, which x + v leaves any x as it is (+0 would turn -0 into +0).
+  __device__ __forceinline__ void set_negative_zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+  }
   template <bool NT = false>
   __device__ __forceinline__ void store(T* row, int v) const {
     typedef unsigned int vec __attribute__((ext_vector_type(kLoad)));
