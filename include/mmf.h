@@ -150,9 +150,10 @@ int mmf_add_act_quant(const void *x, int x_is_f32, const void *branch, int branc
 
 /*
  * Its backward (the straight-through estimator passes the gradient through
- * the quantiser unchanged), for activations y = (s r) gamma that other
- * operators than the layer's own backward consume: from the gradient dY of y
- * and the gradient ds_out that reaches s through the residual stream,
+ * the quantiser unchanged), for activations y = (s r) gamma that the program
+ * itself consumes, such as the final norm's in front of an un-embedding (the
+ * backwards of the layers contain this step and give dx): from the gradient dY
+ * of y and the gradient ds_out that reaches s through the residual stream,
  *   ds = r g - (r^3 t / K) s + ds_out,  g = gamma (.) dY,  t = sum_k g_k s_k
  *   dgamma = sum over tokens of dY (.) s r
  * ds is the gradient of x and of branch alike.  dY [M][K] bf16 bits or float32
