@@ -435,12 +435,15 @@ hipError_t launch_mlgru_train_scan(const MlgruTrainArgs& p, float* o, float* h_l
   const int64_t nchunk = mlgru_train_chunks(p.T);
   const FwdArgs a{p.z, p.lb, p.h0, words, tickets, states, o, h_last, p.B, p.T, p.d, nchunk};
   const dim3 grid(static_cast<unsigned>(mlgru_train_blocks(p.B, p.T, p.d)));
+  const bool nt = p.B * p.T * p.d * 16 >= kLastLevelBytes;  // z and o'
   if (nchunk > 1) {
     if (const hipError_t e = clear(words, p.B * nchunk * p.d, tickets, stream); e != hipSuccess) return e;
-    if (p.B * p.T * p.d * 16 >= kLastLevelBytes)  // z and o'
+    if (nt)
       hipLaunchKernelGGL((mlgru_train_fwd_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
     else
       hipLaunchKernelGGL((mlgru_train_fwd_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
+  } else if (nt) {
+    hipLaunchKernelGGL((mlgru_train_fwd_kernel<false, true>), grid, dim3(kThreads), 0, stream, a);
   } else {
     hipLaunchKernelGGL((mlgru_train_fwd_kernel<false, false>), grid, dim3(kThreads), 0, stream, a);
   }
@@ -451,12 +454,17 @@ namespace {
 template <typename DT>
 hipError_t launch_bwd(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
   const dim3 grid(blocks), block(kThreads);
-  if (a.nchunk == 1)
+  const bool nt = a.B * a.T * a.d * static_cast<int64_t>(18 + sizeof(DT)) >= kLastLevelBytes;  // z, do and dz
+  if (a.nchunk > 1) {
+    if (nt)
+      hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, true>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, false>), grid, block, 0, stream, a);
+  } else if (nt) {
+    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, false, true>), grid, block, 0, stream, a);
+  } else {
     hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, false, false>), grid, block, 0, stream, a);
-  else if (a.B * a.T * a.d * static_cast<int64_t>(18 + sizeof(DT)) >= kLastLevelBytes)  // z, do and dz
-    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, true>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((mlgru_train_bwd_kernel<DT, true, false>), grid, block, 0, stream, a);
+  }
   return hipGetLastError();
 }
 }  // namespace
