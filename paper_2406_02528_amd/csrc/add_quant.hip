@@ -23,6 +23,7 @@ namespace mmf {
 namespace {
 
 constexpr int64_t kMaxBlocks = int64_t(1) << 20;  // rows past them: further passes of the row loop
+constexpr int kOneWaveK = kWave * 32;             // longest row of one wave
 
 // ---------------------------------------------------------------------------
 // forward
@@ -189,21 +190,28 @@ hipError_t launch_fwd_one(const FwdArgs& a, hipStream_t stream) {
   constexpr int kRows = kBlockWaves / W;
   const int64_t blocks = (a.M + kRows - 1) / kRows;
   const dim3 grid(static_cast<unsigned>(blocks < kMaxBlocks ? blocks : kMaxBlocks));
-  if (VPL > 0 && a.M * a.K * static_cast<int64_t>(2 * sizeof(XT) + sizeof(BT) + 1) >= kLastLevelBytes)
-    hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL, (VPL > 0)>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
+  // as streams: rows in registers, and not the few short ones that share four waves
+  constexpr bool kStream = VPL > 0 && !(W == 4 && W * kWave * VPL * E <= kOneWaveK);
+  if (kStream && a.M * a.K * static_cast<int64_t>(2 * sizeof(XT) + sizeof(BT) + 1) >= kLastLevelBytes)
+    hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL, kStream>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
   else
     hipLaunchKernelGGL((add_quant_kernel<XT, BT, E, W, VPL, false>), grid, dim3(kWave * kBlockWaves), 0, stream, a);
   return hipGetLastError();
 }
 
 // The smallest compiled number of vectors per lane that holds the row (loads
-// past the row's end return zeros but cost nearly a real load each).
+// past the row's end return zeros but cost nearly a real load each); 16 waves
+// have rows of more than 8192.
 template <typename XT, typename BT, int E, int W>
 hipError_t launch_fwd_w(const FwdArgs& a, hipStream_t stream) {
   const int vpl = (a.K / E + W * kWave - 1) / (W * kWave);
+  if constexpr (W < 16) {
+    if (vpl == 1) return launch_fwd_one<XT, BT, E, W, 1>(a, stream);
+  }
+  if constexpr (W < 16 || E == 8) {
+    if (vpl == 2) return launch_fwd_one<XT, BT, E, W, 2>(a, stream);
+  }
   switch (vpl) {
-    case 1: return launch_fwd_one<XT, BT, E, W, 1>(a, stream);
-    case 2: return launch_fwd_one<XT, BT, E, W, 2>(a, stream);
     case 3: return launch_fwd_one<XT, BT, E, W, 3>(a, stream);
     case 4: return launch_fwd_one<XT, BT, E, W, 4>(a, stream);
     default: break;
@@ -220,15 +228,24 @@ hipError_t launch_fwd_w(const FwdArgs& a, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
-// Waves per row: up to 32 values per lane stay in registers (K <= 32768);
-// with few rows, when most of the chip idles anyway, more waves share a row.
+// Waves per row: up to 32 values per lane (K <= 32768; what 16 waves hold in
+// their 128 registers spills by up to 12 of them).  Up to a row per compute
+// unit, four waves share a row of more than two vectors per lane, which one
+// wave would keep to itself (1 and 4 waves, us, bf16 stream and fp32 branch,
+// launches replayed back to back; fp32 streams alike):
+//   K = 1024: 1 row 2.82 / 2.58, 64 3.14 / 2.96, 256 3.73 / 3.37, 512 3.97 / 3.87, 2048 7.21 / 8.07
+//   K = 2048: 1 row 3.62 / 2.83, 64 3.98 / 3.21, 256 4.72 / 4.04, 512 5.08 / 4.82, 2048 10.1 / 10.4
+//   K = 528:  1 row 2.65 / 2.64, 64 2.96 / 3.04, 256 3.22 / 3.24, 512 3.57 / 3.67, 2048 5.79 / 7.24
+//   K = 1024, all bf16 (two vectors): 1 row 2.63 / 2.68, 64 2.93 / 3.04, 2048 6.57 / 8.00
+// 16 in place of 4 never gain (K = 5120: 1 row 3.55 / 4.13, 64 4.50 / 4.97;
+// K = 8192: 4.04 / 4.15 and 5.12 / 5.10).
 // bf16 streams with fp32 branches go four values at a time (8-byte and 16-byte
 // loads side by side), bf16 with bf16 eight.
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 256;
 template <typename XT, typename BT, int E>
 hipError_t launch_fwd(const FwdArgs& a, hipStream_t stream) {
-  int w = a.K <= kWave * 32 ? 1 : a.K <= 4 * kWave * 32 ? 4 : 16;
-  if (a.M <= kFewRows && w < 16 && a.K > w * kWave * 8) w *= 4;
+  int w = a.K <= kOneWaveK ? 1 : a.K <= 4 * kOneWaveK ? 4 : 16;
+  if (w == 1 && a.M <= kFewRows && a.K > 2 * kWave * E) w = 4;
   if (w == 1) return launch_fwd_w<XT, BT, E, 1>(a, stream);
   if (w == 4) return launch_fwd_w<XT, BT, E, 4>(a, stream);
   return launch_fwd_w<XT, BT, E, 16>(a, stream);
