@@ -435,9 +435,16 @@ hipError_t launch_bwd_w(const BwdArgs& a, unsigned blocks, hipStream_t stream) {
     else                                                                                                             \
       hipLaunchKernelGGL((add_quant_bwd_kernel<ST, DT, E, W, V, false>), dim3(blocks), dim3(kWave * W), 0, stream, a); \
   } while (0)
+  constexpr int kLeast = W == 1 ? 1 : W == 4 ? 2 : 3;  // of the rows that bwd_waves gives W waves
   switch (vpl) {
-    case 1: MMF_LAUNCH(1); break;
-    case 2: MMF_LAUNCH(2); break;
+    case 1:
+      if constexpr (kLeast <= 1) MMF_LAUNCH(1);
+      else return hipErrorInvalidValue;
+      break;
+    case 2:
+      if constexpr (kLeast <= 2) MMF_LAUNCH(2);
+      else return hipErrorInvalidValue;
+      break;
     case 3: MMF_LAUNCH(3); break;
     case 4: MMF_LAUNCH(4); break;
     default:

@@ -32,8 +32,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_rsrc(const T* row, int K, 
 // reads and writes them without leaving them there (nontemporal: nothing of
 // them would still be there for their next reader, and taking a line in pushes
 // another out, which goes to memory first if it was written).  Smaller ones
-// stay for their next reader.  Rows too long for registers, which are read
-// again in the call, always go through the caches.
+// stay for their next reader.  Rows too long for registers are read through
+// the caches always: the call reads them again.
 constexpr int64_t kLastLevelBytes = int64_t(256) << 20;
 constexpr int kNontemporal = 2;  // buffer cache policy: the nt bit
 
