@@ -115,6 +115,8 @@ int mmf_ternarize_weights(const float *W, int64_t N, int64_t K,
  *   q_k      = clamp(round_half_even(y_k * (127 / a)), -128, 127)
  *   a_scale  = a / 127,   q_rowsum = sum_k q_k.
  * x: [M][K] bf16 bits; gamma: [K] or NULL; q: [M][K] out; a_scale: [M] out.
+ * Activations must be finite: a row with a NaN or an infinity in it gives a
+ * finite a_scale and a q that mean nothing; the other rows are as without it.
  */
 int mmf_act_quant(const uint16_t *x, const float *gamma, int8_t *q,
                   float *a_scale, int64_t M, int64_t K, hipStream_t stream);
@@ -135,13 +137,18 @@ int mmf_act_quant_ex(const void *x, int x_is_f32, const float *gamma, int8_t *q,
  * token m:
  *   s = x + branch                  (fp32, stored in the type of x)
  *   r, q, a_scale, q_rowsum         as mmf_act_quant_ex of the stored s
- * the same bits as an addition followed by that call.  x and s [M][K] bf16
+ * the same bits as an addition followed by that call (r's fp64 sum may be
+ * taken in another order, which moves r's rounding to fp32, and with it an
+ * entry next to a midpoint, in about one row of 10^8).  x and s [M][K] bf16
  * bits or float32 (x_is_f32), branch [M][K] bf16 bits or float32
  * (branch_is_f32; NULL: no branch, s = x, and s may be NULL, not stored);
  * gamma [K] or NULL; q [M][K], a_scale [M], q_rowsum [M] (or NULL) out; rstd
  * [M] out (or NULL), r = 1/sqrt(mean s^2 + 1e-6), as the backwards take it.
  * s may be the same array as x (the stream updated in place); no other
- * overlap is allowed.
+ * overlap is allowed.  A row that holds a NaN or an infinity keeps it in s and
+ * shows it in rstd (NaN, or 0 where there are infinities alone), not in q and
+ * a_scale, which are as mmf_act_quant_ex leaves them: a program that looks for
+ * such rows reads s or rstd.  M == 0 is a no-op.
  */
 int mmf_add_act_quant(const void *x, int x_is_f32, const void *branch, int branch_is_f32,
                       const float *gamma, void *s, int8_t *q, float *a_scale,
@@ -162,7 +169,8 @@ int mmf_add_act_quant(const void *x, int x_is_f32, const void *branch, int branc
  * Outputs: ds [M][K] float32 (may be the same array as ds_out); ds_bf16
  * [M][K], ds rounded to bf16 as mmf_bitlinear_bwd takes the gradient of its
  * output (NULL: not stored); dgamma [K] float32 (NULL: not computed).  t and
- * dgamma are summed in fp64, in a fixed order.  M == 0 is a no-op.  Workspace
+ * dgamma are summed in fp64, in a fixed order.  M == 0 is a no-op, which leaves
+ * dgamma as it was.  Workspace
  * (needed for dgamma only; 256-byte aligned, MMF_ERR_WORKSPACE), or NULL: then
  * allocated stream-ordered on `stream` and freed there.
  */
@@ -419,8 +427,9 @@ int mmf_mlgru_fwd(const void *x, int x_is_f32, const float *gamma, const uint32_
  * states as the forward had and left them.  No other overlap is allowed in
  * either.  Inside both, the tokens are cut into chunks whose maps are joined.
  * d above 2^20 or more than 2^22 workgroups (B ceil(T/128) ceil(d/64)) return MMF_ERR_SHAPE;
- * B == 0 or T == 0 is a no-op.  Workspace as above; the backward's also
- * serves the forward.
+ * B == 0 or T == 0 is a no-op, which leaves every output, h_last, dh0 and dlb
+ * among them, as it was.  Workspace as above; the backward's also serves the
+ * forward.
  */
 size_t mmf_mlgru_train_states_bytes(int64_t B, int64_t T, int64_t d);
 size_t mmf_mlgru_train_scan_workspace_bytes(int64_t B, int64_t T, int64_t d);

@@ -39,3 +39,33 @@ def test_without_a_branch_the_stream_is_copied_bit_for_bit(mmf, M, K, xt, in_pla
                                         a.data_ptr(), None, None, M, K, torch.cuda.current_stream().cuda_stream)
         assert st == 0
         assert torch.equal(bits(s), bits(want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("K", [16, 512, 2048, 2064, 8208, 32784])
+def test_rows_that_are_not_finite(mmf, K, xt):
+    """A NaN or an infinity stays in s and shows in rstd; q and a_scale are
+    finite, those that mmf_act_quant_ex gives for s; other rows do not notice."""
+    M = 7
+    log(f"[add_quant] not finite M={M} K={K} x={xt}")
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.randn((M, K), generator=gen, device=dev()).to(xt)
+    b = torch.randn((M, K), generator=gen, device=dev())
+    gamma = torch.rand(K, generator=gen, device=dev()) + 0.5
+    clean = mmf.add_act_quant(x, b, gamma)
+    nan, inf = float("nan"), float("inf")
+    b[1, K // 2] = nan
+    b[3, 3], b[3, K - 1] = inf, -inf
+    b[5, 0], b[5, 9] = inf, nan
+    x[6, 2], b[6, 2] = inf, -inf  # their sum is a NaN
+    s, q, a, rs, r = mmf.add_act_quant(x, b, gamma)
+    assert s[1, K // 2].isnan() and s[6, 2].isnan() and s[5, 9].isnan()
+    assert s[3, 3] == inf and s[3, K - 1] == -inf and s[5, 0] == inf
+    assert r[1].isnan() and r[5].isnan() and r[6].isnan() and r[3] == 0
+    assert a.isfinite().all() and torch.equal(rs.long(), q.long().sum(1))
+    q2, a2, rs2 = torch.empty_like(q), torch.empty_like(a), torch.empty_like(rs)
+    mmf.mmf_act_quant_ex(s, gamma, q2, a2, rs2)
+    assert torch.equal(q, q2) and torch.equal(a, a2) and torch.equal(rs, rs2)
+    for i in (0, 2, 4):
+        assert all(torch.equal(u[i], v[i]) for u, v in zip((s, q, a, rs, r), clean))
