@@ -11,10 +11,11 @@
 //   dgamma = sum over rows of dY s r.
 //
 // Both are streams, bound by HBM.  Forward: 9 bytes per element with a bf16
-// stream and an fp32 branch; 16384 x 5120 in 116 us (6.5 TB/s; cached accesses
-// instead of streams 129 us), one row of 2048 in 2.7 us (the launch and three
+// stream and an fp32 branch; 16384 x 5120 in 123 us (6.1 TB/s; cached accesses
+// instead of streams 132), one row of 2048 in 2.6 us (the launch and three
 // reductions).  Backward: 16 bytes with bf16 s and fp32 gradients; 8192 x 2048
-// in 45 us (6.0 TB/s) and 4 us for the sums of dgamma's 256 partial rows.
+// in 47 us (5.7 TB/s) and 4.5 us for the sums of dgamma's 256 partial rows.
+// Medians of 61 calls one behind the other; the fastest took 114 and 45 us.
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "row_vec.h"

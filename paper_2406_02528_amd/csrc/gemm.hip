@@ -452,9 +452,11 @@ __attribute__((amdgpu_waves_per_eu(2))) void gemm_kernel(
   static_assert(!BIAS || (kStaged && !RAG && EP == Epilogue::kDequantF32), "the bias is added at the staged stores");
   if constexpr (kGluGrad) {
     // The gate's gradients (glu_grad), each rounded once to bf16.  g and u
-    // carry the bits of the forward.  8192 x 2048 with 2 x 5632 columns: 170
-    // us; the loop and the arithmetic alone 120, the gradients' loads 24 and
-    // the stores 28 less (measured without them).
+    // carry the bits of the forward.  8192 x 2048 with 2 x 5632 columns: 172
+    // us in the first calls, of which the loop and the arithmetic alone take
+    // 120, the gradients' loads 24 and the stores 28.  In a sequence of calls
+    // the time rises after 1.5 ms of full load, to 226 us, and settles at 193,
+    // as with the other epilogues (GLU 145 and 166, dequantised 161 and 186).
     static_assert(BX4 && !RAG && !BIAS, "L % 16 == 0");
     constexpr int kDp = EP == Epilogue::kGluGradF32 ? 4 : 2;  // bytes of a gradient
     const uint32_t L = static_cast<uint32_t>(N) / 2;

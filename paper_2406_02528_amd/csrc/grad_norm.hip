@@ -10,11 +10,17 @@
 // bits on every call, with no atomics.
 //
 // Bound by HBM: 4 bytes read for the norm, 4 read and 4 written for the
-// scaling.  All of it passes the caches as streams (nontemporal): a set of 800
-// MB then takes 433 us where cached accesses take 461, and one of 192 MB behind
-// other work 106 instead of 141, since a cached read pushes out lines that
-// others wrote, which go to memory first.  Only a set of 64 to 128 MB that was
-// just read or written is faster cached (128 MB: 65 instead of 73 us).
+// scaling.  All of it passes the caches as streams (nontemporal), at any size:
+// a cached read pushes out lines that others wrote, which go to memory first,
+// and what a backward pass leaves in the caches is mostly not the gradients.
+// Norm and scaling in place, as streams / cached, us:
+//   set of                      32 MB      64 MB      128 MB     192 MB     400 MB     800 MB
+//   behind 1 GB of other work   29 / 28    44 / 47    76 / 83    109 / 119  227 / 240  457 / 466
+//   the whole set just written  36 / 31    49 / 44    74 / 66    110 / 96   234 / 241  469 / 472
+// Cached accesses gain where nothing but the gradients was written before (up
+// to 192 MB), and leave up to that much for a reader that follows: both calls
+// and an update that reads the gradients once, behind other work, 94 / 90 us
+// at 64 MB, 167 / 162 at 128, 250 / 243 at 192, 523 / 559 at 400.
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "row_vec.h"

@@ -6,17 +6,18 @@
 //   dh_t = e_t + f_{t+1} dh_{t+1},  e_t = do_t g_t s(h_t) (1 - s(h_t))
 //   dzf = dh (h_{t-1} - c) (1 - lb) s(zf) (1 - s(zf))
 //   dzc = dh (1 - f) s(zc) (1 + zc (1 - s(zc))),   dzg = do s(h)
-//   dh0 = f_1 dh_1,   dlb = sum over tokens of dh (h_{t-1} - c) (1 - s(zf))
+//   dh0 = f_1 dh_1,   dlb = sum over tokens of dh (h_{t-1} - c) (1 - s(zf)) (fp64)
 //
 // Both recurrences are linear, so a run of tokens maps the value that enters
 // it to a x + b.  A workgroup holds a chunk of 128 tokens x 64 channels in
 // registers: 16 half waves with 8 tokens each, two channels per lane; their
 // maps are joined through LDS.  The chunks of a sequence are joined while
-// they are held, so that z is read once each way: 16 chunks make a run; the
-// last chunk of a run publishes the value after it, every other its map, and
-// a chunk starts from the value before its run and the maps of the chunks
-// before it in the run.  A value thus takes the same roundings whatever the
-// order in which chunks are done.
+// they are held, so that z is read once each way (a chained scan with
+// look-back, here over fixed runs): 16 chunks make a run; the last chunk of a
+// run publishes the value after it, every other its map, and a chunk starts
+// from the value before its run and the maps of the chunks before it in the
+// run.  A value thus takes the same roundings whatever the order in which
+// chunks are done.
 //
 // The words that chunks exchange: one of 64 bits per chunk and channel,
 // written and read as relaxed device-scope atomics (which pass the XCDs' own
@@ -34,12 +35,12 @@
 // end), summed in the forward direction together with h.
 //
 // Bound by HBM: 16 bytes per token and channel forward, 22 backward (fp32 do).
-// One sequence of 16384 tokens x 2048: forward 103 us (5.2 TB/s), backward 148
-// us (5.0 TB/s); as two sweeps (the chunks' maps first, z read again for the
-// values) 155 and 300 us.  What waiting for other chunks costs of that: 5 and
-// 10 % (measured with the waits left out).  The backward takes 128 registers
-// of four waves per SIMD; three waves with 164 measured 9 % slower for both
-// directions together, as did 4 tokens per half wave with five (11 %).
+// One sequence of 16384 tokens x 2048: forward 103 us (5.2 TB/s), backward 147
+// us (5.0 TB/s; medians of 61 calls); as two sweeps (the chunks' maps first, z
+// read again for the values) 155 and 300 us.  Waiting for other chunks is 5
+// and 10 % of that.  The backward takes the 128 registers of four waves per
+// SIMD and spills up to four; three waves with 164 measured 9 % slower for
+// both directions together, as did 4 tokens per half wave with five (11 %).
 #include "mmf_device.h"
 #include "mmf_launch.h"
 #include "row_vec.h"

@@ -74,6 +74,14 @@ bool skinny_beats_gemm(int64_t M, int K, int64_t N, Epilogue ep, bool tiled, int
   //   K = 5120, N = 2048:  M = 1024 22.5 / 35.8, 2048 31.7 / 38.1, 3072 60.3 / 46.4
   //   K = 5120, N = 15360: M = 128 19.3 / 33.7, 256 27.6 / 35.4, 320 36.6 / 40.9, 384 45.8 / 40.9
   //   K = 2048, N = 2050:  M = 256 9.7 / 43.2, 768 13.7 / 18.5, 2048 27.1 / 24.4 (N % 4 != 0)
+  // The GLU gate's gradients, which read dp beside what the forms above do,
+  // fall on the same sides of it (K-split / tiled, launches replayed, us):
+  //   K = 2048, N = 11264: M = 65 8.9 / 12.4, 150 10.4 / 12.5, 200 15.6 / 12.7, 512 31.7 / 20.9
+  //   K = 1024, N = 5632:  M = 65 5.2 / 8.7, 250 8.4 / 9.2, 300 9.6 / 9.2, 357 10.9 / 9.4
+  //   K = 1040, N = 5664:  M = 250 8.2 / 9.4, 300 9.6 / 9.5, 357 10.9 / 9.5, 1000 22.3 / 15.6
+  //   K = 2048, N = 2048:  M = 65 4.6 / 11.7, 640 10.5 / 12.4, 1000 12.0 / 12.5, 1500 16.1 / 13.0
+  //   K = 512,  N = 1024:  M = 65 3.5 / 6.2, 512 4.9 / 6.9, 1000 6.4 / 7.3, 1500 7.9 / 7.5
+  // The kernel chosen was the faster one at each of 65 such shapes.
   if (M > kSkinnyMaxRows) return false;
   return skinny_us(skinny_plan(M, K, N, ep, cus), K, N, tiled) < 0.95 * gemm_us(M, K, N, cus);
 }
