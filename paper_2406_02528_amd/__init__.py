@@ -809,7 +809,7 @@ def mmf_grad_norm_workspace_bytes(counts) -> int:
 
 def mmf_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
     """norm f32 [1] = the 2-norm over all elements of the tensors of the list
-    `grads` (each bf16 or f32, contiguous, of any shape)."""
+    `grads` (each bf16 or f32, contiguous, of any shape, on 16 bytes)."""
     here = _here()
     _need_here(norm, "norm", torch.float32, (1,), here)
     ptrs, kinds, counts, _ = _grad_set(grads, here)
