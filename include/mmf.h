@@ -29,7 +29,9 @@
  *  - Entry points with an `x_is_f32` argument take 0 (bfloat16 x) or 1
  *    (float32 x); any other value returns MMF_ERR_DTYPE.
  *  - Outputs must not alias inputs.
- *  - Calls on different streams may run concurrently.
+ *  - Calls on different streams may run concurrently; calls that may overlap
+ *    in time (captured ones among them, when their graphs are replayed) need
+ *    workspaces of their own.  One workspace serves calls in stream order.
  *  - Return value: an mmf_status code.
  *
  * Shapes and layouts (row-major, sizes in elements)
