@@ -39,7 +39,7 @@
 // us (5.0 TB/s; medians of 61 calls); as two sweeps (the chunks' maps first, z
 // read again for the values) 155 and 300 us.  Waiting for other chunks is 5
 // and 10 % of that.  The backward takes the 128 registers of four waves per
-// SIMD and spills up to four; three waves with 164 measured 9 % slower for
+// SIMD and spills up to two; three waves with 164 measured 9 % slower for
 // both directions together, as did 4 tokens per half wave with five (11 %).
 #include "mmf_device.h"
 #include "mmf_launch.h"
@@ -82,7 +82,7 @@ struct Place {
   int64_t b, k;     // sequence and chunk
   int64_t row0;     // first row of the chunk in the [B*T] arrays
   int rows;         // of its tokens inside the sequence
-  int64_t c;        // first of the lane's two channels
+  int64_t c0, c;    // first channel of the workgroup and of the lane's two
   bool col;         // inside d
   int sub, lane;    // half wave, lane in it
   int u0;           // its first token in the chunk
@@ -142,7 +142,8 @@ __device__ __forceinline__ Place place(int64_t T, int64_t d, int64_t B, int64_t 
   p.row0 = p.b * T + p.k * kChunk;
   const int64_t left = T - p.k * kChunk;
   p.rows = left < kChunk ? static_cast<int>(left) : kChunk;
-  const int64_t c = static_cast<int64_t>(grp % ncg) * kCh + 2 * p.lane;
+  p.c0 = static_cast<int64_t>(grp % ncg) * kCh;
+  const int64_t c = p.c0 + 2 * p.lane;
   p.col = c < d;
   p.c = p.col ? c : d - 2;
   return p;
@@ -277,6 +278,15 @@ __device__ __forceinline__ float afresh(float v) {
   return v;
 }
 
+// p.c, computed again from the lane's number in its wave: kept from one use to
+// the next it is what the registers spill.
+__device__ __forceinline__ int64_t channel_afresh(const Place& p, int64_t d) {
+  int all = -1;
+  asm volatile("" : "+s"(all));
+  const int64_t c = p.c0 + 2 * (__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0)) % kLanes);
+  return p.col ? c : d - 2;
+}
+
 struct BwdArgs {
   const float* z;
   const float* lb;
@@ -360,7 +370,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
   Map2 whole = kSame;
   if constexpr (MANY) {
     const int64_t pos = a.nchunk - 1 - p.k;
-    uint64_t* words = a.words + p.b * a.nchunk * d + p.c;
+    uint64_t* words = a.words + p.b * a.nchunk * d + channel_afresh(p, d);
     if (p.sub == 0) {
 #pragma unroll 2
       for (int i = kSubs - 1; i >= 0; --i) whole = then(whole, back[i][p.lane]);
@@ -391,7 +401,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     dz.store_bf16(u, 0, dfx, dfy);
     dz.store_bf16(u, dgate, dcx, dcy);
   }
-  if (p.k == 0 && p.sub == 0 && p.col && a.dh0 != nullptr) st2(a.dh0 + p.b * d + p.c, G);
+  if (p.k == 0 && p.sub == 0 && p.col && a.dh0 != nullptr) st2(a.dh0 + p.b * d + channel_afresh(p, d), G);
   if (a.dlb_part != nullptr) {
     s_dlb[p.sub][p.lane] = make_double2(dlx, dly);
     __syncthreads();
@@ -402,7 +412,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
         x += s_dlb[i][p.lane].x;
         y += s_dlb[i][p.lane].y;
       }
-      *reinterpret_cast<double2*>(a.dlb_part + at) = make_double2(x, y);
+      *reinterpret_cast<double2*>(a.dlb_part + (p.b * a.nchunk + p.k) * d + channel_afresh(p, d)) = make_double2(x, y);
     }
   }
 }
