@@ -35,8 +35,8 @@
 // end), summed in the forward direction together with h.
 //
 // Bound by HBM: 16 bytes per token and channel forward, 22 backward (fp32 do).
-// One sequence of 16384 tokens x 2048: forward 103 us (5.2 TB/s), backward 147
-// us (5.0 TB/s; medians of 61 calls); as two sweeps (the chunks' maps first, z
+// One sequence of 16384 tokens x 2048: forward 102 us (5.2 TB/s), backward 142
+// us (5.2 TB/s; medians of 61 calls); as two sweeps (the chunks' maps first, z
 // read again for the values) 155 and 300 us.  Waiting for other chunks is 5
 // and 10 % of that.  The backward takes the 128 registers of four waves per
 // SIMD and spills up to two; three waves with 164 measured 9 % slower for
