@@ -567,6 +567,53 @@ int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *co
                   const float *norm, float max_norm, void *const *outs, hipStream_t stream);
 
 /*
+ * Linear attention with a decay per head, the token mixer whose state is a
+ * matrix: for each sequence and head, with decay l = decay[h],
+ *   S_t = l S_{t-1} + k_t v_t^T   [dk][dv],   o_t = scale S_t^T q_t   [dv]
+ * from the stacked projection qkv [B*T][H (2 dk + dv)], token t of sequence b in
+ * row b*T + t: q of all heads [H][dk], then k [H][dk], then v [H][dv] (one
+ * BitLinear of the stacked latent weights, as f | c | g for the MLGRU).
+ * qkv: bf16 bits or float32 (qkv_is_f32); o [B*T][H][dv] in the same type; decay
+ * [H] float32 (constants of the model, any numbers; 0 keeps the token itself
+ * only); s0 [B][H][dk][dv] float32 or NULL (0); s_last [B][H][dk][dv] float32,
+ * the state after the last token (NULL: not stored; may be the same array as
+ * s0: the state is then updated in place).  No other overlap is allowed.
+ * dk and dv: multiples of 16 up to 256; B*H at most 2^20, H (2 dk + dv) at most
+ * 2^22 (MMF_ERR_SHAPE).
+ * B == 0 or T == 0 is a no-op, which leaves s_last as it was.  Workspace
+ * (256-byte aligned, MMF_ERR_WORKSPACE; mmf_linattn_workspace_bytes, which may
+ * be 0) or NULL: then allocated stream-ordered on `stream` and freed there.
+ */
+size_t mmf_linattn_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
+int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float scale,
+                    const float *s0, void *o, float *s_last, int64_t B, int64_t T, int64_t H,
+                    int64_t dk, int64_t dv, void *workspace, size_t workspace_bytes,
+                    hipStream_t stream);
+/* Its backward, from the gradient dout of o and ds_last of the last state:
+ *   dS_t = l dS_{t+1} + scale q_t dout_t^T   (+ ds_last at the last token)
+ *   dq_t = scale S_t dout_t,  dk_t = dS_t v_t,  dv_t = dS_t^T k_t,  ds0 = l dS_1
+ * dout [B*T][H][dv] bf16 bits or float32 (do_is_f32); ds_last [B][H][dk][dv]
+ * float32 or NULL (0); qkv, decay, scale and s0 as in the forward.  Outputs:
+ * dqkv [B*T][H (2 dk + dv)] bf16 (the dO of mmf_bitlinear_bwd for the stacked
+ * projection), ds0 [B][H][dk][dv] float32 (NULL: not stored; may be the same
+ * array as ds_last).  No other overlap is allowed; nothing is kept from the
+ * forward.  The decay is a constant: it gets no gradient.  Limits, no-op and
+ * workspace as above (the size is mmf_linattn_bwd_workspace_bytes).
+ *
+ * Both directions form their products on the matrix cores where there are more
+ * than a few tokens: bf16 inputs as they are, everything in fp32 (fp32 inputs,
+ * decayed products, states) as sums of bf16 parts, to 2^-16 of each factor
+ * where the result is rounded to bf16 and 2^-24 where it is float32.  Inputs
+ * should be finite: one that is not reaches its own token and the later ones
+ * (backward: the earlier ones) of its sequence and head, there as NaN where the
+ * formula has an infinity, and nothing else. */
+size_t mmf_linattn_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
+int mmf_linattn_bwd(const void *qkv, int qkv_is_f32, const float *decay, float scale,
+                    const float *s0, const void *dout, int do_is_f32, const float *ds_last,
+                    uint16_t *dqkv, float *ds0, int64_t B, int64_t T, int64_t H, int64_t dk,
+                    int64_t dv, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Kernel selection for the contraction: MMF_PATH_AUTO (the fused decode, the
  * K-split or the tiled GEMM kernel by size; see mmf_bitlinear_fwd),
  * MMF_PATH_GEMV or MMF_PATH_GEMM force one kernel for every M (the decode

@@ -105,6 +105,12 @@ _SIGNATURES = {
     "mmf_grad_norm_workspace_bytes": ([_P, _I64], _SZ),
     "mmf_grad_norm": ([_P, _P, _P, _I64, _P, _P, _SZ, _P], ctypes.c_int),
     "mmf_grad_clip": ([_P, _P, _P, _I64, _P, ctypes.c_float, _P, _P], ctypes.c_int),
+    "mmf_linattn_workspace_bytes": ([_I64] * 5, _SZ),
+    "mmf_linattn_fwd": ([_P, ctypes.c_int, _P, ctypes.c_float, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _P, _SZ, _P],
+                        ctypes.c_int),
+    "mmf_linattn_bwd_workspace_bytes": ([_I64] * 5, _SZ),
+    "mmf_linattn_bwd": ([_P, ctypes.c_int, _P, ctypes.c_float, _P, _P, ctypes.c_int, _P, _P, _P, _I64, _I64, _I64, _I64,
+                         _I64, _P, _SZ, _P], ctypes.c_int),
     "mmf_mlgru_fwd": ([_P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                        _I64, _I64, _I64, _P, _SZ, _P], ctypes.c_int),
 }
@@ -837,6 +843,60 @@ def mmf_grad_clip(grads, norm: torch.Tensor, max_norm: float, outs=None, stream=
             raise ValueError("a tensor to write is in the list twice")
     _check(_lib.mmf_grad_clip(_at(ptrs), _at(kinds), _at(counts), len(ptrs), _ptr(norm), max_norm, _at(dst),
                               _stream_here(stream, here)))
+
+
+def mmf_linattn_workspace_bytes(B: int, T: int, H: int, dk: int, dv: int) -> int:
+    return int(_lib.mmf_linattn_workspace_bytes(B, T, H, dk, dv))
+
+
+def mmf_linattn_fwd(qkv: torch.Tensor, B: int, T: int, H: int, dk: int, dv: int, decay: torch.Tensor, scale: float,
+                    s0: torch.Tensor | None, o: torch.Tensor, s_last: torch.Tensor | None,
+                    workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Linear attention with a decay per head: o [B*T][H dv] in the type of qkv
+    bf16/f32 [B*T][H (2 dk + dv)] (q | k | v) and the last state s_last f32
+    [B][H][dk][dv] (or None; may be s0) from decay f32 [H] and the first state
+    s0 (or None)."""
+    here = _here()
+    dt = torch.float32 if _kind(qkv, "qkv") else torch.bfloat16
+    _need_here(qkv, "qkv", dt, (B * T, H * (2 * dk + dv)), here)
+    _need_here(decay, "decay", torch.float32, (H,), here)
+    if s0 is not None:
+        _need_here(s0, "s0", torch.float32, (B, H, dk, dv), here)
+    _need_here(o, "o", dt, (B * T, H * dv), here)
+    if s_last is not None:
+        _need_here(s_last, "s_last", torch.float32, (B, H, dk, dv), here)
+    wp, wn = _ws_here(workspace, here)
+    _check(_lib.mmf_linattn_fwd(_ptr(qkv), dt is torch.float32, _ptr(decay), scale, _ptr(s0), _ptr(o), _ptr(s_last),
+                                B, T, H, dk, dv, wp, wn, _stream_here(stream, here)))
+
+
+def mmf_linattn_bwd_workspace_bytes(B: int, T: int, H: int, dk: int, dv: int) -> int:
+    return int(_lib.mmf_linattn_bwd_workspace_bytes(B, T, H, dk, dv))
+
+
+def mmf_linattn_bwd(qkv: torch.Tensor, B: int, T: int, H: int, dk: int, dv: int, decay: torch.Tensor, scale: float,
+                    s0: torch.Tensor | None, dout: torch.Tensor, ds_last: torch.Tensor | None, dqkv: torch.Tensor,
+                    ds0: torch.Tensor | None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Backward of mmf_linattn_fwd: dqkv bf16 [B*T][H (2 dk + dv)] (the dO of
+    mmf_bitlinear_bwd) and ds0 f32 [B][H][dk][dv] (or None; may be ds_last) from
+    dout bf16/f32 [B*T][H dv], ds_last f32 [B][H][dk][dv] (or None) and the
+    forward's inputs."""
+    here = _here()
+    qkv_f32, do_f32 = _kind(qkv, "qkv"), _kind(dout, "dout")
+    rows, wide, state = B * T, H * (2 * dk + dv), (B, H, dk, dv)
+    _need_here(qkv, "qkv", qkv.dtype, (rows, wide), here)
+    _need_here(decay, "decay", torch.float32, (H,), here)
+    if s0 is not None:
+        _need_here(s0, "s0", torch.float32, state, here)
+    _need_here(dout, "dout", dout.dtype, (rows, H * dv), here)
+    if ds_last is not None:
+        _need_here(ds_last, "ds_last", torch.float32, state, here)
+    _need_here(dqkv, "dqkv", torch.bfloat16, (rows, wide), here)
+    if ds0 is not None:
+        _need_here(ds0, "ds0", torch.float32, state, here)
+    wp, wn = _ws_here(workspace, here)
+    _check(_lib.mmf_linattn_bwd(_ptr(qkv), qkv_f32, _ptr(decay), scale, _ptr(s0), _ptr(dout), do_f32, _ptr(ds_last),
+                                _ptr(dqkv), _ptr(ds0), B, T, H, dk, dv, wp, wn, _stream_here(stream, here)))
 
 
 def mmf_bitlinear_train_workspace_bytes(M: int, K: int, N: int) -> int:

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "linattn.h"
 #include "mmf.h"
 #include "mmf_launch.h"
 
@@ -309,6 +310,25 @@ int check_grads(const void* const* grads, const int* is_f32, const int64_t* coun
     if (!aligned16(grads[i])) return MMF_ERR_ALIGN;
   }
   return MMF_OK;
+}
+
+// ---- linear attention ----
+constexpr int64_t kMaxStates = int64_t(1) << 20;  // B H: a few workgroups each stay within a launch
+int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
+  if (dk <= 0 || dk % 16 != 0 || dk > mmf::kLinattnMaxDim || dv <= 0 || dv % 16 != 0 || dv > mmf::kLinattnMaxDim)
+    return MMF_ERR_SHAPE;
+  if (B < 0 || T < 0 || H < 1 || B > kMaxMN || T > kMaxMN || (T > 0 && B > kMaxMN / T)) return MMF_ERR_SHAPE;
+  if (H > kMaxStates || B > kMaxStates / H) return MMF_ERR_SHAPE;
+  // 64 rows of fp32 within a buffer resource
+  if (H * (2 * dk + dv) > int64_t(1) << 22) return MMF_ERR_SHAPE;
+  return MMF_OK;
+}
+
+// Up to this many tokens go through the state one by one.
+constexpr int64_t kLinattnSteps = 16;
+size_t linattn_fwd_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
+  if (T <= kLinattnSteps) return 0;
+  return round_up(mmf::linattn_chunk_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
 }
 
 // ---- residual addition + quantisation, backward ----
@@ -1210,6 +1230,53 @@ int mmf_glu_bwd(const void* dp, int dp_is_f32, const void* x, int x_is_f32, cons
     return run_bwd({dgu, x, x_is_f32 == 1, gamma, rstd, q, a_scale, Wpacked, w_scale, dx, dW, nullptr, dgamma, M, K,
                     2 * L},
                    s.bwd, scratch + s.bwd_off, stream);
+  });
+}
+
+size_t mmf_linattn_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
+  if (check_linattn(B, T, H, dk, dv) != MMF_OK) return 0;
+  return linattn_fwd_bytes(B, T, H, dk, dv);
+}
+
+int mmf_linattn_fwd(const void* qkv, int qkv_is_f32, const float* decay, float scale, const float* s0, void* o,
+                    float* s_last, int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_dtype(qkv_is_f32)) return st;
+  if (int st = check_linattn(B, T, H, dk, dv)) return st;
+  if (B == 0 || T == 0) return MMF_OK;
+  if (!qkv || !decay || !o) return MMF_ERR_NULL;
+  if (!aligned16(qkv) || !aligned16(decay) || !aligned16_or_null(s0) || !aligned16(o) || !aligned16_or_null(s_last))
+    return MMF_ERR_ALIGN;
+  const mmf::LinattnArgs a{qkv, qkv_is_f32 == 1, decay, scale, s0, o, s_last, B, T, H, static_cast<int>(dk),
+                           static_cast<int>(dv)};
+  return with_workspace(workspace, workspace_bytes, linattn_fwd_bytes(B, T, H, dk, dv), stream, [&](char* scratch) {
+    return hip_status(T <= kLinattnSteps ? mmf::launch_linattn_step(a, stream)
+                                         : mmf::launch_linattn_chunk(a, reinterpret_cast<float*>(scratch), stream));
+  });
+}
+
+size_t mmf_linattn_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
+  if (check_linattn(B, T, H, dk, dv) != MMF_OK) return 0;
+  return round_up(mmf::linattn_bwd_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
+}
+
+int mmf_linattn_bwd(const void* qkv, int qkv_is_f32, const float* decay, float scale, const float* s0,
+                    const void* dout, int do_is_f32, const float* ds_last, uint16_t* dqkv, float* ds0, int64_t B,
+                    int64_t T, int64_t H, int64_t dk, int64_t dv, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
+  if (int st = check_dtype(qkv_is_f32)) return st;
+  if (int st = check_dtype(do_is_f32)) return st;
+  if (int st = check_linattn(B, T, H, dk, dv)) return st;
+  if (B == 0 || T == 0) return MMF_OK;
+  if (!qkv || !decay || !dout || !dqkv) return MMF_ERR_NULL;
+  if (!aligned16(qkv) || !aligned16(decay) || !aligned16_or_null(s0) || !aligned16(dout) ||
+      !aligned16_or_null(ds_last) || !aligned16(dqkv) || !aligned16_or_null(ds0))
+    return MMF_ERR_ALIGN;
+  const mmf::LinattnBwdArgs a{qkv, qkv_is_f32 == 1, decay, scale, s0, dout, do_is_f32 == 1, ds_last, dqkv, ds0, B, T, H,
+                              static_cast<int>(dk), static_cast<int>(dv)};
+  const size_t need = mmf_linattn_bwd_workspace_bytes(B, T, H, dk, dv);
+  return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
+    return hip_status(mmf::launch_linattn_bwd(a, reinterpret_cast<float*>(scratch), stream));
   });
 }
 
