@@ -614,6 +614,75 @@ int mmf_linattn_bwd(const void *qkv, int qkv_is_f32, const float *decay, float s
                     int64_t dv, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * One step of beam search: the n best continuations of the W beams of each of
+ * B batches by one token, from the beams' scores and the logits behind them,
+ *   score(w, v) = scores[b][w] + z[b][w][v] - ln sum_v exp z[b][w][v]
+ * in the order of falling scores; equal scores by rising beam, then falling
+ * logit, then rising token.  logits [B][W][V] bf16 bits or float32
+ * (logits_is_f32); scores [B][W] float32 (-inf: a beam that is not there, such
+ * as all but the first at the first step).  done [B][W] bytes or NULL: a beam
+ * whose byte is not 0 has ended; it goes on as itself, its logits (not read)
+ * taken as 0 at token `end` and -inf elsewhere.  end: the token that ends a
+ * sequence, or -1 (none; done must then be NULL, MMF_ERR_ARG).  Out, [B][n]:
+ * new_scores float32, tokens and parents (the beam, 0 .. W-1) int32, and
+ * new_done bytes (NULL: not stored): 1 where the parent was done or the token
+ * is `end`.  The outputs must not overlap the inputs.
+ * The scores are compared in fp64.  Logits that are NaN count as -inf; +inf
+ * leaves the others of its row at -inf; a row of -inf alone, and scores of NaN
+ * or +inf, give -inf.  Candidates of score -inf come last, in the same order, so
+ * that n are always returned.
+ * W and n: 1 to 64, V up to 2^24, n <= W V, B W ceil(V / 1024) at most 2^23
+ * (MMF_ERR_SHAPE).  B == 0 is a no-op.  Workspace (256-byte aligned,
+ * MMF_ERR_WORKSPACE), or NULL: then allocated stream-ordered on `stream` and
+ * freed there.
+ */
+size_t mmf_beam_select_workspace_bytes(int64_t B, int64_t W, int64_t V, int64_t n);
+int mmf_beam_select(const void *logits, int logits_is_f32, const float *scores,
+                    const uint8_t *done, int64_t end, float *new_scores, int32_t *tokens,
+                    int32_t *parents, uint8_t *new_done, int64_t B, int64_t W, int64_t V,
+                    int64_t n, void *workspace, size_t workspace_bytes, hipStream_t stream);
+/* The states of all beams reordered after their parents: for each of `count`
+ * arrays of B*W rows (the h of mmf_mlgru_fwd, the states of mmf_linattn_fwd,
+ * tokens so far), row (b, j) of outs[i] = row (b, parents[b][j]) of states[i].
+ * states, outs and row_bytes are HOST arrays of `count` entries, read before the
+ * call returns: device addresses (16-byte aligned; any where row_bytes is 0) and
+ * bytes of a row (multiples of 16, B times one at most 2^33, MMF_ERR_SHAPE).
+ * outs[i] may be states[i]: rows that stay where they are are then neither read
+ * nor written.  No other overlap.  parents [B][W] int32 on the device (n = W
+ * above); a row whose entry is not in 0 .. W-1 stays itself.  W: 1 to 64.
+ * Allocates nothing. */
+int mmf_beam_reorder(const void *const *states, void *const *outs, const int64_t *row_bytes,
+                     int64_t count, const int32_t *parents, int64_t B, int64_t W,
+                     hipStream_t stream);
+
+/*
+ * Distillation from a teacher's best tokens: the divergence of the student's
+ * distribution over the vocabulary from the teacher's over K tokens.  For each
+ * row, with the teacher's logits t [K] of the tokens idx [K] and temperature tau:
+ *   p = softmax(t / tau),  ln q = ln softmax(z / tau)  over all V
+ *   loss = tau^2 sum_j p_j (ln p_j - ln q[idx_j])
+ *   dz = dloss tau (q - sum of the p_j at each token)
+ * z [M][V] and t [M][K] bf16 bits or float32 each (z_is_f32, t_is_f32); idx
+ * [M][K] int32; an entry whose idx is outside [0, V) or whose t is -inf is none,
+ * and a token that is there twice counts twice.  Out: loss [M] float32, of the
+ * backward optional (NULL); dz [M][V] bf16 (the dO of mmf_bitlinear_bwd of an
+ * un-embedding) or float32 (dz_is_f32), from dloss [M] float32.  The backward
+ * needs nothing from the forward: a training step that knows dloss is the
+ * backward alone.  dz may be z where the types are equal (MMF_ERR_ARG where they
+ * are not); no other overlap.
+ * Rows without an entry have loss 0 and gradient 0, and rows with dloss 0
+ * gradient 0, whatever z holds (padding).  Else a row of z with a NaN or +inf,
+ * or of -inf alone, gives NaN.  fp32, sums and losses in fp64, rounded once.
+ * V up to 2^24, K up to 1024, M up to 2^22 (MMF_ERR_SHAPE); tau must be positive
+ * and finite (MMF_ERR_ARG).  M == 0 is a no-op.  Allocates nothing.
+ */
+int mmf_distill_fwd(const void *z, int z_is_f32, const int32_t *idx, const void *t, int t_is_f32,
+                    float tau, float *loss, int64_t M, int64_t V, int64_t K, hipStream_t stream);
+int mmf_distill_bwd(const void *z, int z_is_f32, const int32_t *idx, const void *t, int t_is_f32,
+                    float tau, const float *dloss, void *dz, int dz_is_f32, float *loss, int64_t M,
+                    int64_t V, int64_t K, hipStream_t stream);
+
+/*
  * Kernel selection for the contraction: MMF_PATH_AUTO (the fused decode, the
  * K-split or the tiled GEMM kernel by size; see mmf_bitlinear_fwd),
  * MMF_PATH_GEMV or MMF_PATH_GEMM force one kernel for every M (the decode

@@ -111,6 +111,13 @@ _SIGNATURES = {
     "mmf_linattn_bwd_workspace_bytes": ([_I64] * 5, _SZ),
     "mmf_linattn_bwd": ([_P, ctypes.c_int, _P, ctypes.c_float, _P, _P, ctypes.c_int, _P, _P, _P, _I64, _I64, _I64, _I64,
                          _I64, _P, _SZ, _P], ctypes.c_int),
+    "mmf_beam_select_workspace_bytes": ([_I64] * 4, _SZ),
+    "mmf_beam_select": ([_P, ctypes.c_int, _P, _P, _I64, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _P, _SZ, _P],
+                        ctypes.c_int),
+    "mmf_beam_reorder": ([_P, _P, _P, _I64, _P, _I64, _I64, _P], ctypes.c_int),
+    "mmf_distill_fwd": ([_P, ctypes.c_int, _P, _P, ctypes.c_int, ctypes.c_float, _P, _I64, _I64, _I64, _P], ctypes.c_int),
+    "mmf_distill_bwd": ([_P, ctypes.c_int, _P, _P, ctypes.c_int, ctypes.c_float, _P, _P, ctypes.c_int, _P, _I64, _I64,
+                         _I64, _P], ctypes.c_int),
     "mmf_mlgru_fwd": ([_P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                        _I64, _I64, _I64, _P, _SZ, _P], ctypes.c_int),
 }
@@ -897,6 +904,104 @@ def mmf_linattn_bwd(qkv: torch.Tensor, B: int, T: int, H: int, dk: int, dv: int,
     wp, wn = _ws_here(workspace, here)
     _check(_lib.mmf_linattn_bwd(_ptr(qkv), qkv_f32, _ptr(decay), scale, _ptr(s0), _ptr(dout), do_f32, _ptr(ds_last),
                                 _ptr(dqkv), _ptr(ds0), B, T, H, dk, dv, wp, wn, _stream_here(stream, here)))
+
+
+def mmf_beam_select_workspace_bytes(B: int, W: int, V: int, n: int) -> int:
+    return int(_lib.mmf_beam_select_workspace_bytes(B, W, V, n))
+
+
+def mmf_beam_select(logits: torch.Tensor, scores: torch.Tensor, done: torch.Tensor | None, end: int, B: int, W: int,
+                    n: int, new_scores: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor,
+                    new_done: torch.Tensor | None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """One step of beam search: new_scores f32, tokens i32 and parents i32 [B][n]
+    (and new_done u8, or None) of the n best continuations, from logits bf16/f32
+    [B*W][V], scores f32 [B][W], done u8 [B][W] (or None) and the token `end`
+    (-1: none)."""
+    here = _here()
+    is_f32 = _kind(logits, "logits")
+    V = logits.shape[-1]
+    _need_here(logits, "logits", logits.dtype, (B * W, V), here)
+    _need_here(scores, "scores", torch.float32, (B, W), here)
+    if done is not None:
+        _need_here(done, "done", torch.uint8, (B, W), here)
+    _need_here(new_scores, "new_scores", torch.float32, (B, n), here)
+    _need_here(tokens, "tokens", torch.int32, (B, n), here)
+    _need_here(parents, "parents", torch.int32, (B, n), here)
+    if new_done is not None:
+        _need_here(new_done, "new_done", torch.uint8, (B, n), here)
+    wp, wn = _ws_here(workspace, here)
+    _check(_lib.mmf_beam_select(_ptr(logits), is_f32, _ptr(scores), _ptr(done), end, _ptr(new_scores), _ptr(tokens),
+                                _ptr(parents), _ptr(new_done), B, W, V, n, wp, wn, _stream_here(stream, here)))
+
+
+def _state_ptrs(tensors, name, rows, here):
+    """Addresses and row sizes of a list of contiguous tensors of `rows` rows on the current device."""
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}[{i}] must be a torch.Tensor")
+        if t.dim() < 1 or t.shape[0] != rows:
+            raise ValueError(f"{name}[{i}] must have {rows} rows, got shape {tuple(t.shape)}")
+        _need_here(t, f"{name}[{i}]", t.dtype, t.shape, here)
+    return (array.array("Q", [t.data_ptr() for t in tensors]),
+            array.array("q", [t.nbytes // rows if rows else 0 for t in tensors]))
+
+
+def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, stream=None) -> None:
+    """outs[i] row (b, j) = states[i] row (b, parents[b][j]) for a list of tensors
+    [B*W][...] of any type (rows of a multiple of 16 bytes); outs None: in place.
+    parents i32 [B][W].  outs[i] has the type and shape of states[i]; no two of
+    them may overlap."""
+    here = _here()
+    states = _listed(states, "states")
+    _need_here(parents, "parents", torch.int32, (B, W), here)
+    src, rows = _state_ptrs(states, "states", B * W, here)
+    dst = src
+    if outs is not None:
+        outs = _listed(outs, "outs")
+        dst, orows = _state_ptrs(outs, "outs", B * W, here)
+        if orows != rows or [t.dtype for t in outs] != [t.dtype for t in states]:
+            raise ValueError("outs must have the types and shapes of states")
+    full = [p for p, r in zip(dst, rows) if r]
+    if len(set(full)) != len(full):
+        raise ValueError("a tensor to write is in the list twice")
+    _check(_lib.mmf_beam_reorder(_at(src), _at(dst), _at(rows), len(src), _ptr(parents), B, W,
+                                 _stream_here(stream, here)))
+
+
+def _distill_args(z, idx, t, here):
+    z_f32, t_f32 = _kind(z, "z"), _kind(t, "t")
+    M, V = z.shape
+    K = idx.shape[1]
+    _need_here(z, "z", z.dtype, (M, V), here)
+    _need_here(idx, "idx", torch.int32, (M, K), here)
+    _need_here(t, "t", t.dtype, (M, K), here)
+    return M, V, K, z_f32, t_f32
+
+
+def mmf_distill_fwd(z: torch.Tensor, idx: torch.Tensor, t: torch.Tensor, tau: float, loss: torch.Tensor,
+                    stream=None) -> None:
+    """loss f32 [M] of student logits z bf16/f32 [M][V] from a teacher's logits t
+    bf16/f32 [M][K] of the tokens idx i32 [M][K] (outside [0, V): none)."""
+    here = _here()
+    M, V, K, z_f32, t_f32 = _distill_args(z, idx, t, here)
+    _need_here(loss, "loss", torch.float32, (M,), here)
+    _check(_lib.mmf_distill_fwd(_ptr(z), z_f32, _ptr(idx), _ptr(t), t_f32, tau, _ptr(loss), M, V, K,
+                                _stream_here(stream, here)))
+
+
+def mmf_distill_bwd(z: torch.Tensor, idx: torch.Tensor, t: torch.Tensor, tau: float, dloss: torch.Tensor,
+                    dz: torch.Tensor, loss: torch.Tensor | None = None, stream=None) -> None:
+    """dz bf16/f32 [M][V] (may be z) from dloss f32 [M], and the loss f32 [M] (or
+    None), in one pass; z, idx, t and tau as in mmf_distill_fwd."""
+    here = _here()
+    M, V, K, z_f32, t_f32 = _distill_args(z, idx, t, here)
+    dz_f32 = _kind(dz, "dz")
+    _need_here(dloss, "dloss", torch.float32, (M,), here)
+    _need_here(dz, "dz", dz.dtype, (M, V), here)
+    if loss is not None:
+        _need_here(loss, "loss", torch.float32, (M,), here)
+    _check(_lib.mmf_distill_bwd(_ptr(z), z_f32, _ptr(idx), _ptr(t), t_f32, tau, _ptr(dloss), _ptr(dz), dz_f32, _ptr(loss),
+                                M, V, K, _stream_here(stream, here)))
 
 
 def mmf_bitlinear_train_workspace_bytes(M: int, K: int, N: int) -> int:

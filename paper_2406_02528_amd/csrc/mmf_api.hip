@@ -6,6 +6,8 @@
 #include <cstring>
 #include <mutex>
 
+#include "beam.h"
+#include "distill.h"
 #include "linattn.h"
 #include "mmf.h"
 #include "mmf_launch.h"
@@ -312,6 +314,8 @@ int check_grads(const void* const* grads, const int* is_f32, const int64_t* coun
   return MMF_OK;
 }
 
+constexpr int64_t kMaxRows = int64_t(1) << 22;  // workgroups of 1024 threads of a launch
+
 // ---- linear attention ----
 constexpr int64_t kMaxStates = int64_t(1) << 20;  // B H: a few workgroups each stay within a launch
 int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
@@ -329,6 +333,22 @@ constexpr int64_t kLinattnSteps = 16;
 size_t linattn_fwd_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
   if (T <= kLinattnSteps) return 0;
   return round_up(mmf::linattn_chunk_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
+}
+
+// ---- beam search ----
+// Rows of logits and workgroups of a launch stay below 2^23.
+int check_beam(int64_t B, int64_t W, int64_t V, int64_t n) {
+  if (B < 0 || W < 1 || W > mmf::kBeamMax || V < 1 || V > int64_t(1) << 24 || n < 1 || n > mmf::kBeamMax || n > W * V)
+    return MMF_ERR_SHAPE;
+  if (B * W > (int64_t(1) << 23) || B * W * ((V + 1023) / 1024) > (int64_t(1) << 23)) return MMF_ERR_SHAPE;
+  return MMF_OK;
+}
+
+// ---- distillation ----
+int check_distill(int64_t M, int64_t V, int64_t K, float tau) {
+  if (M < 0 || M > kMaxRows || V < 1 || V > int64_t(1) << 24 || K < 1 || K > mmf::kDistillMaxK) return MMF_ERR_SHAPE;
+  if (!(tau > 0.0f) || tau == __builtin_inff()) return MMF_ERR_ARG;
+  return MMF_OK;
 }
 
 // ---- residual addition + quantisation, backward ----
@@ -1278,6 +1298,76 @@ int mmf_linattn_bwd(const void* qkv, int qkv_is_f32, const float* decay, float s
   return with_workspace(workspace, workspace_bytes, need, stream, [&](char* scratch) {
     return hip_status(mmf::launch_linattn_bwd(a, reinterpret_cast<float*>(scratch), stream));
   });
+}
+
+size_t mmf_beam_select_workspace_bytes(int64_t B, int64_t W, int64_t V, int64_t n) {
+  if (check_beam(B, W, V, n) != MMF_OK) return 0;
+  return round_up(mmf::beam_select_bytes(B, static_cast<int>(W), static_cast<int>(V), static_cast<int>(n)),
+                  kScratchAlign);
+}
+
+int mmf_beam_select(const void* logits, int logits_is_f32, const float* scores, const uint8_t* done, int64_t end,
+                    float* new_scores, int32_t* tokens, int32_t* parents, uint8_t* new_done, int64_t B, int64_t W,
+                    int64_t V, int64_t n, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_dtype(logits_is_f32)) return st;
+  if (int st = check_beam(B, W, V, n)) return st;
+  if (end < -1 || end >= V || (done && end < 0)) return MMF_ERR_ARG;
+  if (B == 0) return MMF_OK;
+  if (!logits || !scores || !new_scores || !tokens || !parents) return MMF_ERR_NULL;
+  if (!aligned16(logits) || !aligned16(scores) || !aligned16_or_null(done) || !aligned16(new_scores) ||
+      !aligned16(tokens) || !aligned16(parents) || !aligned16_or_null(new_done))
+    return MMF_ERR_ALIGN;
+  const mmf::BeamSelectArgs a{logits, logits_is_f32 == 1, scores, done, static_cast<int>(end), B, static_cast<int>(W),
+                              static_cast<int>(V), static_cast<int>(n), new_scores, tokens, parents, new_done};
+  return with_workspace(workspace, workspace_bytes, mmf_beam_select_workspace_bytes(B, W, V, n), stream,
+                        [&](char* scratch) { return hip_status(mmf::launch_beam_select(a, scratch, stream)); });
+}
+
+int mmf_beam_reorder(const void* const* states, void* const* outs, const int64_t* row_bytes, int64_t count,
+                     const int32_t* parents, int64_t B, int64_t W, hipStream_t stream) {
+  if (count < 0 || count > kMaxMN || B < 0 || B > (int64_t(1) << 23) || W < 1 || W > mmf::kBeamMax) return MMF_ERR_SHAPE;
+  if (count > 0 && (!states || !outs || !row_bytes)) return MMF_ERR_NULL;
+  const int64_t most = (int64_t(1) << 33) / (B > 0 ? B : 1);  // a launch's workgroups of 256 columns of 4 bytes
+  for (int64_t i = 0; i < count; ++i)
+    if (row_bytes[i] < 0 || row_bytes[i] % 16 != 0 || row_bytes[i] > most) return MMF_ERR_SHAPE;
+  if (count == 0 || B == 0) return MMF_OK;
+  if (!parents) return MMF_ERR_NULL;
+  if (!aligned16(parents)) return MMF_ERR_ALIGN;
+  for (int64_t i = 0; i < count; ++i) {
+    if (row_bytes[i] == 0) continue;
+    if (!states[i] || !outs[i]) return MMF_ERR_NULL;
+    if (!aligned16(states[i]) || !aligned16(outs[i])) return MMF_ERR_ALIGN;
+  }
+  return hip_status(mmf::launch_beam_reorder({states, outs, row_bytes, count, parents, B, static_cast<int>(W)}, stream));
+}
+
+int mmf_distill_fwd(const void* z, int z_is_f32, const int32_t* idx, const void* t, int t_is_f32, float tau,
+                    float* loss, int64_t M, int64_t V, int64_t K, hipStream_t stream) {
+  if (int st = check_dtype(z_is_f32)) return st;
+  if (int st = check_dtype(t_is_f32)) return st;
+  if (int st = check_distill(M, V, K, tau)) return st;
+  if (M == 0) return MMF_OK;
+  if (!z || !idx || !t || !loss) return MMF_ERR_NULL;
+  if (!aligned16(z) || !aligned16(idx) || !aligned16(t) || !aligned16(loss)) return MMF_ERR_ALIGN;
+  return hip_status(mmf::launch_distill({z, z_is_f32 == 1, idx, t, t_is_f32 == 1, tau, nullptr, nullptr, false, loss, M, V, K},
+                                        stream));
+}
+
+int mmf_distill_bwd(const void* z, int z_is_f32, const int32_t* idx, const void* t, int t_is_f32, float tau,
+                    const float* dloss, void* dz, int dz_is_f32, float* loss, int64_t M, int64_t V, int64_t K,
+                    hipStream_t stream) {
+  if (int st = check_dtype(z_is_f32)) return st;
+  if (int st = check_dtype(t_is_f32)) return st;
+  if (int st = check_dtype(dz_is_f32)) return st;
+  if (int st = check_distill(M, V, K, tau)) return st;
+  if (M == 0) return MMF_OK;
+  if (!z || !idx || !t || !dloss || !dz) return MMF_ERR_NULL;
+  if (!aligned16(z) || !aligned16(idx) || !aligned16(t) || !aligned16(dloss) || !aligned16(dz) ||
+      !aligned16_or_null(loss))
+    return MMF_ERR_ALIGN;
+  if (dz == z && z_is_f32 != dz_is_f32) return MMF_ERR_ARG;
+  return hip_status(mmf::launch_distill(
+      {z, z_is_f32 == 1, idx, t, t_is_f32 == 1, tau, dloss, dz, dz_is_f32 == 1, loss, M, V, K}, stream));
 }
 
 size_t mmf_grad_norm_workspace_bytes(const int64_t* counts, int64_t n) {
