@@ -5,15 +5,17 @@
 //   loss = tau^2 sum_j p_j (ln p_j - ln q[idx_j])
 //   dz = dloss tau (q - p at idx)
 //
-// One workgroup of 1024 threads takes a row and keeps it in registers (up to
-// kHeld values per thread), so that the maximum, the sum and the gradient are
-// one pass over memory; longer rows are read again from the caches.  The K
-// teacher entries are handled in LDS; their gradients are written again after
-// the row's, behind a barrier.
+// A workgroup takes a row and keeps it in registers, so that the maximum, the
+// sum and the gradient are one pass over memory; rows of more than 65536 are
+// read again for the gradient.  Rows are vectors of 8 values that start on 16
+// bytes in z and dz alike, and the few values before and after them.  What
+// the teacher's entries need (their softmax, z at their tokens, which of them
+// share a token) is done while the row's loads are in flight; their
+// gradients are written again after the row's, behind a barrier.
 //
-// fp32 with the sums of 4 or 8 exponentials and the rest in fp64; the loss in
-// fp64 (p ln p - p ln q cancels where the student agrees).  Bound by HBM: one
-// read of z, one write of dz.
+// fp32 with the sums of 8 exponentials and the rest in fp64; the loss and the
+// gradient at the entries in fp64 (p ln p - p ln q and q - p cancel where the
+// student agrees).  Bound by HBM: one read of z, one write of dz.
 #include "distill.h"
 #include "mmf_device.h"
 #include "row_vec.h"
@@ -21,7 +23,6 @@
 namespace mmf {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr double kLog2e = 1.4426950408889634074;
 
 template <typename T>
@@ -30,120 +31,278 @@ __device__ __forceinline__ float value(const T* p) {
   else return bf16_to_f32(*p);
 }
 
-struct Shared {
-  double sum[kWaves];
-  float max[kWaves];
-  double part[kWaves];
+// The teacher's entries of a row: token (-1: none, or one that a lower entry
+// has), z there, p (of all entries of that token).
+struct Entries {
   int idx[kDistillMaxK];
   float z[kDistillMaxK];
   double p[kDistillMaxK];
 };
 
-__device__ __forceinline__ float block_max(float v, float* slot) {
-  v = wave_max_f32(v);
-  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float m = slot[0];
+template <int W>
+struct Slots {
+  float tm[W], zm[W];
+  double te[W], ze[W], loss[W];
+};
+
+template <int W>
+__device__ __forceinline__ float max_of(const float* s) {
+  float m = s[0];
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) m = fmaxf(m, slot[i]);
+  for (int i = 1; i < W; ++i) m = fmaxf(m, s[i]);
   return m;
 }
-__device__ __forceinline__ double block_sum(double v, double* slot) {
-  v = wave_sum_f64(v);
-  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double s = slot[0];
+template <int W>
+__device__ __forceinline__ double sum_of(const double* s) {
+  double t = s[0];
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) s += slot[i];
-  return s;
+  for (int i = 1; i < W; ++i) t += s[i];
+  return t;
 }
 
-// The simple form: every pass over the row from memory, a value at a time.
-template <typename T, typename D>
-__global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a) {
-  __shared__ Shared sh;
+// HELD: vectors per thread, kept in registers (0: read twice).
+template <typename T, typename D, int THREADS, int HELD, bool NT>
+__global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a) {
+  constexpr int W = THREADS / kWave, E = 8;
+  __shared__ Entries en;
+  __shared__ Slots<W> sl;
+  __shared__ int s_twice;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t m = blockIdx.x;
   const int V = static_cast<int>(a.V), K = static_cast<int>(a.K);
   const T* const z = static_cast<const T*>(a.z) + m * V;
   D* const dz = a.dz != nullptr ? static_cast<D*>(a.dz) + m * V : nullptr;
-  const double c = kLog2e / a.tau;
-  const float cf = static_cast<float>(c);
+  // values before the first whole vector, whole vectors, values after them
+  const int ahead = static_cast<int>((E - m * V % E) % E);
+  const int head = ahead < V ? ahead : V;
+  const int nv = (V - head) / E, tail = V - head - nv * E;
+  const auto rz = row_rsrc(z + head, nv * E, true);
+  const int own = tid < head ? tid : tid >= E && tid - E < tail ? head + nv * E + tid - E : -1;  // a value outside the vectors
 
-  // the teacher's entries
-  const int j = threadIdx.x;
-  int ij = -1;
-  float tj = -__builtin_inff();
-  if (j < K) {
-    ij = a.idx[m * K + j];
-    if (ij < 0 || ij >= V) ij = -1;
-    if (ij >= 0) tj = a.t_is_f32 ? static_cast<const float*>(a.t)[m * K + j] : bf16_to_f32(static_cast<const uint16_t*>(a.t)[m * K + j]);
-    if (tj == -__builtin_inff()) ij = -1;
-    sh.idx[j] = ij;
-    sh.z[j] = ij >= 0 ? value(z + ij) : 0.0f;
+  RowVec<T, E> in[HELD > 0 ? HELD : 1];
+  if constexpr (HELD > 0) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) in[i].template load<NT>(rz, tid + i * THREADS);
+  }
+  float zx = own >= 0 ? value(z + own) : -__builtin_inff();
+
+  // --- the teacher's entries
+  const double inv = 1.0 / a.tau;
+  const float c = static_cast<float>(kLog2e / a.tau);
+  if (tid == 0) s_twice = 0;
+  float tm = -__builtin_inff();
+  bool any = false;
+  for (int j = tid; j < K; j += THREADS) {
+    int i = a.idx[m * K + j];
+    const float t = a.t_is_f32 ? static_cast<const float*>(a.t)[m * K + j]
+                               : bf16_to_f32(static_cast<const uint16_t*>(a.t)[m * K + j]);
+    if (i < 0 || i >= V || t == -__builtin_inff()) i = -1;
+    en.idx[j] = i;
+    en.z[j] = i >= 0 ? value(z + i) : 0.0f;
+    en.p[j] = t;
+    any |= i >= 0;
+    if (i >= 0) tm = fmaxf(tm, t);
   }
   const float w = a.dloss != nullptr ? a.dloss[m] : 0.0f;
-  const bool none = !__syncthreads_or(ij >= 0);
-  if (none || (dz != nullptr && w == 0.0f && a.loss == nullptr)) {
-    if (threadIdx.x == 0 && a.loss != nullptr) a.loss[m] = 0.0f;
-    if (dz != nullptr)
-      for (int i = threadIdx.x; i < V; i += kThreads) dz[i] = static_cast<D>(0);
+  const bool none = !__syncthreads_or(any);
+  if (none || (w == 0.0f && a.loss == nullptr)) {
+    if (tid == 0 && a.loss != nullptr) a.loss[m] = 0.0f;
+    if (dz != nullptr) {
+      RowVec<D, E> o;
+#pragma unroll
+      for (int i = 0; i < o.kWords; ++i) o.w[i] = 0;
+      for (int v = tid; v < nv; v += THREADS) o.template store<NT>(dz + head, v);
+      if (own >= 0) dz[own] = static_cast<D>(0);
+    }
     return;
   }
-  const float tm = block_max(tj, sh.max);
-  const double u = ij >= 0 ? (static_cast<double>(tj) - tm) / a.tau : 0.0;
-  const double eu = ij >= 0 ? exp(u) : 0.0;
-  const double su = block_sum(eu, sh.sum);
-  const double lnp = u - log(su), p = ij >= 0 ? eu / su : 0.0;
-  if (j < K) sh.p[j] = p;
+  if (dz != nullptr) {  // entries of one token
+    for (int j = tid; j < K; j += THREADS) {
+      const int i = en.idx[j];
+      bool same = false;
+      for (int k = 0; k < K; ++k) same |= k != j && en.idx[k] == i;
+      if (same && i >= 0) s_twice = 1;
+    }
+  }
 
-  float zm = -__builtin_inff();
-  for (int i = threadIdx.x; i < V; i += kThreads) {
-    const float x = value(z + i);
-    zm = fmaxf(zm, x);
+  // --- maxima
+  float zm = zx;
+  double ze = 0.0;
+  if constexpr (HELD > 0) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (tid + i * THREADS < nv) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) zm = fmaxf(zm, in[i].get(e));
+      }
+  } else {
+    // the sum as well, against the thread's own running maximum
+    for (int v = tid; v < nv; v += THREADS) {
+      RowVec<T, E> x;
+      x.load(rz, v);
+      float vm = zm;
+#pragma unroll
+      for (int e = 0; e < E; ++e) vm = fmaxf(vm, x.get(e));
+      if (vm > zm) {
+        ze *= __builtin_amdgcn_exp2f((zm - vm) * c);
+        zm = vm;
+      }
+      float s = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((x.get(e) - zm) * c);
+      ze += s;
+    }
+  }
+  const float own_max = zm;
+  tm = wave_max_f32(tm);
+  zm = wave_max_f32(zm);
+  if (lane == 0) {
+    sl.tm[wave] = tm;
+    sl.zm[wave] = zm;
   }
   __syncthreads();
-  zm = block_max(zm, sh.max);
-  double s = 0.0;
-  for (int i = threadIdx.x; i < V; i += kThreads) s += __builtin_amdgcn_exp2f((value(z + i) - zm) * cf);
-  const double sum = block_sum(s, sh.part);
-  double l = 0.0;
-  if (ij >= 0 && p > 0.0) l = p * (lnp - ((static_cast<double>(sh.z[j]) - zm) / a.tau - log(sum)));
+  tm = max_of<W>(sl.tm);
+  zm = max_of<W>(sl.zm);
+
+  // --- sums; the exponentials stay in place of the row
+  float ex[HELD > 0 ? HELD : 1][E];
+  if constexpr (HELD > 0) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      float s = 0.0f;
+      const bool on = tid + i * THREADS < nv;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        ex[i][e] = __builtin_amdgcn_exp2f((in[i].get(e) - zm) * c);
+        s += ex[i][e];
+      }
+      if (on) ze += s;
+    }
+    zx = __builtin_amdgcn_exp2f((zx - zm) * c);
+    if (own >= 0) ze += zx;
+  } else {
+    // a thread without a value above -inf has no sum
+    ze = own_max == -__builtin_inff() ? (zm == own_max ? __builtin_nan("") : 0.0)
+                                      : ze * __builtin_amdgcn_exp2f((own_max - zm) * c);
+    zx = __builtin_amdgcn_exp2f((zx - zm) * c);
+    if (own >= 0) ze += zx;
+  }
+  double te = 0.0;
+  for (int j = tid; j < K; j += THREADS)
+    if (en.idx[j] >= 0) {
+      const double x = exp((en.p[j] - tm) * inv);
+      te += x;
+    }
+  te = wave_sum_f64(te);
+  ze = wave_sum_f64(ze);
+  if (lane == 0) {
+    sl.te[wave] = te;
+    sl.ze[wave] = ze;
+  }
   __syncthreads();
-  const double loss = block_sum(l, sh.sum);
-  if (threadIdx.x == 0 && a.loss != nullptr) a.loss[m] = static_cast<float>(loss * a.tau * a.tau);
-  if (dz == nullptr) return;
-  const bool zero = w == 0.0f;
+  te = sum_of<W>(sl.te);
+  ze = sum_of<W>(sl.ze);
+
+  // --- the loss, and p in place of t
+  double loss = 0.0;
+  if (wave * kWave < K) {
+    const double lt = log(te), lz = log(ze);
+    for (int j = tid; j < K; j += THREADS)
+      if (en.idx[j] >= 0) {
+        const double u = (en.p[j] - tm) * inv, p = exp(u) / te;
+        if (!(p == 0.0)) loss += p * (u - lt - ((static_cast<double>(en.z[j]) - zm) * inv - lz));
+        en.p[j] = p;
+      }
+  }
+  if (a.loss != nullptr) {
+    loss = wave_sum_f64(loss);
+    if (lane == 0) sl.loss[wave] = loss;
+  }
+
+  // --- the gradient of the row
   const double wt = static_cast<double>(w) * a.tau;
-  const float g = static_cast<float>(wt / sum);
+  const float g = static_cast<float>(wt / ze);
   const auto put = [&](int i, float y) {
-    if (zero) y = 0.0f;
+    if (w == 0.0f) y = 0.0f;
     if constexpr (sizeof(D) == 4) dz[i] = y;
     else dz[i] = static_cast<uint16_t>(pack_bf16(y, 0.0f));
   };
-  for (int i = threadIdx.x; i < V; i += kThreads) put(i, __builtin_amdgcn_exp2f((value(z + i) - zm) * cf) * g);
-  __syncthreads();
-  if (ij >= 0) {
-    bool first = true;
-    double ps = 0.0;
-    for (int k = 0; k < K; ++k)
-      if (sh.idx[k] == ij) {
-        if (k < j) first = false;
-        ps += sh.p[k];
+  if (dz != nullptr) {
+    const bool zero = w == 0.0f;
+    const auto vec = [&](int v, const float* x) {
+      float y[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = zero ? 0.0f : x[e] * g;
+      RowVec<D, E> o;
+      o.set(y);
+      o.template store<NT>(dz + head, v);
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (tid + i * THREADS < nv) vec(tid + i * THREADS, ex[i]);
+    } else {
+      for (int v = tid; v < nv; v += THREADS) {
+        RowVec<T, E> x;
+        x.load(rz, v);
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = __builtin_amdgcn_exp2f((x.get(e) - zm) * c);
+        vec(v, y);
       }
-    if (first) put(ij, static_cast<float>((__builtin_amdgcn_exp2f((sh.z[j] - zm) * cf) / sum - ps) * wt));
+    }
+    if (own >= 0) put(own, zx * g);
   }
+  __syncthreads();
+  if (tid == 0 && a.loss != nullptr) a.loss[m] = static_cast<float>(sum_of<W>(sl.loss) * a.tau * a.tau);
+  if (dz == nullptr) return;
+  // --- and at the teacher's tokens
+  for (int j = tid; j < K; j += THREADS) {
+    const int i = en.idx[j];
+    if (i < 0) continue;
+    double p = en.p[j];
+    if (s_twice != 0) {  // the lowest entry of a token for all of them
+      bool first = true;
+      p = 0.0;
+      for (int k = 0; k < K; ++k)
+        if (en.idx[k] == i) {
+          first &= k >= j;
+          p += en.p[k];
+        }
+      if (!first) continue;
+    }
+    put(i, static_cast<float>((__builtin_amdgcn_exp2f((en.z[j] - zm) * c) / ze - p) * wt));
+  }
+}
+
+template <typename T, typename D, bool NT>
+hipError_t launch(const DistillArgs& a, hipStream_t stream) {
+  const auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(a.M)), dim3(threads), 0, stream, a);
+    return hipGetLastError();
+  };
+  const int64_t nv = a.V / 8;  // the most whole vectors of a row
+  if (nv <= 2 * 256) return go(distill_kernel<T, D, 256, 2, NT>, 256);
+  if (nv <= 4 * 256) return go(distill_kernel<T, D, 256, 4, NT>, 256);
+  if (nv <= 4 * 512) return go(distill_kernel<T, D, 512, 4, NT>, 512);
+  if (nv <= 8 * 512) return go(distill_kernel<T, D, 512, 8, NT>, 512);
+  if (nv <= 8 * 1024) return go(distill_kernel<T, D, 1024, 8, NT>, 1024);
+  return go(distill_kernel<T, D, 1024, 0, NT>, 1024);
 }
 
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(a.M));
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a);
-    return hipGetLastError();
-  };
-  if (a.z_is_f32) return a.dz_is_f32 ? go(distill_kernel<float, float>) : go(distill_kernel<float, uint16_t>);
-  return a.dz_is_f32 ? go(distill_kernel<uint16_t, float>) : go(distill_kernel<uint16_t, uint16_t>);
+  // the loss alone: D does not matter
+  const bool d32 = a.dz != nullptr && a.dz_is_f32;
+  const int64_t bytes = a.M * a.V * ((a.z_is_f32 ? 4 : 2) + (a.dz == nullptr ? 0 : d32 ? 4 : 2));
+  const bool nt = bytes >= kLastLevelBytes && a.V <= 65536 + 7;
+  if (a.z_is_f32) {
+    if (d32) return nt ? launch<float, float, true>(a, stream) : launch<float, float, false>(a, stream);
+    return nt ? launch<float, uint16_t, true>(a, stream) : launch<float, uint16_t, false>(a, stream);
+  }
+  if (d32) return nt ? launch<uint16_t, float, true>(a, stream) : launch<uint16_t, float, false>(a, stream);
+  return nt ? launch<uint16_t, uint16_t, true>(a, stream) : launch<uint16_t, uint16_t, false>(a, stream);
 }
 
 }  // namespace mmf
