@@ -579,7 +579,7 @@ int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *co
  * the state after the last token (NULL: not stored; may be the same array as
  * s0: the state is then updated in place).  No other overlap is allowed.
  * dk and dv: multiples of 16 up to 256; B*H at most 2^20, H (2 dk + dv) at most
- * 2^22 (MMF_ERR_SHAPE).
+ * 2^21 (MMF_ERR_SHAPE).
  * B == 0 or T == 0 is a no-op, which leaves s_last as it was.  Workspace
  * (256-byte aligned, MMF_ERR_WORKSPACE; mmf_linattn_workspace_bytes, which may
  * be 0) or NULL: then allocated stream-ordered on `stream` and freed there.

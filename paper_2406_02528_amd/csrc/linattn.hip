@@ -8,6 +8,7 @@ namespace mmf {
 hipError_t launch_linattn_f32(const LinattnPass& p, bool state, hipStream_t stream);
 hipError_t launch_linattn_bf16(const LinattnPass& p, bool state, hipStream_t stream);
 hipError_t launch_linattn_bwd_bf16(const LinattnPass& p, hipStream_t stream);
+hipError_t launch_linattn_bwd_f32(const LinattnPass& p, hipStream_t stream);
 hipError_t launch_linattn_bwd_any(const LinattnPass& p, bool state, hipStream_t stream);
 
 namespace {
@@ -182,7 +183,9 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* joined, hipStream_
       if (hipError_t e2 = join(p, stream)) return e2;
       p.s_out = nullptr;
     }
-    const hipError_t e = bf16 ? launch_linattn_bwd_bf16(p, stream) : launch_linattn_bwd_any(p, false, stream);
+    const hipError_t e = bf16  ? launch_linattn_bwd_bf16(p, stream)
+                         : f32 ? launch_linattn_bwd_f32(p, stream)
+                               : launch_linattn_bwd_any(p, false, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

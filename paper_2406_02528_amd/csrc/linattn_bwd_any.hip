@@ -1,5 +1,4 @@
-// Linear attention over chunks, backward: fp32 inputs or gradients among the
-// operands.
+// Linear attention over chunks, backward: bf16 and fp32 among the operands.
 #include "linattn_chunk.h"
 
 namespace mmf {

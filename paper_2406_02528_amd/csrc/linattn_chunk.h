@@ -18,21 +18,26 @@
 // segment's own sum, a second joins them into the states that enter the
 // segments, from which the pass itself starts.
 //
-// A workgroup of four waves holds a state of Dk rows and 64 ET columns (16 ET
-// per wave) in the accumulators of its matrix instructions.  The layouts are
-// chosen so that neither the state nor the values ever pass through LDS
-// (v_mfma_f32_16x16x32_bf16; lane = 16 g + n, g = 0..3, n = 0..15; A: row n,
-// B: column n, eight contraction slots j per lane; D: column n, rows 4 g + r):
-//   - the state's tile (b, i) has row 4 g + r = entry d = 64 b + 16 g + 4 r + i
+// A workgroup of eight waves holds a state of Dk rows and 64 ET columns in the
+// accumulators of its matrix instructions: 16 ET columns per wave and, of each
+// four neighbouring rows, two (waves 0-3 and 4-7).  q E of a wave is then a
+// part of the sum; each wave finishes half of the token tiles with the other
+// half's part from LDS.  A chunk's rows are loaded while the chunk before is
+// worked on.  The layouts are chosen so that neither the state nor the values
+// ever pass through LDS (v_mfma_f32_16x16x32_bf16; lane = 16 g + n, g = 0..3, n
+// = 0..15; A: row n, B: column n, eight contraction slots j per lane; D: column
+// n, rows 4 g + r):
+//   - the state's tile (x, i) has row 4 g + r = entry d = 64 x + 16 g + 4 r + i
 //     and column n = entry e = ET n + f of the wave's columns, so that a lane
 //     keeps ET neighbouring columns;
-//   - as the operand B of q E its slots are d = 64 b + 16 g + 4 (j%4) + 2 p +
-//     j/4 (tiles i = 2 p and 2 p + 1 side by side), so a lane's part of a
-//     query or key is 16 consecutive entries of its row, in two operands p;
+//   - as the operand B of q E its slots are d = 64 x + 16 g + 4 (j%4) + 2 h +
+//     j/4 (tiles i = 2 h and 2 h + 1 side by side: h = 0 waves 0-3, 1 waves
+//     4-7), so a lane's part of a query or key is 16 consecutive entries of its
+//     row, in two operands h;
 //   - tokens as contraction slots are s = 32 c + 16 (j/4) + 4 g + j%4, which is
 //     how the transposed products k q^T leave their rows, two tiles side by
 //     side: they go to LDS with 8-byte stores in place;
-//   - a lane's part of the values (and of the transposed keys) are 8 tokens
+//   - a lane's part of the values (and of the transposed keys) are 8 (4) tokens
 //     with ET (4) neighbouring entries each, transposed in registers.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
@@ -50,6 +55,7 @@ namespace mmf {
 namespace la {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
@@ -107,8 +113,8 @@ __device__ __forceinline__ void load_f32(__amdgpu_buffer_rsrc_t r, uint32_t off,
     }
   }
 }
-template <int N>
-__device__ __forceinline__ void load_bf16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t (&w)[N]) {
+template <int N, int W>
+__device__ __forceinline__ void load_bf16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t (&w)[W]) {
   if constexpr (N == 1) {
     w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
   } else {
@@ -118,61 +124,124 @@ __device__ __forceinline__ void load_bf16(__amdgpu_buffer_rsrc_t r, uint32_t off
     for (int i = 0; i < N / 2; ++i) w[i] = h[i];
   }
 }
-// The element e of what was loaded.
-template <int N>
-__device__ __forceinline__ float element(const uint32_t (&w)[N], bool f32, int e) {
-  if (f32) return __uint_as_float(w[e]);
-  if (N == 1) return bf16_lo(w[0]);
-  return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
-}
-
-// Rows of one operand: token i of a chunk and `width` elements of its head.
+// Rows of one operand in a chunk.  A row past the chunk's tokens has an offset
+// past the resource (forward: above it; backward, where token i is row tc - 1 -
+// i: below 0, which is far above it), so it reads as zero with no mask; so
+// has a column past the head's width (kOff, which no token's step reaches:
+// 64 rows take at most 2^29 bytes).
+constexpr uint32_t kOff = 0x80000000u;
 template <Kind K>
 struct Rows {
   __amdgpu_buffer_rsrc_t r;
-  uint32_t ld;      // bytes of a row
+  uint32_t base;    // of token 0
+  int step;         // from a token to the next
   int width;
   bool f32_;
   __device__ __forceinline__ bool f32() const { return K == kEither ? f32_ : K == kF32; }
-  // `n` rows from row `row`.
-  __device__ __forceinline__ void at(const LinattnOperand& x, int64_t row, int n, int64_t h, int w) {
+  // `tc` rows from row `row` of head h, whose entries are `w`.
+  __device__ __forceinline__ void at(const LinattnOperand& x, int64_t row, int tc, int64_t h, int w, bool rev) {
     f32_ = x.is_f32;
-    const uint32_t size = f32() ? 4u : 2u;
-    ld = static_cast<uint32_t>(x.ld) * size;
+    const int size = f32() ? 4 : 2, ld = static_cast<int>(x.ld) * size;
     width = w;
-    char* const base = const_cast<char*>(static_cast<const char*>(x.p)) + (row * x.ld + h * w) * static_cast<int64_t>(size);
-    r = __builtin_amdgcn_make_buffer_rsrc(base, 0, static_cast<int>(static_cast<uint32_t>(n - 1) * ld + w * size), kBufferWord3);
+    step = rev ? -ld : ld;
+    base = rev ? static_cast<uint32_t>((tc - 1) * ld) : 0u;
+    char* const p = const_cast<char*>(static_cast<const char*>(x.p)) + (row * x.ld + h * w) * size;
+    r = __builtin_amdgcn_make_buffer_rsrc(p, 0, (tc - 1) * ld + w * size, kBufferWord3);
   }
-  // Elements d .. d + N - 1 of local row i; `on` false: zeros.
-  template <int N>
-  __device__ __forceinline__ void load(int i, int d, bool on, uint32_t (&w)[N]) const {
-    const uint32_t size = f32() ? 4u : 2u;
-    const uint32_t off = on && d < width ? static_cast<uint32_t>(i) * ld + static_cast<uint32_t>(d) * size : 0x80000000u;
-    if (f32()) load_f32<N>(r, off, w);
-    else load_bf16<N>(r, off, w);
+  // A lane's offset: of token i and column d.  Not a constant of the loop for
+  // the compiler, which would keep an offset in registers for every load.
+  __device__ __forceinline__ uint32_t lane(int i, int d) const {
+    uint32_t o = d < width ? base + static_cast<uint32_t>(i * step + d * (f32() ? 4 : 2)) : kOff;
+    asm volatile("" : "+v"(o));
+    return o;
+  }
+  // N elements, i tokens behind the lane's.
+  template <int N, int W>
+  __device__ __forceinline__ void load(uint32_t lane, int i, uint32_t (&w)[W]) const {
+    const uint32_t off = lane + static_cast<uint32_t>(i * step);
+    if constexpr (K != kBf16) {
+      if (f32()) {
+        load_f32<N>(r, off, w);
+        return;
+      }
+    }
+    if constexpr (K != kF32) load_bf16<N>(r, off, w);
   }
 };
+
+// Dwords that N elements of a kind take in registers.
+template <Kind K, int N>
+constexpr int kDwords = K == kBf16 && N > 1 ? N / 2 : N;
+
+// Eight elements as operand parts: of bf16 elements the bits themselves, two
+// (word, half) each.
+template <Kind K, int NP, typename At>
+__device__ __forceinline__ void operand(At&& at, v4i (&f)[NP]) {
+  if constexpr (K == kBf16) {
+    static_assert(NP == 1, "bf16 operands are exact");
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const auto a = at(2 * w), b = at(2 * w + 1);
+      const uint32_t sel = (a.half ? 0x0302u : 0x0100u) | ((b.half ? 0x0706u : 0x0504u) << 16);
+      f[0][w] = static_cast<int>(__builtin_amdgcn_perm(b.word, a.word, sel));
+    }
+  } else {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = at(j).value();
+    split8<NP>(x, f);
+  }
+}
+struct Element {
+  uint32_t word;
+  bool half, f32;
+  __device__ __forceinline__ float value() const { return f32 ? __uint_as_float(word) : half ? bf16_hi(word) : bf16_lo(word); }
+};
+template <int N>
+__device__ __forceinline__ Element element(const uint32_t (&w)[N], bool f32, int e) {
+  const uint32_t whole = w[e], pair = w[e / 2];
+  return {f32 ? whole : pair, !f32 && (e & 1) != 0, f32};
+}
+// Whether any of N elements of several tokens is not finite: 0 in `bad` else.
+template <int count, int N>
+__device__ __forceinline__ void look(const uint32_t (&w)[N], bool f32, uint32_t& bad) {
+  typedef unsigned short v2us __attribute__((ext_vector_type(2)));
+  // the largest of the magnitudes (bf16: of both halves), as integers
+  if (f32) {
+#pragma unroll
+    for (int i = 0; i < count; ++i) bad = max(bad, (w[i] & 0x7FFFFFFFu) >> 16);
+  } else {
+    constexpr int words = count > 1 ? count / 2 : 1;
+#pragma unroll
+    for (int i = 0; i < words; ++i) {
+      const uint32_t v = count > 1 ? w[i] & 0x7FFF7FFFu : w[i] & 0x7FFFu;
+      bad = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, bad), __builtin_bit_cast(v2us, v)));
+    }
+  }
+}
+__device__ __forceinline__ bool not_finite(uint32_t bad) { return (bad & 0xFFFFu) >= 0x7F80u || (bad >> 16) >= 0x7F80u; }
 
 // MODE: parts of fp32 values in the products of o.  NKT: parts of the weighted
 // keys in the state's.  DK: Dk padded to 64s.  STATE: the segment's own sum
 // only (no queries, no o).
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int ET, int C, bool STATE>
-__global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p) {
-  constexpr int kB = DK / 64;        // 64s of Dk
+__global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p) {
+  constexpr int kX = DK / 64;        // 64s of Dk
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
+  constexpr int kOwn = kT / 2;       // token tiles that a wave finishes
+  constexpr int kPer = 8 / kT;       // waves per tile of keys
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
   constexpr int NV = KV == kBf16 ? 1 : STATE ? NKT : MODE;
-  constexpr int kQFrags = STATE ? 1 : kT * kB * 2 * NQ;
-  constexpr int kKFrags = kB * 4 * kS * NKT;
-  constexpr int kPFrags = STATE ? 1 : kT * kS * MODE;
-  __shared__ v4i q_lds[kQFrags][kWave];   // [t-tile][64s][p][part]
-  __shared__ v4i k_lds[kKFrags][kWave];   // [64s][i][token step][part]
-  __shared__ v4i p_lds[kPFrags][kWave];   // [t-tile][token step][part]
-  __shared__ float pw[C + 1];             // l^i
+  __shared__ v4i q_lds[STATE ? 1 : kT * kX * 2 * NQ][kWave];   // [token tile][64s][h][part]
+  __shared__ v4i k_lds[kX * 4 * kS * NKT][kWave];              // [64s][i][token step][part]
+  __shared__ v4i p_lds[STATE ? 1 : kT * kS * MODE][kWave];     // [token tile][token step][part]
+  __shared__ v4f o_lds[STATE ? 1 : 8 * kOwn * ET][kWave];      // [receiving wave][own tile][f]
+  __shared__ float pw[C + 1];                                  // l^i
   __shared__ int s_bad;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = wave >> 2, ew = wave & 3;
   const int n = lane & 15, g = lane >> 4;
   uint32_t blk = blockIdx.x;
   const uint32_t tile = blk % p.tiles;
@@ -181,8 +250,9 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
   const uint32_t bh = blk / p.nseg;
   if (STATE && seg + 1 == p.nseg && !p.join_last) return;  // no segment follows
   const int64_t b = bh / p.H, h = bh % p.H;
-  const int e0 = static_cast<int>(tile) * 64 * ET + wave * 16 * ET + ET * n;  // the lane's columns e0 .. e0 + ET - 1
-  const bool ewave = static_cast<int>(tile) * 64 * ET + wave * 16 * ET < p.Dv;
+  const int ebase = static_cast<int>(tile) * 64 * ET + ew * 16 * ET;
+  const int e0 = ebase + ET * n;     // the lane's columns e0 .. e0 + ET - 1
+  const bool ewave = ebase < p.Dv;
   const bool eon = e0 < p.Dv;
 
   // powers of l: fp64, by squaring (any l, 0 among them)
@@ -195,7 +265,88 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
     pw[threadIdx.x] = static_cast<float>(y);
   }
   if (threadIdx.x == 0) s_bad = 0;
-  __syncthreads();
+
+  const int64_t begin = static_cast<int64_t>(seg) * p.seg_tokens;
+  const int64_t end = begin + p.seg_tokens < p.T ? begin + p.seg_tokens : p.T;
+  int64_t single = begin;  // tokens before this one go one by one
+  const auto tokens_at = [&](int64_t i) {
+    const int64_t left = end - i;
+    return i < single ? 1 : left < C ? static_cast<int>(left) : C;
+  };
+
+  // --- a chunk's rows: the wave's values; 4 tokens x 4 entries of the keys for
+  // the state; queries and keys of a token tile
+  constexpr int kKItems = kX * kS * 2;
+  const bool has_k = wave < kKItems;
+  const int kx = wave / (2 * kS), kc = wave / 2 % kS, kj = wave & 1;
+  const int qi = kT * kX == 8 ? wave : kT * kX == 4 ? wave - 4 : wave >= 6 ? -1 : wave - 4;   // few: waves 4-7
+  const bool has_q = qi >= 0;
+  const int qt = qi / kX, qx = qi % kX;
+  const int ps = wave % kT, pt = wave / kT;         // the wave's keys, and its first query tile behind them
+  const bool has_p = ps + pt < kT;
+  uint32_t wv[kS][8][kDwords<KV, ET>], wk[4][kDwords<KK, 4>], wq[kDwords<KQ, 16>], wn[kX][kDwords<KK, 16>];
+  Rows<KQ> rq;
+  Rows<KK> rk;
+  Rows<KV> rv;
+  const auto first_row = [&](int64_t i0, int tc) { return b * p.T + (p.rev ? p.T - i0 - tc : i0); };
+  const auto load_most = [&](int64_t i0, int tc) {
+    const int64_t row = first_row(i0, tc);
+    rk.at(p.k, row, tc, h, p.Dk, p.rev);
+    rv.at(p.v, row, tc, h, p.Dv, p.rev);
+    const uint32_t vo = rv.lane(4 * g, e0);
+#pragma unroll
+    for (int c = 0; c < kS; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rv.template load<ET>(vo, 32 * c + 16 * (j / 4) + j % 4, wv[c][j]);
+    if (has_k) {
+      const uint32_t ko = rk.lane(32 * kc + 16 * kj + 4 * g, 64 * kx + 4 * n);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) rk.template load<4>(ko, r, wk[r]);
+    }
+    if constexpr (!STATE) {
+      if (has_q) {
+        rq.at(p.q, row, tc, h, p.Dk, p.rev);
+        rq.template load<16>(rq.lane(16 * qt + n, 64 * qx + 16 * g), 0, wq);
+      }
+    }
+  };
+  const auto load_keys = [&](int64_t i0, int tc) {
+    if constexpr (!STATE) {
+      if (has_p) {
+        rk.at(p.k, first_row(i0, tc), tc, h, p.Dk, p.rev);
+#pragma unroll
+        for (int x = 0; x < kX; ++x) rk.template load<16>(rk.lane(16 * ps + n, 64 * x + 16 * g), 0, wn[x]);
+      }
+    }
+  };
+  load_most(begin, tokens_at(begin));
+  load_keys(begin, tokens_at(begin));
+
+  // the state, [64s][i - 2 half][f]
+  v4f st[kX][2][ET];
+  const float first = p.rev || p.joined != nullptr ? 1.0f : p.decay[h];
+#pragma unroll
+  for (int x = 0; x < kX; ++x)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int f = 0; f < ET; ++f) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v = 0.0f;
+          const int d = 64 * x + 16 * g + 4 * r + 2 * half + i, e = e0 + f;
+          if (!STATE && eon && d < p.Dk) {
+            if (p.joined != nullptr) {
+              v = p.joined[((static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk + d) * p.Dv + e];
+            } else if (p.s_in != nullptr) {
+              v = p.s_in[static_cast<int64_t>(bh) * p.Dk * p.Dv + static_cast<int64_t>(d) * p.in_d + static_cast<int64_t>(e) * p.in_e];
+              v *= first;
+            }
+          }
+          st[x][i][f][r] = v;
+        }
+      }
+  lds_barrier();
 
   const float alpha = p.alpha, beta = p.beta;
   // decays between the rows of a transposed product's tile (keys 4 g + r) and
@@ -212,220 +363,183 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
     }
   }
 
-  // the state, [64s][i][f]
-  v4f st[kB][4][ET];
-#pragma unroll
-  for (int x = 0; x < kB; ++x)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int f = 0; f < ET; ++f) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = 0.0f;
-          const int d = 64 * x + 16 * g + 4 * r + i, e = e0 + f;
-          if (!STATE && eon && d < p.Dk) {
-            if (p.joined != nullptr) {
-              v = p.joined[((static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk + d) * p.Dv + e];
-            } else if (p.s_in != nullptr) {
-              v = p.s_in[static_cast<int64_t>(bh) * p.Dk * p.Dv + static_cast<int64_t>(d) * p.in_d + static_cast<int64_t>(e) * p.in_e];
-              if (!p.rev) v *= pw[1];
-            }
-          }
-          st[x][i][f][r] = v;
-        }
-      }
-
-  const int64_t begin = static_cast<int64_t>(seg) * p.seg_tokens;
-  const int64_t end = begin + p.seg_tokens < p.T ? begin + p.seg_tokens : p.T;
-  int64_t single = begin;  // tokens before this one go one by one
-  Rows<KQ> rq;
-  Rows<KK> rk;
-  Rows<KV> rv;
   for (int64_t i0 = begin; i0 < end;) {
-    const int64_t left = end - i0;
-    const int tc = i0 < single ? 1 : left < C ? static_cast<int>(left) : C;
-    const int64_t row = b * p.T + (p.rev ? p.T - i0 - tc : i0);
-    const auto local = [&](int i) { return p.rev ? tc - 1 - i : i; };
-    rk.at(p.k, row, tc, h, p.Dk);
-    rv.at(p.v, row, tc, h, p.Dv);
+    const int tc = tokens_at(i0);
+    const bool last = i0 + tc == p.T && !p.rev;  // the state behind the last token itself
 
     // --- values of the wave's columns, and whether they are all finite
     v4i vf[kS][ET][NV];
-    float bad = 0.0f;
-    {
-      uint32_t w[kS][8][ET];
+    uint32_t bad = 0;
 #pragma unroll
-      for (int c = 0; c < kS; ++c)
+    for (int c = 0; c < kS; ++c) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int s = 32 * c + 16 * (j / 4) + 4 * g + j % 4;
-          rv.template load<ET>(local(s), e0, s < tc, w[c][j]);
-        }
+      for (int f = 0; f < ET; ++f) operand<KV>([&](int j) { return element(wv[c][j], rv.f32(), f); }, vf[c][f]);
+      if constexpr (!STATE) {
 #pragma unroll
-      for (int c = 0; c < kS; ++c)
-#pragma unroll
-        for (int f = 0; f < ET; ++f) {
-          float x[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            x[j] = element<ET>(w[c][j], rv.f32(), f);
-            bad = fmaf(x[j], 0.0f, bad);
-          }
-          split8<NV>(x, vf[c][f]);
-        }
+        for (int j = 0; j < 8; ++j) look<ET>(wv[c][j], rv.f32(), bad);
+      }
     }
-    if (!STATE && __any(bad != 0.0f) && lane == 0) s_bad = 1;
+    if (!STATE && __any(not_finite(bad)) && lane == 0) s_bad = 1;
 
-    // --- weighted transposed keys: token step and 64s by wave
-    for (int u = wave; u < kB * kS; u += 4) {
-      const int x = u / kS, c = u % kS;
-      uint32_t w[8][4];
-      float wt[8];
+    // --- weighted transposed keys: decays to the next chunk's first token, or
+    // to the last one
+    if (has_k) {
+      float wt[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int s = 32 * c + 16 * (j / 4) + 4 * g + j % 4;
-        rk.template load<4>(local(s), 64 * x + 4 * n, s < tc, w[j]);
-        // decays to the next chunk's first token, or (the forward's last) to
-        // the token itself
-        const int to = i0 + tc == p.T && !p.rev ? tc - 1 - s : tc - s;
-        wt[j] = alpha * pw[to > 0 ? to : 0];
+      for (int r = 0; r < 4; ++r) {
+        const int to = tc - (32 * kc + 16 * kj + 4 * g + r) - (last ? 1 : 0);
+        wt[r] = alpha * pw[to > 0 ? to : 0];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float y[8];
-        v4i f[NKT];
+        float y[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = element<4>(w[j], rk.f32(), i) * wt[j];
-        split8<NKT>(y, f);
+        for (int r = 0; r < 4; ++r) y[r] = element(wk[r], rk.f32(), i).value() * wt[r];
 #pragma unroll
-        for (int k = 0; k < NKT; ++k) k_lds[((x * 4 + i) * kS + c) * NKT + k][lane] = f[k];
-      }
-    }
-
-    if constexpr (!STATE) {
-      // --- queries: token tile by wave
-      rq.at(p.q, row, tc, h, p.Dk);
-      v4i kf[kB * 2][NK];   // the wave's own keys
-      if (wave < kT) {
-        const int t = 16 * wave + n;
-#pragma unroll
-        for (int x = 0; x < kB; ++x) {
-          uint32_t w[16], u[16];
-          rq.template load<16>(local(t), 64 * x + 16 * g, t < tc, w);
-          rk.template load<16>(local(t), 64 * x + 16 * g, t < tc, u);
-#pragma unroll
-          for (int pr = 0; pr < 2; ++pr) {
-            float y[8], z[8];
-            v4i f[NQ];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              y[j] = element<16>(w, rq.f32(), 4 * (j % 4) + 2 * pr + j / 4);
-              z[j] = element<16>(u, rk.f32(), 4 * (j % 4) + 2 * pr + j / 4);
-            }
-            split8<NQ>(y, f);
-            split8<NK>(z, kf[x * 2 + pr]);
-#pragma unroll
-            for (int k = 0; k < NQ; ++k) q_lds[((wave * kB + x) * 2 + pr) * NQ + k][lane] = f[k];
-          }
+        for (int k = 0; k < NKT; ++k) {
+          const uint2 u = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+          reinterpret_cast<uint2*>(&k_lds[((kx * 4 + i) * kS + kc) * NKT + k][lane])[kj] = u;
+          y[0] -= bf16_lo(u.x);
+          y[1] -= bf16_hi(u.x);
+          y[2] -= bf16_lo(u.y);
+          y[3] -= bf16_hi(u.y);
         }
       }
-      __syncthreads();
+    }
+    if constexpr (!STATE) {
+      if (has_q) {
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          v4i f[NQ];
+          operand<KQ>([&](int j) { return element(wq, rq.f32(), 4 * (j % 4) + 2 * hh + j / 4); }, f);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) q_lds[((qt * kX + qx) * 2 + hh) * NQ + k][lane] = f[k];
+        }
+      }
+    }
+    const int64_t next = i0 + tc;
+    if (STATE && next < end) load_most(next, tokens_at(next));
+    lds_barrier();
+
+    if constexpr (!STATE) {
       if (tc > 1 && __builtin_amdgcn_readfirstlane(s_bad) != 0) {  // a value that is not finite reaches no token before it
         single = i0 + tc;
-        __syncthreads();
+        load_most(i0, 1);
+        load_keys(i0, 1);
+        lds_barrier();
         if (threadIdx.x == 0) s_bad = 0;
-        __syncthreads();
+        lds_barrier();
         continue;
       }
-
-      const auto query = [&](int t, int kb, v4i (&f)[NQ]) {
+      const auto query = [&](int t, int x, int hh, v4i (&f)[NQ]) {
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) f[k] = q_lds[(t * kB * 2 + kb) * NQ + k][lane];
+        for (int k = 0; k < NQ; ++k) f[k] = q_lds[((t * kX + x) * 2 + hh) * NQ + k][lane];
       };
-      // --- keys x queries, decayed: rows of the wave's token tile
-      if (wave < kT) {
-        float wx = 1.0f;
+      // --- keys x queries, decayed
+      if (has_p) {
+        v4f acc[(kT + kPer - 1) / kPer];
 #pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          if (t < wave) {
-            if (t == wave - 1 && (wave & 1)) {  // the half of its operand that no tile fills
+        for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) acc[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-              for (int k = 0; k < MODE; ++k)
-                reinterpret_cast<uint2*>(&p_lds[(t * kS + wave / 2) * MODE + k][lane])[1] = make_uint2(0u, 0u);
+        for (int x = 0; x < kX; ++x)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            v4i kf[NK];
+            operand<KK>([&](int j) { return element(wn[x], rk.f32(), 4 * (j % 4) + 2 * hh + j / 4); }, kf);
+#pragma unroll
+            for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) {
+              const int t = ps + pt + u * kPer;
+              if (t >= kT) continue;
+              v4i f[NQ];
+              query(t, x, hh, f);
+              acc[u] = mma<MODE>(kf, f, acc[u]);
             }
-            continue;
           }
-          v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int kb = 0; kb < kB * 2; ++kb) {
-            v4i f[NQ];
-            query(t, kb, f);
-            acc = mma<MODE>(kf[kb], f, acc);
-          }
+        for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) {
+          const int t = ps + pt + u * kPer;
+          if (t >= kT) continue;
           float y[4];
-          if (t == wave) {
+          if (t == ps) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = n >= 4 * g + r ? acc[r] * w_diag[r] : 0.0f;
+            for (int r = 0; r < 4; ++r) y[r] = n >= 4 * g + r ? acc[u][r] * w_diag[r] : 0.0f;
           } else {
+            const float wx = pw[16 * (t - ps - 1)];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = acc[r] * (w_off[r] * wx);
-            wx *= pw[16];
+            for (int r = 0; r < 4; ++r) y[r] = acc[u][r] * (w_off[r] * wx);
           }
 #pragma unroll
           for (int k = 0; k < MODE; ++k) {
-            const uint2 u = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            reinterpret_cast<uint2*>(&p_lds[(t * kS + wave / 2) * MODE + k][lane])[wave & 1] = u;
-            y[0] -= bf16_lo(u.x);
-            y[1] -= bf16_hi(u.x);
-            y[2] -= bf16_lo(u.y);
-            y[3] -= bf16_hi(u.y);
+            const uint2 v = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            reinterpret_cast<uint2*>(&p_lds[(t * kS + ps / 2) * MODE + k][lane])[ps & 1] = v;
+            y[0] -= bf16_lo(v.x);
+            y[1] -= bf16_hi(v.x);
+            y[2] -= bf16_lo(v.y);
+            y[3] -= bf16_hi(v.y);
           }
         }
       }
-      // --- queries x state
-      v4f o[kT][ET];
+      if ((ps & 1) && pt == 1) {  // the half of an operand that no tile fills
+#pragma unroll
+        for (int k = 0; k < MODE; ++k)
+          reinterpret_cast<uint2*>(&p_lds[((ps - 1) * kS + ps / 2) * MODE + k][lane])[1] = make_uint2(0u, 0u);
+      }
+
+      // --- queries x the wave's half of the state; what other waves finish
+      v4f o[kOwn][ET];
       if (ewave) {
+        v4f a[kT][ET];
 #pragma unroll
         for (int t = 0; t < kT; ++t)
 #pragma unroll
-          for (int f = 0; f < ET; ++f) o[t][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int f = 0; f < ET; ++f) a[t][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int x = 0; x < kB; ++x)
+        for (int x = 0; x < kX; ++x) {
+          v4i sf[ET][MODE];
 #pragma unroll
-          for (int pr = 0; pr < 2; ++pr) {
-            v4i sf[ET][MODE];
+          for (int f = 0; f < ET; ++f) {
+            float y[8];
 #pragma unroll
-            for (int f = 0; f < ET; ++f) {
-              float y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = st[x][2 * pr + j / 4][f][j % 4];
-              split8<MODE>(y, sf[f]);
-            }
-#pragma unroll
-            for (int t = 0; t < kT; ++t) {
-              v4i q[NQ];
-              query(t, x * 2 + pr, q);
-#pragma unroll
-              for (int f = 0; f < ET; ++f) o[t][f] = mma<MODE>(q, sf[f], o[t][f]);
-            }
+            for (int j = 0; j < 8; ++j) y[j] = st[x][j / 4][f][j % 4];
+            split8<MODE>(y, sf[f]);
           }
-        float wx = 1.0f;
 #pragma unroll
-        for (int t = 0; t < kT; ++t) {
+          for (int t = 0; t < kT; ++t) {
+            v4i q[NQ];
+            query(t, x, half, q);
 #pragma unroll
-          for (int f = 0; f < ET; ++f)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[t][f][r] *= w_row[r] * wx;
-          wx *= pw[16];
+            for (int f = 0; f < ET; ++f) a[t][f] = mma<MODE>(q, sf[f], a[t][f]);
+          }
         }
+        // tiles 0 and 3 (of 4) or 0 (of 2) are finished by waves 0-3
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u)
+#pragma unroll
+          for (int f = 0; f < ET; ++f) {
+            const int t0 = kT == 4 ? 3 * u : u, t1 = kT == 4 ? 1 + u : 1;
+            o[u][f] = half ? a[t1][f] : a[t0][f];
+            o_lds[((wave ^ 4) * kOwn + u) * ET + f][lane] = half ? a[t0][f] : a[t1][f];
+          }
       }
-      __syncthreads();
+      // the next chunk's rows, in the registers that the sums over all tiles had
+      if (next < end) {
+        load_most(next, tokens_at(next));
+        load_keys(next, tokens_at(next));
+      }
+      lds_barrier();
       if (threadIdx.x == 0) s_bad = 0;
       if (ewave) {
-        // --- products x values
 #pragma unroll
-        for (int t = 0; t < kT; ++t)
+        for (int u = 0; u < kOwn; ++u) {
+          const int t = kT == 4 ? (half ? 1 + u : 3 * u) : half;
+          const float wx = pw[16 * t];
+#pragma unroll
+          for (int f = 0; f < ET; ++f) {
+            const v4f more = o_lds[(wave * kOwn + u) * ET + f][lane];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[u][f][r] = (o[u][f][r] + more[r]) * (w_row[r] * wx);
+          }
+          // --- products x values
 #pragma unroll
           for (int c = 0; c < kS; ++c) {
             if (2 * c > t) continue;
@@ -433,41 +547,42 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
 #pragma unroll
             for (int k = 0; k < MODE; ++k) f[k] = p_lds[(t * kS + c) * MODE + k][lane];
 #pragma unroll
-            for (int e = 0; e < ET; ++e) o[t][e] = mma<MODE>(f, vf[c][e], o[t][e]);
+            for (int e = 0; e < ET; ++e) o[u][e] = mma<MODE>(f, vf[c][e], o[u][e]);
           }
+        }
         // --- store
-        if (eon) {
+        const int size = OF32 ? 4 : 2, ld = static_cast<int>(p.ldo) * size;
+        const auto ro = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.o) + (first_row(i0, tc) * p.ldo + h * p.Dv) * size,
+                                                          0, (tc - 1) * ld + p.Dv * size, kBufferWord3);
+        const int step = p.rev ? -ld : ld;
+        uint32_t at = eon ? static_cast<uint32_t>((p.rev ? (tc - 1) * ld : 0) + 4 * g * step + e0 * size) : kOff;
+        asm volatile("" : "+v"(at));
 #pragma unroll
-          for (int t = 0; t < kT; ++t)
+        for (int u = 0; u < kOwn; ++u) {
+          const int t = kT == 4 ? (half ? 1 + u : 3 * u) : half;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int i = 16 * t + 4 * g + r;
-              if (i < tc) {
-                const int64_t at = (row + local(i)) * p.ldo + h * p.Dv + e0;
-                if constexpr (OF32) {
-                  float* const y = static_cast<float*>(p.o) + at;
-                  if constexpr (ET == 2) *reinterpret_cast<float2*>(y) = make_float2(o[t][0][r], o[t][1][r]);
-                  else *y = o[t][0][r];
-                } else {
-                  uint16_t* const y = static_cast<uint16_t*>(p.o) + at;
-                  if constexpr (ET == 2) *reinterpret_cast<uint32_t*>(y) = pack_bf16(o[t][0][r], o[t][1][r]);
-                  else *y = static_cast<uint16_t>(pack_bf16(o[t][0][r], 0.0f));
-                }
-              }
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t off = at + static_cast<uint32_t>((16 * t + r) * step);
+            if constexpr (OF32) {
+              if constexpr (ET == 2)
+                __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(o[u][0][r]), __float_as_uint(o[u][1][r])}, ro, off, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(o[u][0][r]), ro, off, 0, 0);
+            } else {
+              if constexpr (ET == 2) __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(o[u][0][r], o[u][1][r]), ro, off, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(pack_bf16(o[u][0][r], 0.0f)), ro, off, 0, 0);
             }
+          }
         }
       }
-    } else {
-      __syncthreads();
     }
 
     // --- keys x values into the state
     if (ewave) {
-      const float w = pw[i0 + tc == p.T && !p.rev ? tc - 1 : tc];
+      const float w = pw[last ? tc - 1 : tc];
 #pragma unroll
-      for (int x = 0; x < kB; ++x)
+      for (int x = 0; x < kX; ++x)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
           for (int f = 0; f < ET; ++f)
 #pragma unroll
@@ -476,14 +591,14 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
           for (int c = 0; c < kS; ++c) {
             v4i k[NKT];
 #pragma unroll
-            for (int y = 0; y < NKT; ++y) k[y] = k_lds[((x * 4 + i) * kS + c) * NKT + y][lane];
+            for (int y = 0; y < NKT; ++y) k[y] = k_lds[((x * 4 + 2 * half + i) * kS + c) * NKT + y][lane];
 #pragma unroll
             for (int f = 0; f < ET; ++f) st[x][i][f] = mma<NKT>(k, vf[c][f], st[x][i][f]);
           }
         }
     }
-    __syncthreads();
-    i0 += tc;
+    lds_barrier();
+    i0 = next;
   }
 
   // the segment's own sum, or the state after the last token
@@ -498,35 +613,35 @@ __global__ __launch_bounds__(256) void linattn_chunk_kernel(const LinattnPass p)
   }
   if (out != nullptr && eon) {
 #pragma unroll
-    for (int x = 0; x < kB; ++x)
+    for (int x = 0; x < kX; ++x)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int f = 0; f < ET; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int d = 64 * x + 16 * g + 4 * r + i;
+            const int d = 64 * x + 16 * g + 4 * r + 2 * half + i;
             if (d < p.Dk) out[d * od + (e0 + f) * oe] = st[x][i][f][r];
           }
   }
 }
 
-constexpr int chunk_tokens(int DK) { return DK == 256 ? 32 : 64; }
+constexpr int chunk_tokens(int DK, int MODE, bool STATE) { return DK == 256 || (MODE == 3 && !STATE) ? 32 : 64; }
 
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
 hipError_t launch_pass(const LinattnPass& p, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(p.B * p.H * p.nseg * p.tiles));
   const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(kernel, grid, dim3(512), 0, stream, p);
     return hipGetLastError();
   };
 #define MMF_DIMS(DK)                                                                                          \
-  return p.et == 1 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 1, chunk_tokens(DK), STATE>)    \
-                   : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 2, chunk_tokens(DK), STATE>)
+  return p.et == 1 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 1, chunk_tokens(DK, MODE, STATE), STATE>)    \
+                   : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 2, chunk_tokens(DK, MODE, STATE), STATE>)
   if (p.Dk <= 64) MMF_DIMS(64);
   if (p.Dk <= 128) MMF_DIMS(128);
-  MMF_DIMS(256);
 #undef MMF_DIMS
+  return go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, 256, 1, chunk_tokens(256, MODE, STATE), STATE>);
 }
 
 }  // namespace la

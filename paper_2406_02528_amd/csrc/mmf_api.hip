@@ -323,8 +323,8 @@ int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
     return MMF_ERR_SHAPE;
   if (B < 0 || T < 0 || H < 1 || B > kMaxMN || T > kMaxMN || (T > 0 && B > kMaxMN / T)) return MMF_ERR_SHAPE;
   if (H > kMaxStates || B > kMaxStates / H) return MMF_ERR_SHAPE;
-  // 64 rows of fp32 within a buffer resource
-  if (H * (2 * dk + dv) > int64_t(1) << 22) return MMF_ERR_SHAPE;
+  // 64 rows of fp32 within 2^29 bytes (linattn_chunk.h)
+  if (H * (2 * dk + dv) > int64_t(1) << 21) return MMF_ERR_SHAPE;
   return MMF_OK;
 }
 
