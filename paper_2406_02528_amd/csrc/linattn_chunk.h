@@ -231,6 +231,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
   constexpr int kS = C / 32;         // contraction steps over tokens
   constexpr int kOwn = kT / 2;       // token tiles that a wave finishes
   constexpr int kPer = 8 / kT;       // waves per tile of keys
+  constexpr bool kEarly = STATE || KV == kBf16;   // registers hold the next rows from the start of a chunk
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
   constexpr int NV = KV == kBf16 ? 1 : STATE ? NKT : MODE;
   __shared__ v4i q_lds[STATE ? 1 : kT * kX * 2 * NQ][kWave];   // [token tile][64s][h][part]
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
       }
     }
     const int64_t next = i0 + tc;
-    if (STATE && next < end) load_most(next, tokens_at(next));
+    if (kEarly && next < end) load_most(next, tokens_at(next));
     lds_barrier();
 
     if constexpr (!STATE) {
@@ -484,6 +485,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         for (int k = 0; k < MODE; ++k)
           reinterpret_cast<uint2*>(&p_lds[((ps - 1) * kS + ps / 2) * MODE + k][lane])[1] = make_uint2(0u, 0u);
       }
+      if (kEarly && next < end) load_keys(next, tokens_at(next));
 
       // --- queries x the wave's half of the state; what other waves finish
       v4f o[kOwn][ET];
@@ -522,7 +524,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
           }
       }
       // the next chunk's rows, in the registers that the sums over all tiles had
-      if (next < end) {
+      if (!kEarly && next < end) {
         load_most(next, tokens_at(next));
         load_keys(next, tokens_at(next));
       }
@@ -626,7 +628,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
   }
 }
 
-constexpr int chunk_tokens(int DK, int MODE, bool STATE) { return DK == 256 || (MODE == 3 && !STATE) ? 32 : 64; }
+constexpr int chunk_tokens(int DK, Kind K, bool STATE) { return DK == 256 || (K != kBf16 && !STATE) ? 32 : 64; }
 
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
 hipError_t launch_pass(const LinattnPass& p, hipStream_t stream) {
@@ -636,12 +638,12 @@ hipError_t launch_pass(const LinattnPass& p, hipStream_t stream) {
     return hipGetLastError();
   };
 #define MMF_DIMS(DK)                                                                                          \
-  return p.et == 1 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 1, chunk_tokens(DK, MODE, STATE), STATE>)    \
-                   : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 2, chunk_tokens(DK, MODE, STATE), STATE>)
+  return p.et == 1 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 1, chunk_tokens(DK, KQ, STATE), STATE>)    \
+                   : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 2, chunk_tokens(DK, KQ, STATE), STATE>)
   if (p.Dk <= 64) MMF_DIMS(64);
   if (p.Dk <= 128) MMF_DIMS(128);
 #undef MMF_DIMS
-  return go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, 256, 1, chunk_tokens(256, MODE, STATE), STATE>);
+  return go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, 256, 1, chunk_tokens(256, KQ, STATE), STATE>);
 }
 
 }  // namespace la
