@@ -27,13 +27,15 @@
 // ever pass through LDS (v_mfma_f32_16x16x32_bf16; lane = 16 g + n, g = 0..3, n
 // = 0..15; A: row n, B: column n, eight contraction slots j per lane; D: column
 // n, rows 4 g + r):
-//   - the state's tile (x, i) has row 4 g + r = entry d = 64 x + 16 g + 4 r + i
-//     and column n = entry e = ET n + f of the wave's columns, so that a lane
-//     keeps ET neighbouring columns;
-//   - as the operand B of q E its slots are d = 64 x + 16 g + 4 (j%4) + 2 h +
-//     j/4 (tiles i = 2 h and 2 h + 1 side by side: h = 0 waves 0-3, 1 waves
-//     4-7), so a lane's part of a query or key is 16 consecutive entries of its
-//     row, in two operands h;
+//   - the state's tile (x, i) has row m = entry d = 64 x + 4 pi(m) + i (pi a
+//     permutation of 16, below) and column n = entry e = ET n + f of the wave's
+//     columns, so that a lane keeps ET neighbouring columns;
+//   - as the operand B of q E its slots are the rows m = 4 g + j%4 of tiles i =
+//     2 h + j/4 (side by side: h = 0 waves 0-3, 1 waves 4-7), so a lane's part of a
+//     query or key is four times four entries of its row, in two operands h; pi
+//     puts the four lanes g of a row side by side in each load (16 bytes of fp32:
+//     d = 16 r + 4 g + i, of bf16: d = 8 g + 4 (r%2) + 32 (r/2) + i), where 16
+//     entries in a row per lane would have each load touch four times the lines;
 //   - tokens as contraction slots are s = 32 c + 16 (j/4) + 4 g + j%4, which is
 //     how the transposed products k q^T leave their rows, two tiles side by
 //     side: they go to LDS with 8-byte stores in place;
@@ -169,6 +171,40 @@ struct Rows {
   }
 };
 
+// pi: in fours of fp32 (FOURS) or eights of bf16, see above.
+template <bool FOURS>
+__device__ __forceinline__ int pi(int m) {
+  const int g = m >> 2, r = m & 3;
+  return FOURS ? g + 4 * r : 2 * g + (r & 1) + 8 * (r >> 1);
+}
+// A lane's 16 entries of the 64 from d0 of the token at its offset: rows 4 g + r
+// of tile i at w's element 4 r + i.
+template <bool FOURS, Kind K, int W>
+__device__ __forceinline__ void load_entries(const Rows<K>& x, int token, int d0, int g, uint32_t (&w)[W]) {
+  constexpr int kRun = FOURS ? 4 : 8;   // entries side by side
+#pragma unroll
+  for (int c = 0; c < 16 / kRun; ++c) {
+    const uint32_t o = x.lane(token, d0 + kRun * g + 4 * kRun * c);
+    if constexpr (K == kBf16) {
+      uint32_t h[kRun / 2];
+      load_f32<kRun / 2>(x.r, o, h);
+#pragma unroll
+      for (int i = 0; i < kRun / 2; ++i) w[kRun / 2 * c + i] = h[i];
+    } else {
+      uint32_t h[kRun];
+      if (x.f32()) {
+        load_f32<kRun>(x.r, o, h);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) w[kRun * c + i] = h[i];
+      } else if constexpr (K == kEither) {
+        load_f32<kRun / 2>(x.r, o, reinterpret_cast<uint32_t(&)[kRun / 2]>(h));
+#pragma unroll
+        for (int i = 0; i < kRun / 2; ++i) w[kRun / 2 * c + i] = h[i];
+      }
+    }
+  }
+}
+
 // Dwords that N elements of a kind take in registers.
 template <Kind K, int N>
 constexpr int kDwords = K == kBf16 && N > 1 ? N / 2 : N;
@@ -229,17 +265,18 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
   constexpr int kX = DK / 64;        // 64s of Dk
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
+  constexpr bool kFours = KQ == kF32 && KK == kF32;
   constexpr int kOwn = kT / 2;       // token tiles that a wave finishes
   constexpr int kPer = 8 / kT;       // waves per tile of keys
   constexpr bool kEarly = STATE || KV == kBf16;   // registers hold the next rows from the start of a chunk
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
   constexpr int NV = KV == kBf16 ? 1 : STATE ? NKT : MODE;
   __shared__ v4i q_lds[STATE ? 1 : kT * kX * 2 * NQ][kWave];   // [token tile][64s][h][part]
-  __shared__ v4i k_lds[kX * 4 * kS * NKT][kWave];              // [64s][i][token step][part]
+  __shared__ v4i k_lds[STATE ? 2 : 1][kX * 4 * kS * NKT][kWave];   // [in turn][64s][i][token step][part]
   __shared__ v4i p_lds[STATE ? 1 : kT * kS * MODE][kWave];     // [token tile][token step][part]
   __shared__ v4f o_lds[STATE ? 1 : 8 * kOwn * ET][kWave];      // [receiving wave][own tile][f]
   __shared__ float pw[C + 1];                                  // l^i
-  __shared__ int s_bad;
+  __shared__ int s_bad[2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = wave >> 2, ew = wave & 3;
@@ -265,7 +302,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
     }
     pw[threadIdx.x] = static_cast<float>(y);
   }
-  if (threadIdx.x == 0) s_bad = 0;
+  if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
 
   const int64_t begin = static_cast<int64_t>(seg) * p.seg_tokens;
   const int64_t end = begin + p.seg_tokens < p.T ? begin + p.seg_tokens : p.T;
@@ -300,14 +337,14 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
 #pragma unroll
       for (int j = 0; j < 8; ++j) rv.template load<ET>(vo, 32 * c + 16 * (j / 4) + j % 4, wv[c][j]);
     if (has_k) {
-      const uint32_t ko = rk.lane(32 * kc + 16 * kj + 4 * g, 64 * kx + 4 * n);
+      const uint32_t ko = rk.lane(32 * kc + 16 * kj + 4 * g, 64 * kx + 4 * pi<kFours>(n));
 #pragma unroll
       for (int r = 0; r < 4; ++r) rk.template load<4>(ko, r, wk[r]);
     }
     if constexpr (!STATE) {
       if (has_q) {
         rq.at(p.q, row, tc, h, p.Dk, p.rev);
-        rq.template load<16>(rq.lane(16 * qt + n, 64 * qx + 16 * g), 0, wq);
+        load_entries<kFours>(rq, 16 * qt + n, 64 * qx, g, wq);
       }
     }
   };
@@ -316,7 +353,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
       if (has_p) {
         rk.at(p.k, first_row(i0, tc), tc, h, p.Dk, p.rev);
 #pragma unroll
-        for (int x = 0; x < kX; ++x) rk.template load<16>(rk.lane(16 * ps + n, 64 * x + 16 * g), 0, wn[x]);
+        for (int x = 0; x < kX; ++x) load_entries<kFours>(rk, 16 * ps + n, 64 * x, g, wn[x]);
       }
     }
   };
@@ -335,7 +372,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float v = 0.0f;
-          const int d = 64 * x + 16 * g + 4 * r + 2 * half + i, e = e0 + f;
+          const int d = 64 * x + 4 * pi<kFours>(4 * g + r) + 2 * half + i, e = e0 + f;
           if (!STATE && eon && d < p.Dk) {
             if (p.joined != nullptr) {
               v = p.joined[((static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk + d) * p.Dv + e];
@@ -364,12 +401,12 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
     }
   }
 
-  for (int64_t i0 = begin; i0 < end;) {
-    const int tc = tokens_at(i0);
+  // --- a chunk's rows, as loaded, into operands: values in registers, keys and
+  // queries in LDS
+  v4i vf[kS][ET][NV];
+  const auto stage = [&](int64_t i0, int tc, int flag) {
     const bool last = i0 + tc == p.T && !p.rev;  // the state behind the last token itself
-
-    // --- values of the wave's columns, and whether they are all finite
-    v4i vf[kS][ET][NV];
+    // values of the wave's columns, and whether they are all finite
     uint32_t bad = 0;
 #pragma unroll
     for (int c = 0; c < kS; ++c) {
@@ -380,10 +417,9 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         for (int j = 0; j < 8; ++j) look<ET>(wv[c][j], rv.f32(), bad);
       }
     }
-    if (!STATE && __any(not_finite(bad)) && lane == 0) s_bad = 1;
-
-    // --- weighted transposed keys: decays to the next chunk's first token, or
-    // to the last one
+    if (!STATE && __any(not_finite(bad)) && lane == 0) s_bad[flag] = 1;
+    // weighted transposed keys: decays to the next chunk's first token, or to
+    // the last one
     if (has_k) {
       float wt[4];
 #pragma unroll
@@ -399,7 +435,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
 #pragma unroll
         for (int k = 0; k < NKT; ++k) {
           const uint2 u = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-          reinterpret_cast<uint2*>(&k_lds[((kx * 4 + i) * kS + kc) * NKT + k][lane])[kj] = u;
+          reinterpret_cast<uint2*>(&k_lds[STATE ? flag : 0][((kx * 4 + i) * kS + kc) * NKT + k][lane])[kj] = u;
           y[0] -= bf16_lo(u.x);
           y[1] -= bf16_hi(u.x);
           y[2] -= bf16_lo(u.y);
@@ -418,18 +454,38 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         }
       }
     }
-    const int64_t next = i0 + tc;
-    if (kEarly && next < end) load_most(next, tokens_at(next));
-    lds_barrier();
+  };
+  // the rows of the chunk at i0, where there is one
+  const auto load = [&](int64_t i0) {
+    if (i0 < end) load_most(i0, tokens_at(i0));
+  };
 
+  // Two barriers per chunk: the products of staged operands lie between them
+  // (keys x queries, queries x state, the state's update), what follows from
+  // other waves' products (products x values) and the next chunk's staging
+  // behind them.  Whether a chunk's values are finite is told in two flags in
+  // turn: one is cleared while the other is read.
+  int64_t i0 = begin;
+  int tc = tokens_at(i0), flag = 0;
+  stage(i0, tc, flag);
+  for (;;) {
+    const int64_t next = i0 + tc;
+    if (kEarly) load(next);
+    lds_barrier();
+    const bool last = next == p.T && !p.rev;
+
+    v4f o[kOwn][ET];
     if constexpr (!STATE) {
-      if (tc > 1 && __builtin_amdgcn_readfirstlane(s_bad) != 0) {  // a value that is not finite reaches no token before it
-        single = i0 + tc;
+      const bool redo = tc > 1 && __builtin_amdgcn_readfirstlane(s_bad[flag]) != 0;
+      if (threadIdx.x == 0) s_bad[flag ^ 1] = 0;
+      if (redo) {  // a value that is not finite reaches no token before it
+        single = next;
+        lds_barrier();
+        tc = 1;
+        flag ^= 1;
         load_most(i0, 1);
         load_keys(i0, 1);
-        lds_barrier();
-        if (threadIdx.x == 0) s_bad = 0;
-        lds_barrier();
+        stage(i0, 1, flag);
         continue;
       }
       const auto query = [&](int t, int x, int hh, v4i (&f)[NQ]) {
@@ -437,10 +493,11 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         for (int k = 0; k < NQ; ++k) f[k] = q_lds[((t * kX + x) * 2 + hh) * NQ + k][lane];
       };
       // --- keys x queries, decayed
+      constexpr int kU = (kT + kPer - 1) / kPer;
       if (has_p) {
-        v4f acc[(kT + kPer - 1) / kPer];
+        v4f acc[kU];
 #pragma unroll
-        for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) acc[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int u = 0; u < kU; ++u) acc[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int x = 0; x < kX; ++x)
 #pragma unroll
@@ -448,7 +505,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
             v4i kf[NK];
             operand<KK>([&](int j) { return element(wn[x], rk.f32(), 4 * (j % 4) + 2 * hh + j / 4); }, kf);
 #pragma unroll
-            for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) {
+            for (int u = 0; u < kU; ++u) {
               const int t = ps + pt + u * kPer;
               if (t >= kT) continue;
               v4i f[NQ];
@@ -457,7 +514,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
             }
           }
 #pragma unroll
-        for (int u = 0; u < (kT + kPer - 1) / kPer; ++u) {
+        for (int u = 0; u < kU; ++u) {
           const int t = ps + pt + u * kPer;
           if (t >= kT) continue;
           float y[4];
@@ -488,7 +545,6 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
       if (kEarly && next < end) load_keys(next, tokens_at(next));
 
       // --- queries x the wave's half of the state; what other waves finish
-      v4f o[kOwn][ET];
       if (ewave) {
         v4f a[kT][ET];
 #pragma unroll
@@ -524,12 +580,34 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
           }
       }
       // the next chunk's rows, in the registers that the sums over all tiles had
-      if (!kEarly && next < end) {
-        load_most(next, tokens_at(next));
-        load_keys(next, tokens_at(next));
-      }
+      if (!kEarly) load(next);
+    }
+
+    // --- keys x values into the state
+    if (ewave) {
+      const float w = pw[last ? tc - 1 : tc];
+#pragma unroll
+      for (int x = 0; x < kX; ++x)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int f = 0; f < ET; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[x][i][f][r] *= w;
+#pragma unroll
+          for (int c = 0; c < kS; ++c) {
+            v4i k[NKT];
+#pragma unroll
+            for (int y = 0; y < NKT; ++y) k[y] = k_lds[STATE ? flag : 0][((x * 4 + 2 * half + i) * kS + c) * NKT + y][lane];
+#pragma unroll
+            for (int f = 0; f < ET; ++f) st[x][i][f] = mma<NKT>(k, vf[c][f], st[x][i][f]);
+          }
+        }
+    }
+
+    if constexpr (!STATE) {
+      if (!kEarly && next < end) load_keys(next, tokens_at(next));
       lds_barrier();
-      if (threadIdx.x == 0) s_bad = 0;
       if (ewave) {
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
@@ -577,30 +655,11 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         }
       }
     }
-
-    // --- keys x values into the state
-    if (ewave) {
-      const float w = pw[last ? tc - 1 : tc];
-#pragma unroll
-      for (int x = 0; x < kX; ++x)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-          for (int f = 0; f < ET; ++f)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) st[x][i][f][r] *= w;
-#pragma unroll
-          for (int c = 0; c < kS; ++c) {
-            v4i k[NKT];
-#pragma unroll
-            for (int y = 0; y < NKT; ++y) k[y] = k_lds[((x * 4 + 2 * half + i) * kS + c) * NKT + y][lane];
-#pragma unroll
-            for (int f = 0; f < ET; ++f) st[x][i][f] = mma<NKT>(k, vf[c][f], st[x][i][f]);
-          }
-        }
-    }
-    lds_barrier();
+    if (next >= end) break;
     i0 = next;
+    tc = tokens_at(i0);
+    flag ^= 1;
+    stage(i0, tc, flag);
   }
 
   // the segment's own sum, or the state after the last token
@@ -622,7 +681,7 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         for (int f = 0; f < ET; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int d = 64 * x + 16 * g + 4 * r + 2 * half + i;
+            const int d = 64 * x + 4 * pi<kFours>(4 * g + r) + 2 * half + i;
             if (d < p.Dk) out[d * od + (e0 + f) * oe] = st[x][i][f][r];
           }
   }
