@@ -631,7 +631,7 @@ int mmf_linattn_bwd(const void *qkv, int qkv_is_f32, const float *decay, float s
  * leaves the others of its row at -inf; a row of -inf alone, and scores of NaN
  * or +inf, give -inf.  Candidates of score -inf come last, in the same order, so
  * that n are always returned.
- * W and n: 1 to 64, V up to 2^24, n <= W V, B W ceil(V / 1024) at most 2^23
+ * W and n: 1 to 64, V up to 2^18, n <= W V, B W ceil(V / 1024) at most 2^23
  * (MMF_ERR_SHAPE).  B == 0 is a no-op.  Workspace (256-byte aligned,
  * MMF_ERR_WORKSPACE), or NULL: then allocated stream-ordered on `stream` and
  * freed there.
@@ -646,7 +646,8 @@ int mmf_beam_select(const void *logits, int logits_is_f32, const float *scores,
  * tokens so far), row (b, j) of outs[i] = row (b, parents[b][j]) of states[i].
  * states, outs and row_bytes are HOST arrays of `count` entries, read before the
  * call returns: device addresses (16-byte aligned; any where row_bytes is 0) and
- * bytes of a row (multiples of 16, B times one at most 2^33, MMF_ERR_SHAPE).
+ * bytes of a row (multiples of 16 below 2^31, B times one at most 2^33,
+ * MMF_ERR_SHAPE).
  * outs[i] may be states[i]: rows that stay where they are are then neither read
  * nor written.  No other overlap.  parents [B][W] int32 on the device (n = W
  * above); a row whose entry is not in 0 .. W-1 stays itself.  W: 1 to 64.

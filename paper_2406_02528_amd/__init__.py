@@ -934,16 +934,25 @@ def mmf_beam_select(logits: torch.Tensor, scores: torch.Tensor, done: torch.Tens
                                 _ptr(parents), _ptr(new_done), B, W, V, n, wp, wn, _stream_here(stream, here)))
 
 
+_nbytes_of = operator.attrgetter("nbytes")
+
+
 def _state_ptrs(tensors, name, rows, here):
     """Addresses and row sizes of a list of contiguous tensors of `rows` rows on the current device."""
+    try:
+        if (all(map(_T.is_contiguous, tensors)) and set(map(_T.get_device, tensors)) <= {here}
+                and set(map(len, tensors)) <= {rows}):
+            return (array.array("Q", list(map(_T.data_ptr, tensors))),
+                    array.array("q", [n // rows if rows else 0 for n in map(_nbytes_of, tensors)]))
+    except (AttributeError, TypeError, RuntimeError):
+        pass
     for i, t in enumerate(tensors):
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name}[{i}] must be a torch.Tensor")
         if t.dim() < 1 or t.shape[0] != rows:
             raise ValueError(f"{name}[{i}] must have {rows} rows, got shape {tuple(t.shape)}")
         _need_here(t, f"{name}[{i}]", t.dtype, t.shape, here)
-    return (array.array("Q", [t.data_ptr() for t in tensors]),
-            array.array("q", [t.nbytes // rows if rows else 0 for t in tensors]))
+    raise ValueError(f"{name} must be tensors on the current device")
 
 
 def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, stream=None) -> None:

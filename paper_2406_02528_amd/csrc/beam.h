@@ -9,7 +9,8 @@ namespace mmf {
 
 // The n best of W x V candidates of each of B batches; done, new_done may be
 // nullptr, end < 0: no such token.
-constexpr int kBeamMax = 64;   // beams, and candidates kept
+constexpr int kBeamMax = 64;          // beams, and candidates kept
+constexpr int kBeamMaxV = 1 << 18;    // tokens
 struct BeamSelectArgs {
   const void* logits;
   bool is_f32;

@@ -7,10 +7,16 @@
 // being read: it goes on as itself.  NaN logits count as -inf.
 //
 // Within a row the order is that of the logits, so a first kernel keeps the n
-// best logits of each piece of a row, with the piece's maximum and its sum of
-// exponentials (one pass over the logits); a second computes the scores of
-// what is left, in fp64 (scores next to each other are told apart, and a tie
-// is a tie of equal inputs), and takes the n best.
+// best logits of each piece of a row, sorted, with the piece's maximum and its
+// sum of exponentials (one pass over the logits); a second merges the lists of
+// a row (equal logits: the piece with the lower tokens first), then those of
+// the beams by their scores, in fp64 (scores next to each other are told apart,
+// and a tie is a tie of equal inputs).
+//
+// The n best of a piece: of the 64 lanes' own maxima, the n-th largest is at
+// most the piece's n-th largest logit, so only what reaches the largest such
+// bound of the four waves goes to LDS (of the logits that are equal to it, the
+// first n of each wave), where each counts those before it.
 #include "beam.h"
 #include "mmf_device.h"
 #include "row_vec.h"
@@ -20,19 +26,16 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr double kLog2e = 1.4426950408889634074;
-constexpr int kVals = 16;                      // logits per thread
-constexpr int kPiece = kThreads * kVals;       // logits per piece at most
 
-// A logit and its token, as a number whose order is theirs (higher logit, then
-// lower token); 0: none.
-__device__ __forceinline__ uint64_t key_of(float z, int token) {
+// A logit as a number whose order is its own; 0: none.
+__device__ __forceinline__ uint32_t order_of(float z) {
   const uint32_t b = __float_as_uint(z + 0.0f);  // -0 is 0
-  const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~token);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float logit_of(uint64_t key) {
-  const uint32_t o = static_cast<uint32_t>(key >> 32);
-  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+__device__ __forceinline__ float logit_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+// With its token: higher logits, then lower tokens first.
+__device__ __forceinline__ uint64_t key_of(uint32_t o, int token) {
+  return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~token);
 }
 __device__ __forceinline__ int token_of(uint64_t key) { return static_cast<int>(~static_cast<uint32_t>(key)); }
 
@@ -42,35 +45,57 @@ struct Stat {
   float pad;
 };
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
+  return static_cast<uint32_t>(dpp_i32<CTRL>(static_cast<int>(v)));
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, dpp_u32<kDppXor1>(v));
+  v = max(v, dpp_u32<kDppXor2>(v));
+  v = max(v, dpp_u32<kDppHalfMirror>(v));
+  v = max(v, dpp_u32<kDppMirror>(v));
+  const auto at = [&](int lane) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane)); };
+  return max(max(at(0), at(16)), max(at(32), at(48)));
+}
+
+// The largest x that at least n lanes' values reach.
+__device__ __forceinline__ uint32_t nth_largest(uint32_t v, int n) {
+  uint32_t x = 0;
 #pragma unroll
-  for (int x = 1; x < kWave; x *= 2) {
-    const uint64_t o = __shfl_xor(v, x);
-    v = o > v ? o : v;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t t = x | (1u << bit);
+    if (__popcll(__ballot(v >= t)) >= n) x = t;
   }
-  return v;
+  return x;
 }
 
 struct Scratch {
-  uint64_t* keys;  // [rows][pieces][n]
+  uint64_t* keys;  // [rows][pieces][n], sorted; 0: none
   Stat* stats;     // [rows][pieces]
   int pieces, piece;
 };
 
-template <typename T>
+// Candidates of a piece that LDS holds, and those that are ranked by counting.
+constexpr int list_size(int vals, int n) { return kWaves * ((n - 1) * vals + n); }
+constexpr int kCounted = 1024;
+
+template <typename T, int VALS>
 __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectArgs a, const Scratch s) {
+  extern __shared__ uint64_t s_list[];
   __shared__ float s_max[kWaves];
   __shared__ double s_sum[kWaves];
+  __shared__ uint32_t s_bound[kWaves];
   __shared__ uint64_t s_key[kWaves];
+  __shared__ int s_count;
   const int piece = blockIdx.x % s.pieces;
   const int64_t row = blockIdx.x / s.pieces;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int begin = piece * s.piece, end = min(begin + s.piece, a.V);
   const bool done = a.done != nullptr && a.done[row] != 0;
   const T* const z = static_cast<const T*>(a.logits) + row * a.V;
-  float v[kVals];
+  float v[VALS];
 #pragma unroll
-  for (int i = 0; i < kVals; ++i) {
+  for (int i = 0; i < VALS; ++i) {
     const int t = begin + i * kThreads + threadIdx.x;
     float x = -__builtin_inff();
     if (done) {
@@ -78,121 +103,187 @@ __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectAr
     } else if (t < end) {
       if constexpr (sizeof(T) == 4) x = z[t];
       else x = bf16_to_f32(z[t]);
-      if (x != x) x = -__builtin_inff();
     }
     v[i] = x;
   }
-  float m = v[0];
+  if (threadIdx.x == 0) s_count = 0;
+  float m = -__builtin_inff();
+  uint32_t o[VALS], top = 0;
 #pragma unroll
-  for (int i = 1; i < kVals; ++i) m = fmaxf(m, v[i]);
+  for (int i = 0; i < VALS; ++i) {
+    if (v[i] != v[i]) v[i] = -__builtin_inff();
+    m = fmaxf(m, v[i]);
+    o[i] = begin + i * kThreads + static_cast<int>(threadIdx.x) < end ? order_of(v[i]) : 0u;
+    top = max(top, o[i]);
+  }
   m = wave_max_f32(m);
-  if (lane == 0) s_max[wave] = m;
+  const uint32_t bound_w = nth_largest(top, a.n);
+  if (lane == 0) {
+    s_max[wave] = m;
+    s_bound[wave] = bound_w;
+  }
   __syncthreads();
   m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  const uint32_t bound = max(max(s_bound[0], s_bound[1]), max(s_bound[2], s_bound[3]));
+
+  // what reaches the bound
+  int equal = 0;  // of the wave's, so far
+#pragma unroll
+  for (int i = 0; i < VALS; ++i) {
+    const uint64_t same = __ballot(o[i] == bound && o[i] != 0);
+    const uint64_t below = same & ((uint64_t(1) << lane) - 1);
+    const bool take = o[i] > bound || (((same >> lane) & 1) != 0 && equal + __popcll(below) < a.n);
+    equal += __popcll(same);
+    const uint64_t mask = __ballot(take);
+    if (mask != 0) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s_count, __popcll(mask));  // their order in the list does not matter
+      at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((uint64_t(1) << lane) - 1));
+      if (take) s_list[at] = key_of(o[i], begin + i * kThreads + threadIdx.x);
+    }
+  }
   float e = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kVals; ++i)
+  for (int i = 0; i < VALS; ++i)
     e += v[i] == m ? 1.0f : __builtin_amdgcn_exp2f((v[i] - m) * static_cast<float>(kLog2e));
+  // what is behind the piece's end is -inf: nothing, but as many as the piece where all of it is
   const double sum = wave_sum_f64(e);
   if (lane == 0) s_sum[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) s.stats[row * s.pieces + piece] = {(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), m, 0.0f};
-  // the n best, one after the other
-  uint64_t last = ~uint64_t(0);
+  const int count = s_count;
+  uint64_t* const out = s.keys + (row * s.pieces + piece) * a.n;
+  if (count <= kCounted) {
+    for (int j = threadIdx.x; j < count; j += kThreads) {
+      const uint64_t k = s_list[j];
+      int before = 0;
+      for (int i = 0; i < count; ++i) before += s_list[i] > k;
+      if (before < a.n) out[before] = k;
+    }
+    if (threadIdx.x < a.n && static_cast<int>(threadIdx.x) >= count) out[threadIdx.x] = 0;
+    return;
+  }
+  uint64_t last = ~uint64_t(0);  // many: one after the other
   for (int j = 0; j < a.n; ++j) {
     uint64_t best = 0;
-#pragma unroll
-    for (int i = 0; i < kVals; ++i) {
-      const int t = begin + i * kThreads + threadIdx.x;
-      const uint64_t k = t < end ? key_of(v[i], t) : 0;
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+      const uint64_t k = s_list[i];
       if (k < last && k > best) best = k;
     }
-    best = wave_max(best);
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) {
+      const uint64_t k = __shfl_xor(best, x);
+      best = k > best ? k : best;
+    }
     if (lane == 0) s_key[wave] = best;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) best = s_key[w] > best ? s_key[w] : best;
-    if (threadIdx.x == 0) s.keys[(row * s.pieces + piece) * a.n + j] = best;
+    if (threadIdx.x == 0) out[j] = best;
     last = best;
     __syncthreads();
   }
 }
 
-struct Candidate {
-  double score;
-  uint64_t key;
-  int beam;      // -1: none
-};
-__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {
-  if (b.beam < 0) return a.beam >= 0;
-  if (a.beam < 0) return false;
-  if (a.score != b.score) return a.score > b.score;
-  if (a.beam != b.beam) return a.beam < b.beam;
-  return a.key > b.key;
+// A score as a number whose order is its own.
+__device__ __forceinline__ uint64_t order_of(double s) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, s + 0.0);
+  return b >> 63 ? ~b : b | (uint64_t(1) << 63);
 }
 
-__global__ __launch_bounds__(kThreads) void beam_final_kernel(const BeamSelectArgs a, const Scratch s) {
-  __shared__ double s_score[kBeamMax];   // of each beam
-  __shared__ double s_log[kBeamMax];     // ln of its sum of exponentials
+constexpr int kFinalWaves = 16;
+constexpr int kStaged = 6144;   // keys of a batch's lists that LDS holds
+constexpr int kRanked = 512;    // candidates of a batch that are ranked by counting
+
+// A wave merges the lists of a row (a lane per piece); the beams' are then ranked
+// by counting, or, of many, merged by wave 0 (a lane per beam).
+__global__ __launch_bounds__(kFinalWaves* kWave) void beam_final_kernel(const BeamSelectArgs a, const Scratch s, bool staged) {
+  extern __shared__ uint64_t s_dyn[];           // [W][n] merged; the lists where they are staged, then [W][n] scores
+  __shared__ double s_score[kBeamMax];          // of each beam
+  __shared__ double s_log[kBeamMax];            // ln of its sum of exponentials
   __shared__ float s_max[kBeamMax];
-  __shared__ Candidate s_best[kWaves];
   const int64_t b = blockIdx.x;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (threadIdx.x < a.W) {
-    const Stat* const st = s.stats + (b * a.W + threadIdx.x) * s.pieces;
-    float m = -__builtin_inff();
-    for (int p = 0; p < s.pieces; ++p) m = fmaxf(m, st[p].max);
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int per = s.pieces * a.n;
+  const uint64_t* lists = s.keys + b * a.W * per;
+  if (staged) {
+    uint64_t* const l = s_dyn + a.W * a.n;
+    for (int i = threadIdx.x; i < a.W * per; i += blockDim.x) l[i] = lists[i];
+    lists = l;
+  }
+  for (int w = wave; w < a.W; w += waves) {
+    Stat st{0.0, -__builtin_inff(), 0.0f};
+    if (lane < s.pieces) st = s.stats[(b * a.W + w) * s.pieces + lane];
+    const float m = wave_max_f32(st.max);
     double sum = 0.0;
-    for (int p = 0; p < s.pieces; ++p) sum += st[p].max == m ? st[p].sum : st[p].sum * exp(static_cast<double>(st[p].max) - m);
-    const float c = a.scores[b * a.W + threadIdx.x];
-    // scores that are no number, and rows in which no token is possible
-    const bool none = !(c < __builtin_inff()) || m == -__builtin_inff();
-    s_score[threadIdx.x] = none ? -__builtin_inf() : static_cast<double>(c);
-    s_log[threadIdx.x] = none ? 0.0 : log(sum);
-    s_max[threadIdx.x] = m;
+    if (lane < s.pieces) sum = st.max == m ? st.sum : st.sum * exp(static_cast<double>(st.max) - m);
+    sum = wave_sum_f64(sum);
+    if (lane == 0) {
+      const float c = a.scores[b * a.W + w];
+      // scores that are no number, and rows in which no token is possible
+      const bool none = !(c < __builtin_inff()) || m == -__builtin_inff();
+      s_score[w] = none ? -__builtin_inf() : static_cast<double>(c);
+      s_log[w] = none ? 0.0 : log(sum);
+      s_max[w] = m;
+    }
   }
   __syncthreads();
-  const int per = s.pieces * a.n, total = a.W * per;
-  const uint64_t* const keys = s.keys + b * total;
-  const auto candidate = [&](int i) {
-    Candidate c{0.0, keys[i], i / per};
-    if (c.key == 0) {
-      c.beam = -1;
-    } else {
-      const float z = logit_of(c.key), m = s_max[c.beam];
-      const double d = z == m ? 0.0 : static_cast<double>(z) - m;
-      c.score = s_score[c.beam] + (d - s_log[c.beam]);
+  for (int w = wave; w < a.W; w += waves) {
+    const uint64_t* const l = lists + w * per + lane * a.n;
+    int at = 0;
+    uint64_t head = lane < s.pieces ? l[0] : 0;
+    for (int j = 0; j < a.n; ++j) {
+      const uint32_t o = static_cast<uint32_t>(head >> 32), best = wave_max_u32(o);
+      const int from = __ffsll(__ballot(o == best)) - 1;  // of equal logits the lowest tokens
+      if (lane == from) {
+        s_dyn[w * a.n + j] = head;
+        ++at;
+        head = head != 0 && at < a.n ? l[at] : 0;
+      }
     }
-    return c;
+  }
+  __syncthreads();
+  // --- the scores, and the n best of them
+  uint64_t* const order = s_dyn + a.W * a.n;   // in place of the lists
+  const int all = a.W * a.n;
+  const auto score_of = [&](uint64_t key, int w) {
+    const float z = logit_of(static_cast<uint32_t>(key >> 32)), m = s_max[w];
+    const double d = z == m ? 0.0 : static_cast<double>(z) - m;
+    return s_score[w] + (d - s_log[w]);
   };
-  Candidate last{__builtin_inf(), ~uint64_t(0), 0};
+  const auto put = [&](int j, uint64_t key, int w, double score) {
+    const int64_t out = b * a.n + j;
+    const int token = token_of(key);
+    a.new_scores[out] = static_cast<float>(score);
+    a.tokens[out] = token;
+    a.parents[out] = w;
+    if (a.new_done != nullptr) a.new_done[out] = token == a.end || (a.done != nullptr && a.done[b * a.W + w] != 0);
+  };
+  for (int i = threadIdx.x; i < all; i += blockDim.x) order[i] = s_dyn[i] != 0 ? order_of(score_of(s_dyn[i], i / a.n)) : 0;
+  __syncthreads();
+  if (all <= kRanked) {  // each counts those before it: higher scores, and equal ones of lower beams or places
+    for (int i = threadIdx.x; i < all; i += blockDim.x) {
+      const uint64_t o = order[i];
+      int before = 0;
+      for (int k = 0; k < all; ++k) before += order[k] > o || (order[k] == o && k < i);
+      if (before < a.n) put(before, s_dyn[i], i / a.n, score_of(s_dyn[i], i / a.n));
+    }
+    return;
+  }
+  if (wave != 0) return;
+  int at = 0;
+  uint64_t o = lane < a.W ? order[lane * a.n] : 0;
   for (int j = 0; j < a.n; ++j) {
-    Candidate best{0.0, 0, -1};
-    for (int i = threadIdx.x; i < total; i += kThreads) {
-      const Candidate c = candidate(i);
-      if (before(last, c) && before(c, best)) best = c;
+    const uint32_t hi = static_cast<uint32_t>(o >> 32), best_hi = wave_max_u32(hi);
+    const uint32_t lo = hi == best_hi ? static_cast<uint32_t>(o) : 0u, best_lo = wave_max_u32(lo);
+    const int from = __ffsll(__ballot(hi == best_hi && lo == best_lo)) - 1;  // of equal scores the lowest beam
+    if (lane == from) {
+      const uint64_t key = s_dyn[lane * a.n + at];
+      put(j, key, lane, score_of(key, lane));
+      ++at;
+      o = at < a.n ? order[lane * a.n + at] : 0;
     }
-#pragma unroll
-    for (int x = 1; x < kWave; x *= 2) {
-      const Candidate o{__shfl_xor(best.score, x), __shfl_xor(best.key, x), __shfl_xor(best.beam, x)};
-      if (before(o, best)) best = o;
-    }
-    if (lane == 0) s_best[wave] = best;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      if (before(s_best[w], best)) best = s_best[w];
-    if (threadIdx.x == 0) {
-      const int64_t at = b * a.n + j;
-      const int token = token_of(best.key);
-      a.new_scores[at] = static_cast<float>(best.score);
-      a.tokens[at] = token;
-      a.parents[at] = best.beam;
-      if (a.new_done != nullptr)
-        a.new_done[at] = token == a.end || (a.done != nullptr && a.done[b * a.W + best.beam] != 0);
-    }
-    last = best;
-    __syncthreads();
   }
 }
 
@@ -210,7 +301,10 @@ struct Set {
   int n;
 };
 
-template <typename U, int MAXW>
+// Every row goes through a buffer resource of its own, of size 0 where it stays:
+// no branch, so all loads are in flight at once (branches for every row made
+// the compiler lay out a path for every set of rows, in 242 registers).
+template <int WORDS, int MAXW, bool NT>
 __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(const Set s, const int32_t* __restrict__ parents, int W) {
   int lo = 0, hi = s.n - 1;  // the last array whose first workgroup is at most this one
   while (lo < hi) {
@@ -220,55 +314,88 @@ __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(const Set s, con
   }
   const uint32_t blk = blockIdx.x - s.first[lo];
   const int64_t b = blk / s.cols[lo];
-  const int64_t col = (static_cast<int64_t>(blk % s.cols[lo]) * kThreads + threadIdx.x) * sizeof(U);
+  const uint32_t col = ((blk % s.cols[lo]) * kThreads + threadIdx.x) * (4u * WORDS);
   const int64_t row = s.row[lo];
-  if (col >= row) return;
-  const char* const src = s.src[lo] + b * W * row + col;
-  char* const dst = s.dst[lo] + b * W * row + col;
+  const char* const src = s.src[lo] + b * W * row;
+  char* const dst = s.dst[lo] + b * W * row;
   const bool moved = src != dst;
   const int32_t* const p = parents + b * W;
-  U v[MAXW];
+  constexpr int kPolicy = NT ? kNontemporal : 0;
+  typedef unsigned int vec __attribute__((ext_vector_type(WORDS == 4 ? 4 : 2)));
+  vec v[MAXW];
+  const auto from = [&](int j) {
+    const int f = j < W ? __builtin_amdgcn_readfirstlane(p[j]) : j;
+    return f < 0 || f >= W ? j : f;
+  };
+  const auto rsrc = [&](const char* base, int j, int f) {
+    const bool on = j < W && (f != j || moved);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, on ? static_cast<int>(row) : 0, kBufferWord3);
+  };
 #pragma unroll
   for (int j = 0; j < MAXW; ++j) {
-    if (j >= W) break;
-    int from = p[j];
-    if (from < 0 || from >= W) from = j;
-    if (from != j || moved) v[j] = *reinterpret_cast<const U*>(src + from * row);
+    const int f = from(j);
+    const auto r = rsrc(src + f * row, j, f);
+    if constexpr (WORDS == 4) v[j] = __builtin_amdgcn_raw_buffer_load_b128(r, col, 0, kPolicy);
+    else v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(r, col, 0, kPolicy);
   }
 #pragma unroll
   for (int j = 0; j < MAXW; ++j) {
-    if (j >= W) break;
-    const int from = p[j];
-    if ((from != j && from >= 0 && from < W) || moved) *reinterpret_cast<U*>(dst + j * row) = v[j];
+    const auto r = rsrc(dst + j * row, j, from(j));
+    if constexpr (WORDS == 4) __builtin_amdgcn_raw_buffer_store_b128(v[j], r, col, 0, kPolicy);
+    else __builtin_amdgcn_raw_buffer_store_b32(v[j][0], r, col, 0, kPolicy);
   }
 }
 
-int pieces_of(int V) { return (V + kPiece - 1) / kPiece; }
+// Logits per thread: few where there are few rows, as long as a wave holds a
+// row's pieces.
+constexpr int kMaxPieces = kWave;
+int vals_of(int64_t rows, int V) {
+  const int64_t small = (V + 4 * kThreads - 1) / (4 * kThreads);
+  return small <= kMaxPieces && rows * small <= 4096 ? 4 : 16;
+}
+int pieces_of(int64_t rows, int V) {
+  const int piece = vals_of(rows, V) * kThreads;
+  return (V + piece - 1) / piece;
+}
+static_assert(kBeamMaxV <= kMaxPieces * 16 * kThreads, "a lane per piece");
 
 }  // namespace
 
 size_t beam_select_bytes(int64_t B, int W, int V, int n) {
-  const int64_t pieces = B * W * pieces_of(V);
+  const int64_t pieces = B * W * pieces_of(B * W, V);
   return static_cast<size_t>(pieces) * (sizeof(Stat) + sizeof(uint64_t) * n);
 }
 
 hipError_t launch_beam_select(const BeamSelectArgs& a, void* scratch, hipStream_t stream) {
+  const int64_t rows = a.B * a.W;
+  const int vals = vals_of(rows, a.V);
   Scratch s;
-  s.pieces = pieces_of(a.V);
+  s.pieces = pieces_of(rows, a.V);
   s.piece = (a.V + s.pieces - 1) / s.pieces;
   s.stats = static_cast<Stat*>(scratch);
-  s.keys = reinterpret_cast<uint64_t*>(s.stats + a.B * a.W * s.pieces);
-  const dim3 grid(static_cast<uint32_t>(a.B * a.W * s.pieces));
-  if (a.is_f32) hipLaunchKernelGGL(beam_piece_kernel<float>, grid, dim3(kThreads), 0, stream, a, s);
-  else hipLaunchKernelGGL(beam_piece_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, a, s);
-  if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL(beam_final_kernel, dim3(static_cast<uint32_t>(a.B)), dim3(kThreads), 0, stream, a, s);
+  s.keys = reinterpret_cast<uint64_t*>(s.stats + rows * s.pieces);
+  const auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(rows * s.pieces)), dim3(kThreads),
+                       list_size(vals, a.n) * sizeof(uint64_t), stream, a, s);
+    return hipGetLastError();
+  };
+  const hipError_t e = a.is_f32 ? vals == 4 ? go(beam_piece_kernel<float, 4>) : go(beam_piece_kernel<float, 16>)
+                       : vals == 4 ? go(beam_piece_kernel<uint16_t, 4>) : go(beam_piece_kernel<uint16_t, 16>);
+  if (e != hipSuccess) return e;
+  const int total = a.W * s.pieces * a.n;
+  const bool staged = total <= kStaged;
+  hipLaunchKernelGGL(beam_final_kernel, dim3(static_cast<uint32_t>(a.B)),
+                     dim3(kWave * (a.W < kFinalWaves ? a.W : kFinalWaves)),
+                     (a.W * a.n + (staged && s.pieces > 1 ? total : a.W * a.n)) * sizeof(uint64_t), stream, a, s, staged);
   return hipGetLastError();
 }
 
 hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t stream) {
   const int unit = a.W <= 16 ? 16 : 4;
   const int64_t most = int64_t(1) << 23;  // workgroups per launch
+  int64_t bytes = 0;
+  for (int64_t i = 0; i < a.count; ++i) bytes += a.row_bytes[i] * a.B * a.W;
+  const bool nt = bytes >= kLastLevelBytes;
   int64_t done = 0;
   while (done < a.count) {
     Set s{};
@@ -290,10 +417,10 @@ hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t stream) {
       hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(groups)), dim3(kThreads), 0, stream, s, a.parents, a.W);
       return hipGetLastError();
     };
-    const hipError_t e = a.W <= 4    ? go(beam_reorder_kernel<uint4, 4>)
-                         : a.W <= 8  ? go(beam_reorder_kernel<uint4, 8>)
-                         : a.W <= 16 ? go(beam_reorder_kernel<uint4, 16>)
-                                     : go(beam_reorder_kernel<uint32_t, 64>);
+    const hipError_t e = a.W <= 4    ? nt ? go(beam_reorder_kernel<4, 4, true>) : go(beam_reorder_kernel<4, 4, false>)
+                         : a.W <= 8  ? nt ? go(beam_reorder_kernel<4, 8, true>) : go(beam_reorder_kernel<4, 8, false>)
+                         : a.W <= 16 ? go(beam_reorder_kernel<4, 16, false>)
+                                     : go(beam_reorder_kernel<1, 64, false>);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -338,7 +338,7 @@ size_t linattn_fwd_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv
 // ---- beam search ----
 // Rows of logits and workgroups of a launch stay below 2^23.
 int check_beam(int64_t B, int64_t W, int64_t V, int64_t n) {
-  if (B < 0 || W < 1 || W > mmf::kBeamMax || V < 1 || V > int64_t(1) << 24 || n < 1 || n > mmf::kBeamMax || n > W * V)
+  if (B < 0 || W < 1 || W > mmf::kBeamMax || V < 1 || V > mmf::kBeamMaxV || n < 1 || n > mmf::kBeamMax || n > W * V)
     return MMF_ERR_SHAPE;
   if (B * W > (int64_t(1) << 23) || B * W * ((V + 1023) / 1024) > (int64_t(1) << 23)) return MMF_ERR_SHAPE;
   return MMF_OK;
@@ -1329,7 +1329,7 @@ int mmf_beam_reorder(const void* const* states, void* const* outs, const int64_t
   if (count > 0 && (!states || !outs || !row_bytes)) return MMF_ERR_NULL;
   const int64_t most = (int64_t(1) << 33) / (B > 0 ? B : 1);  // a launch's workgroups of 256 columns of 4 bytes
   for (int64_t i = 0; i < count; ++i)
-    if (row_bytes[i] < 0 || row_bytes[i] % 16 != 0 || row_bytes[i] > most) return MMF_ERR_SHAPE;
+    if (row_bytes[i] < 0 || row_bytes[i] % 16 != 0 || row_bytes[i] > most || row_bytes[i] > kMaxMN) return MMF_ERR_SHAPE;
   if (count == 0 || B == 0) return MMF_OK;
   if (!parents) return MMF_ERR_NULL;
   if (!aligned16(parents)) return MMF_ERR_ALIGN;
