@@ -22,6 +22,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import itertools
 import operator
 import os
 
@@ -941,7 +942,7 @@ def _state_ptrs(tensors, name, rows, here):
     """Addresses and row sizes of a list of contiguous tensors of `rows` rows on the current device."""
     try:
         if (all(map(_T.is_contiguous, tensors)) and set(map(_T.get_device, tensors)) <= {here}
-                and set(map(len, tensors)) <= {rows}):
+                and set(map(_T.size, tensors, itertools.repeat(0))) <= {rows}):
             return (array.array("Q", list(map(_T.data_ptr, tensors))),
                     array.array("q", [n // rows if rows else 0 for n in map(_nbytes_of, tensors)]))
     except (AttributeError, TypeError, RuntimeError):

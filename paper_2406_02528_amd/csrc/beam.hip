@@ -58,11 +58,13 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return max(max(at(0), at(16)), max(at(32), at(48)));
 }
 
-// The largest x that at least n lanes' values reach.
+// The largest x that at least n lanes' values reach; LOW: the lowest bit in
+// which values differ (all below it are those of a bf16 logit's order).
+template <int LOW>
 __device__ __forceinline__ uint32_t nth_largest(uint32_t v, int n) {
   uint32_t x = 0;
 #pragma unroll
-  for (int bit = 31; bit >= 0; --bit) {
+  for (int bit = 31; bit >= LOW; --bit) {
     const uint32_t t = x | (1u << bit);
     if (__popcll(__ballot(v >= t)) >= n) x = t;
   }
@@ -92,60 +94,70 @@ __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectAr
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int begin = piece * s.piece, end = min(begin + s.piece, a.V);
   const bool done = a.done != nullptr && a.done[row] != 0;
-  const T* const z = static_cast<const T*>(a.logits) + row * a.V;
-  float v[VALS];
+  // no branches: all loads in flight at once (a done row's read nothing)
+  const auto z = row_rsrc(static_cast<const T*>(a.logits) + row * a.V + begin, end - begin, !done);
+  uint32_t w[VALS];
+#pragma unroll
+  for (int i = 0; i < VALS; ++i) {
+    const uint32_t at = (i * kThreads + threadIdx.x) * sizeof(T);
+    if constexpr (sizeof(T) == 4) w[i] = __builtin_amdgcn_raw_buffer_load_b32(z, at, 0, 0);
+    else w[i] = static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(z, at, 0, 0)) << 16;
+  }
+  float v[VALS];   // NaN, and what is behind the piece's end, as -inf
 #pragma unroll
   for (int i = 0; i < VALS; ++i) {
     const int t = begin + i * kThreads + threadIdx.x;
-    float x = -__builtin_inff();
-    if (done) {
-      if (t == a.end) x = 0.0f;
-    } else if (t < end) {
-      if constexpr (sizeof(T) == 4) x = z[t];
-      else x = bf16_to_f32(z[t]);
-    }
-    v[i] = x;
+    v[i] = t < end && !done ? __uint_as_float(w[i]) : -__builtin_inff();
+    if (done && t == a.end) v[i] = 0.0f;
   }
   if (threadIdx.x == 0) s_count = 0;
   float m = -__builtin_inff();
-  uint32_t o[VALS], top = 0;
 #pragma unroll
   for (int i = 0; i < VALS; ++i) {
-    if (v[i] != v[i]) v[i] = -__builtin_inff();
+    v[i] = fmaxf(v[i], -__builtin_inff());
     m = fmaxf(m, v[i]);
-    o[i] = begin + i * kThreads + static_cast<int>(threadIdx.x) < end ? order_of(v[i]) : 0u;
-    top = max(top, o[i]);
   }
+  // the lane's largest, where it has a logit at all.  A bf16 logit differs from
+  // the others in the upper half only: the lower is 0, or of negative ones all ones
+  const uint32_t top = begin + static_cast<int>(threadIdx.x) < end ? order_of(m) : 0u;
   m = wave_max_f32(m);
-  const uint32_t bound_w = nth_largest(top, a.n);
+  uint32_t bound_w = nth_largest<sizeof(T) == 4 ? 0 : 16>(top, a.n);
+  if (sizeof(T) == 2 && bound_w != 0 && (bound_w >> 31) == 0) bound_w |= 0xFFFFu;
   if (lane == 0) {
     s_max[wave] = m;
     s_bound[wave] = bound_w;
   }
   __syncthreads();
   m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const uint32_t bound = max(max(s_bound[0], s_bound[1]), max(s_bound[2], s_bound[3]));
+  const uint32_t bound_o = max(max(s_bound[0], s_bound[1]), max(s_bound[2], s_bound[3]));
+  const float bound = bound_o != 0 ? logit_of(bound_o) : -__builtin_inff();
 
-  // what reaches the bound
+  // what reaches the bound; all of a piece that no wave has n lanes of
   int equal = 0;  // of the wave's, so far
 #pragma unroll
   for (int i = 0; i < VALS; ++i) {
-    const uint64_t same = __ballot(o[i] == bound && o[i] != 0);
+    if (__ballot(v[i] >= bound) == 0) continue;
+    const int t = begin + i * kThreads + threadIdx.x;
+    const uint64_t same = __ballot(v[i] == bound && t < end);
     const uint64_t below = same & ((uint64_t(1) << lane) - 1);
-    const bool take = o[i] > bound || (((same >> lane) & 1) != 0 && equal + __popcll(below) < a.n);
+    const bool take = t < end && (v[i] > bound || (((same >> lane) & 1) != 0 && equal + __popcll(below) < a.n));
     equal += __popcll(same);
     const uint64_t mask = __ballot(take);
     if (mask != 0) {
       int at = 0;
       if (lane == 0) at = atomicAdd(&s_count, __popcll(mask));  // their order in the list does not matter
       at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((uint64_t(1) << lane) - 1));
-      if (take) s_list[at] = key_of(o[i], begin + i * kThreads + threadIdx.x);
+      if (take) s_list[at] = key_of(order_of(v[i]), t);
     }
   }
   float e = 0.0f;
+  if (__builtin_fabsf(m) < __builtin_inff()) {
 #pragma unroll
-  for (int i = 0; i < VALS; ++i)
-    e += v[i] == m ? 1.0f : __builtin_amdgcn_exp2f((v[i] - m) * static_cast<float>(kLog2e));
+    for (int i = 0; i < VALS; ++i) e += __builtin_amdgcn_exp2f((v[i] - m) * static_cast<float>(kLog2e));
+  } else {
+#pragma unroll
+    for (int i = 0; i < VALS; ++i) e += v[i] == m ? 1.0f : 0.0f;
+  }
   // what is behind the piece's end is -inf: nothing, but as many as the piece where all of it is
   const double sum = wave_sum_f64(e);
   if (lane == 0) s_sum[wave] = sum;
@@ -351,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(const Set s, con
 constexpr int kMaxPieces = kWave;
 int vals_of(int64_t rows, int V) {
   const int64_t small = (V + 4 * kThreads - 1) / (4 * kThreads);
-  return small <= kMaxPieces && rows * small <= 4096 ? 4 : 16;
+  return small <= kMaxPieces && rows * small <= 512 ? 4 : 16;
 }
 int pieces_of(int64_t rows, int V) {
   const int piece = vals_of(rows, V) * kThreads;
