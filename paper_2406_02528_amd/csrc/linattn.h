@@ -27,8 +27,7 @@ hipError_t launch_linattn_step(const LinattnArgs& a, hipStream_t stream);
 
 // A pass over chunks (linattn_chunk.h).  Operands: the first row of a segment
 // of the stacked rows, `ld` elements from one row to the next, head h at h
-// times its width.  The state s_in, s_out (nullptr: 0, not stored) has strides
-// in_d and in_e within a head's Dk Dv entries.
+// times its width.
 struct LinattnOperand {
   const void* p;
   int64_t ld;
@@ -41,28 +40,30 @@ struct LinattnPass {
   const float* decay;
   float alpha, beta;
   bool rev;
-  const float* s_in;
+  // the state that enters segment `seg` of state bh: entry (d, e) at e_in[bh
+  // e_bh + seg e_seg + d e_d + e e_e] (nullptr: 0), times the decay if e_decay
+  const float* e_in;
+  int64_t e_bh, e_seg;
+  int e_d, e_e;
+  bool e_decay;
+  // the state behind the last token (nullptr: not stored); of a pass for
+  // states alone the segments' own sums [B H][nseg][Dk][Dv], those of segments
+  // below `segs`
   float* s_out;
-  int64_t in_d, in_e;
+  uint32_t segs;
   uint32_t B, H;
   int64_t T;
   int Dk, Dv;
-  // from linattn_plan
-  uint32_t nseg, tiles;
-  int et;
+  uint32_t nseg, tiles;   // segments; workgroups per state
+  int waves;              // of a workgroup, 16 columns each
   int64_t seg_tokens;
-  float* joined;   // [B H][nseg][Dk][Dv]; nullptr: one segment, from s_in
-  bool join_last;  // the joining gives s_out (the last segment's own sum too)
 };
-// How a pass is cut: columns of the state per workgroup (64 et) and tokens per
-// segment.
-struct LinattnPlan {
-  uint32_t nseg, tiles;
-  int et;
-  int64_t seg_tokens;
-  size_t joined_bytes;
+// Up to three passes of one kernel in a launch, one after the other in its
+// workgroups.
+struct LinattnPasses {
+  LinattnPass p[3];
+  uint32_t first[3];
 };
-LinattnPlan linattn_plan(int64_t B, int64_t T, int64_t H, int Dk, int Dv);
 size_t linattn_chunk_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv);
 hipError_t launch_linattn_chunk(const LinattnArgs& a, float* joined, hipStream_t stream);
 // Backward: dqkv bf16; s0, ds_last, ds0 may be nullptr, ds0 may be ds_last.

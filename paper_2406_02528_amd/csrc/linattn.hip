@@ -1,20 +1,22 @@
-// Linear attention over chunks: how a pass is cut into segments, the joining
-// of the segments' states, and the passes of the forward.
+// Linear attention over chunks: how the passes are cut into segments, the
+// joining of the segments' states, and the passes of both directions.
 #include "linattn.h"
 #include "mmf_device.h"
 
 namespace mmf {
 
-hipError_t launch_linattn_f32(const LinattnPass& p, bool state, hipStream_t stream);
-hipError_t launch_linattn_bf16(const LinattnPass& p, bool state, hipStream_t stream);
-hipError_t launch_linattn_bwd_bf16(const LinattnPass& p, hipStream_t stream);
-hipError_t launch_linattn_bwd_f32(const LinattnPass& p, hipStream_t stream);
-hipError_t launch_linattn_bwd_any(const LinattnPass& p, bool state, hipStream_t stream);
+hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_bf16(const LinattnPass* p, int n, bool last, hipStream_t stream);
+hipError_t launch_linattn_bwd_f32(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_bwd_any(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_states_f32(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_states_bf16(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_states_any(const LinattnPass* p, int n, hipStream_t stream);
 
 namespace {
 
-constexpr int64_t kCus = 256;
-constexpr int kJoinBlock = 256, kJoinAhead = 8;
+constexpr int64_t kSlots = 512;   // workgroups that run at once: two on a compute unit
+constexpr int kJoinBlock = 256;
 
 __device__ __forceinline__ double power(double x, int64_t n) {
   double y = 1.0;
@@ -25,87 +27,160 @@ __device__ __forceinline__ double power(double x, int64_t n) {
   return y;
 }
 
-// joined[seg] <- the state that enters segment seg: E_0 from s_in (with its
-// decay to the first token, forward), E_{seg+1} = l^tokens E_seg + joined[seg].
-__global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const LinattnPass p) {
-  const int64_t size = static_cast<int64_t>(p.Dk) * p.Dv;
-  const uint32_t per = static_cast<uint32_t>((size + kJoinBlock - 1) / kJoinBlock);
+// The states that enter the segments: E_0 is s_in (with its decay to the first
+// token where the pass is forward), E_{s+1} = l^tokens E_s + u_s.  E_s takes the
+// place of u_s for the multiples s of `sub`; s_out (nullptr: not wanted) is the
+// state behind the last token (forward: of the token itself, backward: with
+// its decay).
+struct Join {
+  float* u;         // [states][n][size]
+  const float* s_in;
+  float* s_out;
+  bool rev;
+};
+struct Joins {
+  Join j[2];
+  const float* decay;
+  uint32_t states, H, n, sub;
+  int64_t size, tokens, T;
+};
+
+template <int N>
+__global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const Joins a) {
+  typedef float vec __attribute__((ext_vector_type(N)));
+  const Join& j = a.j[blockIdx.y];
+  const uint32_t per = static_cast<uint32_t>((a.size / N + kJoinBlock - 1) / kJoinBlock);
   const int64_t bh = blockIdx.x / per;
-  const int64_t at = static_cast<int64_t>(blockIdx.x % per) * kJoinBlock + threadIdx.x;
-  if (at >= size) return;
-  const double l = p.decay[bh % p.H];
-  const float w = static_cast<float>(power(l, p.seg_tokens));
-  float e = 0.0f;
-  if (p.s_in != nullptr) {
-    e = p.s_in[bh * size + at / p.Dv * p.in_d + at % p.Dv * p.in_e];
-    if (!p.rev) e *= p.decay[bh % p.H];
+  const int64_t at = N * (static_cast<int64_t>(blockIdx.x % per) * kJoinBlock + threadIdx.x);
+  if (at >= a.size) return;
+  const float l = a.decay[bh % a.H];
+  const auto load = [](const float* p) { return *reinterpret_cast<const vec*>(p); };
+  vec e = 0.0f;
+  if (j.s_in != nullptr) {
+    e = load(j.s_in + bh * a.size + at);
+    if (!j.rev) e *= l;
   }
-  float* const u = p.joined + bh * p.nseg * size + at;
-  float last = 0.0f;
-  if (p.join_last) last = u[(p.nseg - 1) * size];
-  for (uint32_t s = 0; s < p.nseg; s += kJoinAhead) {
-    float v[kJoinAhead];
+  float* const u = j.u + bh * a.n * a.size + at;
+  // a sum that nothing follows is not there unless s_out is wanted
+  const uint32_t have = j.s_out != nullptr ? a.n : a.n - a.sub;
+  const float full = static_cast<float>(power(l, a.tokens));
+  constexpr int kJoinAhead = 32 / N;   // loads in flight
+  for (uint32_t s = 0; s < a.n; s += kJoinAhead) {
+    vec v[kJoinAhead];
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) v[i] = s + i + 1 < p.nseg ? u[(s + i) * size] : 0.0f;
+    for (int i = 0; i < kJoinAhead; ++i)
+      if (s + i < have) v[i] = load(u + (s + i) * a.size);
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i) {
-      if (s + i >= p.nseg) break;
-      u[(s + i) * size] = e;
-      if (s + i + 1 < p.nseg) e = fmaf(w, e, v[i]);
+      if (s + i >= a.n) break;
+      if ((s + i) % a.sub == 0) *reinterpret_cast<vec*>(u + (s + i) * a.size) = e;
+      if (s + i >= have) continue;
+      const int64_t left = a.T - (s + i) * a.tokens;   // tokens from here on
+      float w = full;
+      if (left <= a.tokens) w = left <= 0 ? 1.0f : static_cast<float>(power(l, j.rev ? left : left - 1));
+#pragma unroll
+      for (int c = 0; c < N; ++c) e[c] = fmaf(w, e[c], v[i][c]);
     }
   }
-  if (p.join_last) {
-    const float wl = static_cast<float>(power(l, p.T - (p.nseg - 1) * p.seg_tokens));
-    p.s_out[bh * size + at / p.Dv * p.in_d + at % p.Dv * p.in_e] = fmaf(wl, e, last);
-  }
+  if (j.s_out != nullptr) *reinterpret_cast<vec*>(j.s_out + bh * a.size + at) = e;
 }
 
-}  // namespace
-
-LinattnPlan linattn_plan(int64_t B, int64_t T, int64_t H, int Dk, int Dv) {
-  LinattnPlan plan;
-  plan.et = Dv <= 64 || Dk > 128 ? 1 : 2;
-  plan.tiles = static_cast<uint32_t>((Dv + 64 * plan.et - 1) / (64 * plan.et));
-  const int64_t C = Dk > 128 ? 32 : 64;
-  const int64_t chunks = (T + C - 1) / C, groups = B * H * plan.tiles;
-  // rounds of workgroups x chunks of a segment, half as much again for the
-  // segments' own sums
-  int64_t best = 1, cost = ((groups + kCus - 1) / kCus) * chunks * 2;
-  for (int64_t s = 2; s <= chunks && groups * (s - 1) < 4 * kCus; ++s) {
-    const int64_t per = (chunks + s - 1) / s;
-    const int64_t c = ((groups * s + kCus - 1) / kCus) * per * 3 + 4;
-    if (c < cost) {
-      best = s;
-      cost = c;
-    }
-  }
+// How both directions are cut: segments, and the finer ones whose sums are
+// joined (their kernel runs two workgroups on a compute unit).
+struct Plan {
+  uint32_t nseg, sub;
+  int64_t seg_tokens;
+};
+int waves_of(int Dv) { return Dv <= 64 ? 4 : 8; }
+uint32_t tiles_of(int Dv) {
+  const int w = 16 * waves_of(Dv);
+  return static_cast<uint32_t>((Dv + w - 1) / w);
+}
+Plan plan_of(int64_t T, int64_t groups, int passes) {
+  constexpr int64_t C = 64;
+  const int64_t chunks = (T + C - 1) / C;
+  // rounds of workgroups x (chunks of a segment + about 3 for its start), and
+  // half as much again with the states' sums and their joining
+  const auto cost = [&](int64_t s) {
+    const int64_t per = (chunks + s - 1) / s, rounds = (groups * passes * s + kSlots - 1) / kSlots;
+    return s == 1 ? 2 * rounds * (per + 3) : 3 * rounds * (per + 3) + 4;
+  };
+  int64_t best = 1;
+  for (int64_t s = 2; s <= chunks && groups * (s - 1) < 2 * kSlots; ++s)
+    if (cost(s) < cost(best)) best = s;
   const int64_t per = (chunks + best - 1) / best;
+  Plan plan;
   plan.nseg = static_cast<uint32_t>((chunks + per - 1) / per);
   plan.seg_tokens = per * C;
-  plan.joined_bytes = sizeof(float) * static_cast<size_t>(B * H) * plan.nseg * Dk * Dv;
+  plan.sub = per % 2 == 0 && groups * plan.nseg <= kSlots ? 2 : 1;
   return plan;
 }
+Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), 1); }
+Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv) {
+  const uint32_t a = tiles_of(dv), b = tiles_of(dk);
+  return plan_of(T, B * H * (a > b ? a : b), 3);
+}
+size_t sums_bytes(const Plan& plan, int64_t states, int dk, int dv) {
+  return sizeof(float) * static_cast<size_t>(states) * plan.nseg * plan.sub * dk * dv;
+}
 
-namespace {
-
-LinattnPass with_plan(LinattnPass p, const LinattnPlan& plan, float* joined) {
+LinattnPass cut(LinattnPass p, const Plan& plan) {
+  p.waves = waves_of(p.Dv);
+  p.tiles = tiles_of(p.Dv);
   p.nseg = plan.nseg;
-  p.tiles = plan.tiles;
-  p.et = plan.et;
   p.seg_tokens = plan.seg_tokens;
-  p.joined = plan.nseg > 1 || p.join_last ? joined : nullptr;
+  return p;
+}
+// The same over the finer segments for the sums alone.
+LinattnPass sums_of(LinattnPass p, const Plan& plan, float* u, bool all) {
+  p.nseg = plan.nseg * plan.sub;
+  p.seg_tokens = plan.seg_tokens / plan.sub;
+  p.segs = all ? p.nseg : p.nseg - plan.sub;
+  p.s_out = u;
+  return p;
+}
+// The pass from the joined states u of sums [dk][dv]; `turned`: its state is
+// their transpose.
+LinattnPass from_joined(LinattnPass p, const Plan& plan, const float* u, bool turned) {
+  const int64_t size = static_cast<int64_t>(p.Dk) * p.Dv;
+  p.e_in = u;
+  p.e_bh = size * plan.nseg * plan.sub;
+  p.e_seg = size * plan.sub;
+  p.e_d = turned ? 1 : p.Dv;
+  p.e_e = turned ? p.Dk : 1;
+  p.e_decay = false;
   return p;
 }
 
-hipError_t join(const LinattnPass& p, hipStream_t stream) {
-  const uint32_t per = static_cast<uint32_t>((static_cast<int64_t>(p.Dk) * p.Dv + kJoinBlock - 1) / kJoinBlock);
-  hipLaunchKernelGGL(linattn_join_kernel, dim3(p.B * p.H * per), dim3(kJoinBlock), 0, stream, p);
+hipError_t join(const Join* j, int n, const LinattnPass& p, const Plan& plan, hipStream_t stream) {
+  Joins a{};
+  for (int i = 0; i < n; ++i) a.j[i] = j[i];
+  a.decay = p.decay;
+  a.states = p.B * p.H;
+  a.H = p.H;
+  a.n = plan.nseg * plan.sub;
+  a.sub = plan.sub;
+  a.size = static_cast<int64_t>(p.Dk) * p.Dv;
+  a.tokens = plan.seg_tokens / plan.sub;
+  a.T = p.T;
+  // a lane's entries side by side where the lanes are still many
+  const bool wide = a.size * a.states * n >= int64_t(1) << 20;
+  const int64_t lanes = a.size / (wide ? 4 : 1);
+  const dim3 grid(a.states * static_cast<uint32_t>((lanes + kJoinBlock - 1) / kJoinBlock), static_cast<uint32_t>(n));
+  if (wide) hipLaunchKernelGGL(linattn_join_kernel<4>, grid, dim3(kJoinBlock), 0, stream, a);
+  else hipLaunchKernelGGL(linattn_join_kernel<1>, grid, dim3(kJoinBlock), 0, stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_linattn_chunk(const LinattnArgs& a, float* joined, hipStream_t stream) {
+size_t linattn_chunk_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
+  const Plan plan = plan_fwd(B, T, H, dk, dv);
+  return plan.nseg > 1 ? sums_bytes(plan, B * H, dk, dv) : 0;
+}
+
+hipError_t launch_linattn_chunk(const LinattnArgs& a, float* scratch, hipStream_t stream) {
+  const Plan plan = plan_fwd(a.B, a.T, a.H, a.dk, a.dv);
   const int64_t size = a.is_f32 ? 4 : 2, ld = a.H * (2 * a.dk + a.dv);
   const char* const x = static_cast<const char*>(a.qkv);
   LinattnPass p{};
@@ -117,78 +192,101 @@ hipError_t launch_linattn_chunk(const LinattnArgs& a, float* joined, hipStream_t
   p.decay = a.decay;
   p.alpha = 1.0f;
   p.beta = a.scale;
-  p.s_in = a.s0;
-  p.s_out = a.s_last;
-  p.in_d = a.dv;
-  p.in_e = 1;
   p.B = static_cast<uint32_t>(a.B);
   p.H = static_cast<uint32_t>(a.H);
   p.T = a.T;
   p.Dk = a.dk;
   p.Dv = a.dv;
-  p = with_plan(p, linattn_plan(a.B, a.T, a.H, a.dk, a.dv), joined);
-  const auto pass = a.is_f32 ? launch_linattn_f32 : launch_linattn_bf16;
-  if (p.joined != nullptr) {
-    if (hipError_t e = pass(p, true, stream)) return e;
-    if (hipError_t e = join(p, stream)) return e;
+  p = cut(p, plan);
+  if (plan.nseg == 1) {
+    p.e_in = a.s0;
+    p.e_bh = static_cast<int64_t>(a.dk) * a.dv;
+    p.e_d = a.dv;
+    p.e_e = 1;
+    p.e_decay = true;
+    p.s_out = a.s_last;
+    return a.is_f32 ? launch_linattn_f32(&p, 1, stream) : launch_linattn_bf16(&p, 1, a.s_last != nullptr, stream);
   }
-  return pass(p, false, stream);
-}
-
-size_t linattn_chunk_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
-  const LinattnPlan plan = linattn_plan(B, T, H, dk, dv);
-  return plan.nseg > 1 ? plan.joined_bytes : 0;
+  // of bf16 the last state comes from the sums, which are more exact than what
+  // a bf16 o needs of the state within a segment
+  const bool joined_last = !a.is_f32 && a.s_last != nullptr;
+  const LinattnPass u = sums_of(p, plan, scratch, joined_last);
+  if (hipError_t e = (a.is_f32 ? launch_linattn_states_f32 : launch_linattn_states_bf16)(&u, 1, stream)) return e;
+  const Join j{scratch, a.s0, joined_last ? a.s_last : nullptr, false};
+  if (hipError_t e = join(&j, 1, p, plan, stream)) return e;
+  p = from_joined(p, plan, scratch, false);
+  p.s_out = joined_last ? nullptr : a.s_last;
+  return a.is_f32 ? launch_linattn_f32(&p, 1, stream) : launch_linattn_bf16(&p, 1, false, stream);
 }
 
 size_t linattn_bwd_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
-  const size_t a = linattn_plan(B, T, H, dk, dv).joined_bytes, b = linattn_plan(B, T, H, dv, dk).joined_bytes;
-  return a > b ? a : b;
+  return 2 * sums_bytes(plan_bwd(B, T, H, dk, dv), B * H, dk, dv);
 }
 
-hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* joined, hipStream_t stream) {
+hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream_t stream) {
+  const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv);
   const int64_t size = a.is_f32 ? 4 : 2, ld = a.H * (2 * a.dk + a.dv);
   const char* const x = static_cast<const char*>(a.qkv);
   const LinattnOperand q{x, ld, a.is_f32}, k{x + a.H * a.dk * size, ld, a.is_f32},
       v{x + 2 * a.H * a.dk * size, ld, a.is_f32}, d{a.dout, a.H * a.dv, a.do_is_f32};
-  uint16_t* const dq = a.dqkv;
   const bool bf16 = !a.is_f32 && !a.do_is_f32, f32 = a.is_f32 && a.do_is_f32;
-  // [0] dq, [1] dk, [2] dv: the last writes ds0, which may be ds_last
-  for (int i = 0; i < 3; ++i) {
-    LinattnPass p{};
-    p.q = i == 0 ? d : i == 1 ? v : k;
-    p.k = i == 0 ? v : i == 1 ? d : q;
-    p.v = i == 0 ? k : i == 1 ? q : d;
-    p.o = dq + (i == 0 ? 0 : i == 1 ? a.H * a.dk : 2 * a.H * a.dk);
-    p.ldo = ld;
-    p.decay = a.decay;
-    p.alpha = i == 0 ? 1.0f : a.scale;
-    p.beta = i == 0 ? a.scale : 1.0f;
-    p.rev = i != 0;
-    p.s_in = i == 0 ? a.s0 : a.ds_last;
-    p.join_last = i == 2 && a.ds0 != nullptr;
-    p.B = static_cast<uint32_t>(a.B);
-    p.H = static_cast<uint32_t>(a.H);
-    p.T = a.T;
-    p.Dk = i == 2 ? a.dk : a.dv;
-    p.Dv = i == 2 ? a.dv : a.dk;
-    p.in_d = i == 2 ? a.dv : 1;
-    p.in_e = i == 2 ? 1 : a.dv;
-    p = with_plan(p, linattn_plan(a.B, a.T, a.H, p.Dk, p.Dv), joined);
-    if (p.joined != nullptr) {
-      p.s_out = p.join_last ? a.ds0 : nullptr;
-      const hipError_t e = bf16  ? launch_linattn_bf16(p, true, stream)
-                           : f32 ? launch_linattn_f32(p, true, stream)
-                                 : launch_linattn_bwd_any(p, true, stream);
-      if (e != hipSuccess) return e;
-      if (hipError_t e2 = join(p, stream)) return e2;
-      p.s_out = nullptr;
-    }
-    const hipError_t e = bf16  ? launch_linattn_bwd_bf16(p, stream)
-                         : f32 ? launch_linattn_bwd_f32(p, stream)
-                               : launch_linattn_bwd_any(p, false, stream);
-    if (e != hipSuccess) return e;
+  LinattnPass base{};
+  base.decay = a.decay;
+  base.B = static_cast<uint32_t>(a.B);
+  base.H = static_cast<uint32_t>(a.H);
+  base.T = a.T;
+  base.ldo = ld;
+  // dq, dk, dv; [3], [4]: the sums of S and of its gradient
+  LinattnPass p[5];
+  for (int i = 0; i < 5; ++i) {
+    p[i] = base;
+    const bool turned = i < 2;
+    p[i].q = i == 0 ? d : i == 1 ? v : k;
+    p[i].k = i == 0 ? v : i == 1 ? d : i == 3 ? k : q;
+    p[i].v = i == 0 || i == 2 ? (i == 0 ? k : d) : i == 1 ? q : i == 3 ? v : d;
+    p[i].o = a.dqkv + (i == 1 ? a.H * a.dk : i == 2 ? 2 * a.H * a.dk : 0);
+    const bool s = i == 0 || i == 3;
+    p[i].rev = !s;
+    p[i].alpha = s ? 1.0f : a.scale;
+    p[i].beta = s ? a.scale : 1.0f;
+    p[i].Dk = turned ? a.dv : a.dk;
+    p[i].Dv = turned ? a.dk : a.dv;
+    p[i] = cut(p[i], plan);
+    p[i].e_in = s ? a.s0 : a.ds_last;
+    p[i].e_bh = static_cast<int64_t>(a.dk) * a.dv;
+    p[i].e_d = turned ? 1 : a.dv;
+    p[i].e_e = turned ? a.dv : 1;
+    p[i].e_decay = s;
   }
-  return hipSuccess;
+  float* const us = scratch;
+  float* const ug = scratch + sums_bytes(plan, a.B * a.H, a.dk, a.dv) / sizeof(float);
+  const bool some = plan.nseg > 1;
+  if (some || a.ds0 != nullptr) {
+    LinattnPass u[2];
+    Join j[2];
+    int n = 0;
+    if (some) {
+      u[n] = sums_of(p[3], plan, us, false);
+      j[n++] = {us, a.s0, nullptr, false};
+    }
+    u[n] = sums_of(p[4], plan, ug, a.ds0 != nullptr);
+    j[n++] = {ug, a.ds_last, a.ds0, true};
+    const auto states = bf16 ? launch_linattn_states_bf16 : f32 ? launch_linattn_states_f32 : launch_linattn_states_any;
+    if (hipError_t e = states(u, n, stream)) return e;
+    if (hipError_t e = join(j, n, p[4], plan, stream)) return e;
+    if (some) p[0] = from_joined(p[0], plan, us, true);
+    // from here on ds_last may be overwritten by ds0
+    p[1] = from_joined(p[1], plan, ug, true);
+    p[2] = from_joined(p[2], plan, ug, false);
+  }
+  const auto passes = [&](const LinattnPass* first, int n) {
+    return bf16 ? launch_linattn_bf16(first, n, false, stream)
+           : f32 ? launch_linattn_bwd_f32(first, n, stream) : launch_linattn_bwd_any(first, n, stream);
+  };
+  const auto width = [](int d) { return d <= 64 ? 0 : d <= 128 ? 1 : 2; };
+  if (width(a.dk) == width(a.dv) && p[0].waves == p[2].waves) return passes(p, 3);
+  if (hipError_t e = passes(p, 2)) return e;
+  return passes(p + 2, 1);
 }
 
 }  // namespace mmf

@@ -1,10 +1,14 @@
-// Linear attention over chunks, backward: bf16 and fp32 among the operands.
+// Linear attention over chunks: operands of both types, o in bf16 (backward); and
+// the states' sums.
 #include "linattn_chunk.h"
 
 namespace mmf {
-hipError_t launch_linattn_bwd_any(const LinattnPass& p, bool state, hipStream_t stream) {
+hipError_t launch_linattn_bwd_any(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return state ? launch_pass<kEither, kEither, kEither, true, 3, 3, true>(p, stream)
-               : launch_pass<kEither, kEither, kEither, false, 2, 2, false>(p, stream);
+  return launch_passes<kEither, kEither, kEither, false, 2, 2, false>(p, n, stream);
+}
+hipError_t launch_linattn_states_any(const LinattnPass* p, int n, hipStream_t stream) {
+  using namespace la;
+  return launch_passes<kEither, kEither, kEither, true, 3, 3, true>(p, n, stream);
 }
 }  // namespace mmf

@@ -1,9 +1,9 @@
-// Linear attention over chunks, backward: fp32 inputs and gradients.
+// Linear attention over chunks: fp32 operands, o in bf16 (backward).
 #include "linattn_chunk.h"
 
 namespace mmf {
-hipError_t launch_linattn_bwd_f32(const LinattnPass& p, hipStream_t stream) {
+hipError_t launch_linattn_bwd_f32(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_pass<kF32, kF32, kF32, false, 2, 2, false>(p, stream);
+  return launch_passes<kF32, kF32, kF32, false, 2, 2, false>(p, n, stream);
 }
 }  // namespace mmf

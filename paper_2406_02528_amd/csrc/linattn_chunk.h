@@ -18,29 +18,23 @@
 // segment's own sum, a second joins them into the states that enter the
 // segments, from which the pass itself starts.
 //
-// A workgroup of eight waves holds a state of Dk rows and 64 ET columns in the
-// accumulators of its matrix instructions: 16 ET columns per wave and, of each
-// four neighbouring rows, two (waves 0-3 and 4-7).  q E of a wave is then a
-// part of the sum; each wave finishes half of the token tiles with the other
-// half's part from LDS.  A chunk's rows are loaded while the chunk before is
-// worked on.  The layouts are chosen so that neither the state nor the values
-// ever pass through LDS (v_mfma_f32_16x16x32_bf16; lane = 16 g + n, g = 0..3, n
-// = 0..15; A: row n, B: column n, eight contraction slots j per lane; D: column
-// n, rows 4 g + r):
-//   - the state's tile (x, i) has row m = entry d = 64 x + 4 pi(m) + i (pi a
-//     permutation of 16, below) and column n = entry e = ET n + f of the wave's
-//     columns, so that a lane keeps ET neighbouring columns;
-//   - as the operand B of q E its slots are the rows m = 4 g + j%4 of tiles i =
-//     2 h + j/4 (side by side: h = 0 waves 0-3, 1 waves 4-7), so a lane's part of a
-//     query or key is four times four entries of its row, in two operands h; pi
-//     puts the four lanes g of a row side by side in each load (16 bytes of fp32:
-//     d = 16 r + 4 g + i, of bf16: d = 8 g + 4 (r%2) + 32 (r/2) + i), where 16
-//     entries in a row per lane would have each load touch four times the lines;
-//   - tokens as contraction slots are s = 32 c + 16 (j/4) + 4 g + j%4, which is
-//     how the transposed products k q^T leave their rows, two tiles side by
-//     side: they go to LDS with 8-byte stores in place;
-//   - a lane's part of the values (and of the transposed keys) are 8 (4) tokens
-//     with ET (4) neighbouring entries each, transposed in registers.
+// A workgroup of 8 (4) waves holds a state of Dk rows and 128 (64) columns in the
+// accumulators of its matrix instructions, 16 columns per wave.  A chunk's rows
+// are read once, 16 bytes of bf16 per lane and row, a chunk ahead of their use,
+// and go to LDS as they are (fp32: as bf16 parts); every operand of the products
+// comes from there, along the rows or, by the transposing read, across them.
+// With v_mfma_f32_16x16x32_bf16 (lane = 16 g + n, g = 0..3, n = 0..15; A: row n,
+// B: column n, eight contraction slots 8 g + j; D: column n, rows 4 g + r):
+//   keys x queries  A: keys as rows, B: queries; D: keys 4 g + r of query n, which
+//                   LDS takes as rows of queries, 8 bytes per lane
+//   state x queries A: the state's columns as rows, B: queries
+//   values x products  A: the values' columns as rows (across), B: the products'
+//                   rows; D: columns 4 g + r of query n, side by side in memory
+//   keys x values   A: the keys' entries as rows (across), B: the decayed
+//                   values' columns (across); D: the state
+// The state's tile (b, h) has row m = entry d = 32 b + 8 (m / 4) + 4 h + m % 4, so
+// that the rows a lane keeps of the two tiles h are the slots d = 32 b + 8 g + j
+// of the operand it is for the next chunk: the state never leaves its registers.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
 // decayed products, the state, the weighted keys) go to the matrix cores as
@@ -58,6 +52,8 @@ namespace la {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
@@ -81,6 +77,21 @@ __device__ __forceinline__ void split8(const float* x, v4i (&p)[N]) {
     }
   }
 }
+// And back.
+template <int N>
+__device__ __forceinline__ void sum8(const v4i (&p)[N], float* x) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    float a = bf16_lo(p[N - 1][w]), b = bf16_hi(p[N - 1][w]);
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) {
+      a += bf16_lo(p[i][w]);
+      b += bf16_hi(p[i][w]);
+    }
+    x[2 * w] = a;
+    x[2 * w + 1] = b;
+  }
+}
 
 // acc += a b over the parts' products of relative size above 2^(-8 L).
 template <int L, int NA, int NB>
@@ -93,39 +104,39 @@ __device__ __forceinline__ v4f mma(const v4i (&a)[NA], const v4i (&b)[NB], v4f a
   return acc;
 }
 
+// Tiles in LDS: rows of W bf16 values in chunks of 16 bytes, chunk q of a row at
+// q ^ swizzle(row).  The 8 lanes that one cycle serves, 8 rows at the same
+// chunk (along the rows) or 4 rows at 4 neighbouring ones (across), then touch
+// all banks once.  Rows 16 apart have the same swizzle, and chunks 4 b apart
+// differ in address bits that no other part of the sum reaches: ^ (b << 6).
+template <int W>
+__device__ __forceinline__ int tile_at(int row, int chunk) {
+  const int f = W == 32 ? (row >> 2) & 3
+              : W == 64 ? 4 * ((row >> 1) & 1) + ((row >> 2) & 3) : 4 * (row & 3) + ((row >> 2) & 3);
+  return row * (2 * W) + ((chunk ^ f) << 4);
+}
+__device__ __forceinline__ v4i tile_read(const char* tile, int at) { return *reinterpret_cast<const v4i*>(tile + at); }
+// Across: 4 rows (from lanes 4 k .. 4 k + 3 of 16, each 4 of 16 columns) to 16
+// lanes, a column each.
+__device__ __forceinline__ v2u tile_turn(const char* tile, int at) {
+  typedef __attribute__((address_space(3))) v4s lds_v4s;
+  return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + at)));
+}
+__device__ __forceinline__ v4i tile_turn8(const char* tile, int at0, int at1) {
+  const v2u a = tile_turn(tile, at0), b = tile_turn(tile, at1);
+  return v4i{static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(b.x), static_cast<int>(b.y)};
+}
+
 // How an operand's elements are stored: bf16, fp32, or as the pass says.
 enum Kind { kBf16, kF32, kEither };
+template <Kind K>
+constexpr int kUnitDwords = K == kBf16 ? 4 : 8;   // of 8 elements in registers
 
-// N (1, 2, 4, 16) consecutive elements at byte offset off, zero past the
-// resource; bf16 ones two to a dword.
-template <int N>
-__device__ __forceinline__ void load_f32(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t (&w)[N]) {
-  if constexpr (N == 1) {
-    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
-  } else if constexpr (N == 2) {
-    const Words<2> p = load_stream<2, false>(r, off);
-    w[0] = p.w[0];
-    w[1] = p.w[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const Words<4> p = load_stream<4, false>(r, off + 4 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[i + j] = p.w[j];
-    }
-  }
-}
-template <int N, int W>
-__device__ __forceinline__ void load_bf16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t (&w)[W]) {
-  if constexpr (N == 1) {
-    w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
-  } else {
-    uint32_t h[N / 2];
-    load_f32<N / 2>(r, off, h);
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) w[i] = h[i];
-  }
-}
+template <Kind K>
+struct KindOf {
+  static constexpr Kind value = K;
+};
+
 // Rows of one operand in a chunk.  A row past the chunk's tokens has an offset
 // past the resource (forward: above it; backward, where token i is row tc - 1 -
 // i: below 0, which is far above it), so it reads as zero with no mask; so
@@ -150,159 +161,91 @@ struct Rows {
     char* const p = const_cast<char*>(static_cast<const char*>(x.p)) + (row * x.ld + h * w) * size;
     r = __builtin_amdgcn_make_buffer_rsrc(p, 0, (tc - 1) * ld + w * size, kBufferWord3);
   }
-  // A lane's offset: of token i and column d.  Not a constant of the loop for
-  // the compiler, which would keep an offset in registers for every load.
-  __device__ __forceinline__ uint32_t lane(int i, int d) const {
-    uint32_t o = d < width ? base + static_cast<uint32_t>(i * step + d * (f32() ? 4 : 2)) : kOff;
-    asm volatile("" : "+v"(o));
-    return o;
-  }
-  // N elements, i tokens behind the lane's.
-  template <int N, int W>
-  __device__ __forceinline__ void load(uint32_t lane, int i, uint32_t (&w)[W]) const {
-    const uint32_t off = lane + static_cast<uint32_t>(i * step);
-    if constexpr (K != kBf16) {
-      if (f32()) {
-        load_f32<N>(r, off, w);
-        return;
+  // Units of 8 elements: those of `threads` threads from token i, column d on,
+  // U of them `apart` tokens from each other.
+  template <int U>
+  __device__ __forceinline__ void load(int i, int d, int apart, uint32_t (&w)[U][kUnitDwords<K>]) const {
+    const uint32_t size = f32() ? 4u : 2u;
+    const uint32_t o = d < width ? base + static_cast<uint32_t>(i * step) + static_cast<uint32_t>(d) * size : kOff;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t off = o + static_cast<uint32_t>(u * apart * step);
+      const Words<4> a = load_stream<4, false>(r, off);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[u][j] = a.w[j];
+      if constexpr (K != kBf16) {
+        // (of bf16 rows these are not used)
+        const Words<4> b = load_stream<4, false>(r, off + 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[u][4 + j] = b.w[j];
       }
     }
-    if constexpr (K != kF32) load_bf16<N>(r, off, w);
   }
 };
-
-// pi: in fours of fp32 (FOURS) or eights of bf16, see above.
-template <bool FOURS>
-__device__ __forceinline__ int pi(int m) {
-  const int g = m >> 2, r = m & 3;
-  return FOURS ? g + 4 * r : 2 * g + (r & 1) + 8 * (r >> 1);
-}
-// A lane's 16 entries of the 64 from d0 of the token at its offset: rows 4 g + r
-// of tile i at w's element 4 r + i.
-template <bool FOURS, Kind K, int W>
-__device__ __forceinline__ void load_entries(const Rows<K>& x, int token, int d0, int g, uint32_t (&w)[W]) {
-  constexpr int kRun = FOURS ? 4 : 8;   // entries side by side
-#pragma unroll
-  for (int c = 0; c < 16 / kRun; ++c) {
-    const uint32_t o = x.lane(token, d0 + kRun * g + 4 * kRun * c);
-    if constexpr (K == kBf16) {
-      uint32_t h[kRun / 2];
-      load_f32<kRun / 2>(x.r, o, h);
-#pragma unroll
-      for (int i = 0; i < kRun / 2; ++i) w[kRun / 2 * c + i] = h[i];
-    } else {
-      uint32_t h[kRun];
-      if (x.f32()) {
-        load_f32<kRun>(x.r, o, h);
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) w[kRun * c + i] = h[i];
-      } else if constexpr (K == kEither) {
-        load_f32<kRun / 2>(x.r, o, reinterpret_cast<uint32_t(&)[kRun / 2]>(h));
-#pragma unroll
-        for (int i = 0; i < kRun / 2; ++i) w[kRun / 2 * c + i] = h[i];
-      }
-    }
-  }
-}
-
-// Dwords that N elements of a kind take in registers.
-template <Kind K, int N>
-constexpr int kDwords = K == kBf16 && N > 1 ? N / 2 : N;
-
-// Eight elements as operand parts: of bf16 elements the bits themselves, two
-// (word, half) each.
-template <Kind K, int NP, typename At>
-__device__ __forceinline__ void operand(At&& at, v4i (&f)[NP]) {
+// A unit's values in fp32.
+template <Kind K>
+__device__ __forceinline__ void unit_values(const uint32_t (&w)[kUnitDwords<K>], bool f32, float* x) {
   if constexpr (K == kBf16) {
-    static_assert(NP == 1, "bf16 operands are exact");
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const auto a = at(2 * w), b = at(2 * w + 1);
-      const uint32_t sel = (a.half ? 0x0302u : 0x0100u) | ((b.half ? 0x0706u : 0x0504u) << 16);
-      f[0][w] = static_cast<int>(__builtin_amdgcn_perm(b.word, a.word, sel));
-    }
+    for (int j = 0; j < 8; ++j) x[j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
   } else {
-    float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = at(j).value();
-    split8<NP>(x, f);
+    for (int j = 0; j < 8; ++j) {
+      const float whole = __uint_as_float(w[j]);
+      x[j] = whole;
+      if constexpr (K == kEither) {
+        const uint32_t pair = w[j / 2];
+        const float part = j & 1 ? bf16_hi(pair) : bf16_lo(pair);
+        x[j] = f32 ? whole : part;
+      }
+    }
   }
 }
-struct Element {
-  uint32_t word;
-  bool half, f32;
-  __device__ __forceinline__ float value() const { return f32 ? __uint_as_float(word) : half ? bf16_hi(word) : bf16_lo(word); }
-};
-template <int N>
-__device__ __forceinline__ Element element(const uint32_t (&w)[N], bool f32, int e) {
-  const uint32_t whole = w[e], pair = w[e / 2];
-  return {f32 ? whole : pair, !f32 && (e & 1) != 0, f32};
-}
-// Whether any of N elements of several tokens is not finite: 0 in `bad` else.
-template <int count, int N>
-__device__ __forceinline__ void look(const uint32_t (&w)[N], bool f32, uint32_t& bad) {
+// The largest magnitude's upper 16 bits so far, in both halves of `top`.
+__device__ __forceinline__ void look_bf16(uint32_t w, uint32_t& top) {
   typedef unsigned short v2us __attribute__((ext_vector_type(2)));
-  // the largest of the magnitudes (bf16: of both halves), as integers
-  if (f32) {
-#pragma unroll
-    for (int i = 0; i < count; ++i) bad = max(bad, (w[i] & 0x7FFFFFFFu) >> 16);
-  } else {
-    constexpr int words = count > 1 ? count / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < words; ++i) {
-      const uint32_t v = count > 1 ? w[i] & 0x7FFF7FFFu : w[i] & 0x7FFFu;
-      bad = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, bad), __builtin_bit_cast(v2us, v)));
-    }
-  }
+  top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, top), __builtin_bit_cast(v2us, w & 0x7FFF7FFFu)));
 }
-__device__ __forceinline__ bool not_finite(uint32_t bad) { return (bad & 0xFFFFu) >= 0x7F80u || (bad >> 16) >= 0x7F80u; }
+__device__ __forceinline__ bool not_finite(uint32_t top) { return (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u; }
 
-// MODE: parts of fp32 values in the products of o.  NKT: parts of the weighted
-// keys in the state's.  DK: Dk padded to 64s.  STATE: the segment's own sum
-// only (no queries, no o).
-template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int ET, int C, bool STATE>
-__global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p) {
-  constexpr int kX = DK / 64;        // 64s of Dk
+// MODE: parts of fp32 values in the products of o.  NKT: parts of the decayed
+// values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of 16 columns
+// each.  STATE: the segment's own sum only (no queries, no o; the values go to
+// LDS decayed).
+template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int C, bool STATE>
+__global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
+  constexpr int kThreads = 64 * WAVES, WC = 16 * WAVES;
+  constexpr int kB = DK / 32;        // contraction steps over Dk
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
-  constexpr bool kFours = KQ == kF32 && KK == kF32;
-  constexpr int kOwn = kT / 2;       // token tiles that a wave finishes
-  constexpr int kPer = 8 / kT;       // waves per tile of keys
-  constexpr bool kEarly = STATE || KV == kBf16;   // registers hold the next rows from the start of a chunk
+  constexpr int kPer = WAVES / kT;   // waves per tile of keys
+  constexpr int kU = (kT + kPer - 1) / kPer;
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
-  constexpr int NV = KV == kBf16 ? 1 : STATE ? NKT : MODE;
-  __shared__ v4i q_lds[STATE ? 1 : kT * kX * 2 * NQ][kWave];   // [token tile][64s][h][part]
-  __shared__ v4i k_lds[STATE ? 2 : 1][kX * 4 * kS * NKT][kWave];   // [in turn][64s][i][token step][part]
-  __shared__ v4i p_lds[STATE ? 1 : kT * kS * MODE][kWave];     // [token tile][token step][part]
-  __shared__ v4f o_lds[STATE ? 1 : 8 * kOwn * ET][kWave];      // [receiving wave][own tile][f]
-  __shared__ float pw[C + 1];                                  // l^i
+  constexpr int NV = STATE ? NKT : KV == kBf16 ? 1 : MODE;
+  // units of 8 elements per thread (half the threads have one where a chunk has fewer)
+  constexpr bool kHalf = C * DK / 8 < kThreads;
+  constexpr int kKUnits = kHalf ? 1 : C * DK / 8 / kThreads, kVUnits = C * WC / 8 / kThreads;
+  static_assert(kVUnits >= 1 && kThreads % (DK / 8) == 0 && kThreads % (WC / 8) == 0, "whole rows");
+  __shared__ __attribute__((aligned(16))) char q_t[STATE ? 1 : NQ][STATE ? 16 : C * DK * 2];
+  __shared__ __attribute__((aligned(16))) char k_t[NK][C * DK * 2];
+  __shared__ __attribute__((aligned(16))) char v_t[NV][C * WC * 2];
+  __shared__ __attribute__((aligned(16))) char p_t[STATE ? 1 : MODE][STATE ? 16 : C * C * 2];
+  __shared__ float pr[2 * C + 2];    // l^(C - i); 1 behind i = C
   __shared__ int s_bad[2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int half = wave >> 2, ew = wave & 3;
   const int n = lane & 15, g = lane >> 4;
-  uint32_t blk = blockIdx.x;
+  const int which = blockIdx.x >= args.first[2] ? 2 : blockIdx.x >= args.first[1] ? 1 : 0;
+  const LinattnPass& p = args.p[which];
+  uint32_t blk = blockIdx.x - args.first[which];
   const uint32_t tile = blk % p.tiles;
   blk /= p.tiles;
   const uint32_t seg = blk % p.nseg;
   const uint32_t bh = blk / p.nseg;
-  if (STATE && seg + 1 == p.nseg && !p.join_last) return;  // no segment follows
+  if (STATE && seg >= p.segs) return;
   const int64_t b = bh / p.H, h = bh % p.H;
-  const int ebase = static_cast<int>(tile) * 64 * ET + ew * 16 * ET;
-  const int e0 = ebase + ET * n;     // the lane's columns e0 .. e0 + ET - 1
-  const bool ewave = ebase < p.Dv;
-  const bool eon = e0 < p.Dv;
-
-  // powers of l: fp64, by squaring (any l, 0 among them)
-  if (threadIdx.x <= C) {
-    double x = p.decay[h], y = 1.0;
-    for (int i = threadIdx.x; i != 0; i >>= 1) {
-      if (i & 1) y *= x;
-      x *= x;
-    }
-    pw[threadIdx.x] = static_cast<float>(y);
-  }
-  if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
+  const int c0 = static_cast<int>(tile) * WC, w0 = c0 + 16 * wave;  // first column of the workgroup, of the wave
+  const bool ewave = w0 < p.Dv;      // widths are multiples of 16
 
   const int64_t begin = static_cast<int64_t>(seg) * p.seg_tokens;
   const int64_t end = begin + p.seg_tokens < p.T ? begin + p.seg_tokens : p.T;
@@ -311,170 +254,155 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
     const int64_t left = end - i;
     return i < single ? 1 : left < C ? static_cast<int>(left) : C;
   };
+  const auto first_row = [&](int64_t i0, int tc) { return b * p.T + (p.rev ? p.T - i0 - tc : i0); };
 
-  // --- a chunk's rows: the wave's values; 4 tokens x 4 entries of the keys for
-  // the state; queries and keys of a token tile
-  constexpr int kKItems = kX * kS * 2;
-  const bool has_k = wave < kKItems;
-  const int kx = wave / (2 * kS), kc = wave / 2 % kS, kj = wave & 1;
-  const int qi = kT * kX == 8 ? wave : kT * kX == 4 ? wave - 4 : wave >= 6 ? -1 : wave - 4;   // few: waves 4-7
-  const bool has_q = qi >= 0;
-  const int qt = qi / kX, qx = qi % kX;
-  const int ps = wave % kT, pt = wave / kT;         // the wave's keys, and its first query tile behind them
-  const bool has_p = ps + pt < kT;
-  uint32_t wv[kS][8][kDwords<KV, ET>], wk[4][kDwords<KK, 4>], wq[kDwords<KQ, 16>], wn[kX][kDwords<KK, 16>];
+  // --- a chunk's rows into registers
+  const int kr = threadIdx.x / (DK / 8), kq = threadIdx.x % (DK / 8);   // row and chunk of the thread's first unit
+  const int vr = threadIdx.x / (WC / 8), vq = threadIdx.x % (WC / 8);
+  constexpr int kKApart = kThreads / (DK / 8), kVApart = kThreads / (WC / 8);
+  const bool k_on = !kHalf || threadIdx.x < C * DK / 8;
+  uint32_t wq[STATE ? 1 : kKUnits][kUnitDwords<KQ>], wk[kKUnits][kUnitDwords<KK>], wv[kVUnits][kUnitDwords<KV>];
   Rows<KQ> rq;
   Rows<KK> rk;
   Rows<KV> rv;
-  const auto first_row = [&](int64_t i0, int tc) { return b * p.T + (p.rev ? p.T - i0 - tc : i0); };
-  const auto load_most = [&](int64_t i0, int tc) {
+  const auto load = [&](int64_t i0, int tc) {
     const int64_t row = first_row(i0, tc);
     rk.at(p.k, row, tc, h, p.Dk, p.rev);
+    rk.load(kr, k_on ? 8 * kq : p.Dk, kKApart, wk);
     rv.at(p.v, row, tc, h, p.Dv, p.rev);
-    const uint32_t vo = rv.lane(4 * g, e0);
-#pragma unroll
-    for (int c = 0; c < kS; ++c)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) rv.template load<ET>(vo, 32 * c + 16 * (j / 4) + j % 4, wv[c][j]);
-    if (has_k) {
-      const uint32_t ko = rk.lane(32 * kc + 16 * kj + 4 * g, 64 * kx + 4 * pi<kFours>(n));
-#pragma unroll
-      for (int r = 0; r < 4; ++r) rk.template load<4>(ko, r, wk[r]);
-    }
+    rv.load(vr, c0 + 8 * vq, kVApart, wv);
     if constexpr (!STATE) {
-      if (has_q) {
-        rq.at(p.q, row, tc, h, p.Dk, p.rev);
-        load_entries<kFours>(rq, 16 * qt + n, 64 * qx, g, wq);
-      }
+      rq.at(p.q, row, tc, h, p.Dk, p.rev);
+      rq.load(kr, k_on ? 8 * kq : p.Dk, kKApart, wq);
     }
   };
-  const auto load_keys = [&](int64_t i0, int tc) {
-    if constexpr (!STATE) {
-      if (has_p) {
-        rk.at(p.k, first_row(i0, tc), tc, h, p.Dk, p.rev);
-#pragma unroll
-        for (int x = 0; x < kX; ++x) load_entries<kFours>(rk, 16 * ps + n, 64 * x, g, wn[x]);
-      }
-    }
-  };
-  load_most(begin, tokens_at(begin));
-  load_keys(begin, tokens_at(begin));
+  const bool some = begin < end;   // a segment of a pass for states may have no tokens
+  if (some) load(begin, tokens_at(begin));
 
-  // the state, [64s][i - 2 half][f]
-  v4f st[kX][2][ET];
-  const float first = p.rev || p.joined != nullptr ? 1.0f : p.decay[h];
+  // powers of l: fp64, by squaring (any l, 0 among them)
+  for (int i = threadIdx.x; i < 2 * C + 2; i += kThreads) {
+    double x = p.decay[h], y = 1.0;
+    for (int e = i < C ? C - i : 0; e != 0; e >>= 1) {
+      if (e & 1) y *= x;
+      x *= x;
+    }
+    pr[i] = static_cast<float>(y);
+  }
+  if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
+
+  // --- the state: st[b][h] rows 8 g + 4 h + r of 32 b, column w0 + n
+  v4f st[kB][2];
+  const bool given = !STATE && p.e_in != nullptr;
+  const auto re = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<float*>(given ? p.e_in + bh * p.e_bh + seg * p.e_seg : nullptr), 0, given ? p.Dk * p.Dv * 4 : 0, kBufferWord3);
 #pragma unroll
-  for (int x = 0; x < kX; ++x)
+  for (int x = 0; x < kB; ++x)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      const int d = 32 * x + 8 * g + 4 * i;
+      if constexpr (STATE) {
+        st[x][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      } else {
+        const uint32_t at = ewave && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.e_d + (w0 + n) * p.e_e) : kOff;
+        if (p.e_d == 1) {
+          const Words<4> w = load_stream<4, false>(re, at);
 #pragma unroll
-      for (int f = 0; f < ET; ++f) {
+          for (int r = 0; r < 4; ++r) st[x][i][r] = __uint_as_float(w.w[r]);
+        } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = 0.0f;
-          const int d = 64 * x + 4 * pi<kFours>(4 * g + r) + 2 * half + i, e = e0 + f;
-          if (!STATE && eon && d < p.Dk) {
-            if (p.joined != nullptr) {
-              v = p.joined[((static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk + d) * p.Dv + e];
-            } else if (p.s_in != nullptr) {
-              v = p.s_in[static_cast<int64_t>(bh) * p.Dk * p.Dv + static_cast<int64_t>(d) * p.in_d + static_cast<int64_t>(e) * p.in_e];
-              v *= first;
-            }
-          }
-          st[x][i][f][r] = v;
+          for (int r = 0; r < 4; ++r) st[x][i][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(re, at + 4u * r * p.e_d, 0, 0));
         }
       }
+    }
+  if (!STATE && p.e_decay) {
+    const float l = p.decay[h];
+#pragma unroll
+    for (int x = 0; x < kB; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) st[x][i] *= l;
+  }
   lds_barrier();
 
   const float alpha = p.alpha, beta = p.beta;
-  // decays between the rows of a transposed product's tile (keys 4 g + r) and
-  // its column (query n), on the diagonal and one tile before it, and of the
-  // rows 4 g + r of q E
-  float w_diag[4], w_off[4], w_row[4];
-  if constexpr (!STATE) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int s = 4 * g + r;
-      w_diag[r] = n >= s ? alpha * beta * pw[n >= s ? n - s : 0] : 0.0f;
-      w_off[r] = alpha * beta * pw[16 + n - s];
-      w_row[r] = beta * pw[s];
-    }
-  }
+  // lane's places in the tiles
+  const int k_row = tile_at<DK>(n, g);                                        // along: row n, slots 8 g + j
+  const int p_row = tile_at<C>(n, g);
+  const int t_row = 8 * g + (n >> 2);                                         // across: rows 8 g .. + 3, + 4 .. + 7
+  const int k_a0 = tile_at<DK>(t_row, n & 3), k_a1 = tile_at<DK>(t_row + 4, n & 3);
+  const int v_a0 = tile_at<WC>(t_row, 2 * wave + ((n & 3) >> 1)) + 8 * (n & 1);
+  const int v_a1 = tile_at<WC>(t_row + 4, 2 * wave + ((n & 3) >> 1)) + 8 * (n & 1);
+  const int ps = wave % kT, pt = wave / kT;   // the wave's tile of keys, and its first tile of queries behind it
 
-  // --- a chunk's rows, as loaded, into operands: values in registers, keys and
-  // queries in LDS
-  v4i vf[kS][ET][NV];
+  // --- a chunk's rows from registers to LDS; whether its values are finite
   const auto stage = [&](int64_t i0, int tc, int flag) {
-    const bool last = i0 + tc == p.T && !p.rev;  // the state behind the last token itself
-    // values of the wave's columns, and whether they are all finite
-    uint32_t bad = 0;
+    const int last = i0 + tc == p.T && !p.rev ? 1 : 0;  // the state behind the last token itself
+    uint32_t top = 0;
 #pragma unroll
-    for (int c = 0; c < kS; ++c) {
+    for (int u = 0; u < kVUnits; ++u) {
+      const int at = tile_at<WC>(vr, vq) + u * kVApart * (2 * WC);
+      static_assert(kVApart % 16 == 0, "the same swizzle");
+      if constexpr (KV == kBf16 && !STATE) {
+        const v4i w = {static_cast<int>(wv[u][0]), static_cast<int>(wv[u][1]), static_cast<int>(wv[u][2]), static_cast<int>(wv[u][3])};
+        *reinterpret_cast<v4i*>(&v_t[0][at]) = w;
 #pragma unroll
-      for (int f = 0; f < ET; ++f) operand<KV>([&](int j) { return element(wv[c][j], rv.f32(), f); }, vf[c][f]);
-      if constexpr (!STATE) {
+        for (int j = 0; j < 4; ++j) look_bf16(wv[u][j], top);
+      } else {
+        float x[8];
+        unit_values<KV>(wv[u], rv.f32(), x);
+        v4i f[NV];
+        if constexpr (STATE) {
+          const float w = alpha * pr[vr + u * kVApart + C - tc + last];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) look<ET>(wv[c][j], rv.f32(), bad);
-      }
-    }
-    if (!STATE && __any(not_finite(bad)) && lane == 0) s_bad[flag] = 1;
-    // weighted transposed keys: decays to the next chunk's first token, or to
-    // the last one
-    if (has_k) {
-      float wt[4];
+          for (int j = 0; j < 8; ++j) x[j] *= w;
+        } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int to = tc - (32 * kc + 16 * kj + 4 * g + r) - (last ? 1 : 0);
-        wt[r] = alpha * pw[to > 0 ? to : 0];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float y[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = element(wk[r], rk.f32(), i).value() * wt[r];
-#pragma unroll
-        for (int k = 0; k < NKT; ++k) {
-          const uint2 u = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-          reinterpret_cast<uint2*>(&k_lds[STATE ? flag : 0][((kx * 4 + i) * kS + kc) * NKT + k][lane])[kj] = u;
-          y[0] -= bf16_lo(u.x);
-          y[1] -= bf16_hi(u.x);
-          y[2] -= bf16_lo(u.y);
-          y[3] -= bf16_hi(u.y);
+          for (int j = 0; j < 8; ++j) top = max(top, (__float_as_uint(x[j]) & 0x7FFFFFFFu) >> 16);
         }
+        split8<NV>(x, f);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) *reinterpret_cast<v4i*>(&v_t[k][at]) = f[k];
       }
     }
-    if constexpr (!STATE) {
-      if (has_q) {
+    if (!STATE && __any(not_finite(top)) && lane == 0) s_bad[flag] = 1;
+    const auto put = [&](auto kind, const auto& w, bool f32, auto& t) {
+      constexpr Kind K = decltype(kind)::value;
+      constexpr int N = sizeof(t) / sizeof(t[0]);
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          v4i f[NQ];
-          operand<KQ>([&](int j) { return element(wq, rq.f32(), 4 * (j % 4) + 2 * hh + j / 4); }, f);
-#pragma unroll
-          for (int k = 0; k < NQ; ++k) q_lds[((qt * kX + qx) * 2 + hh) * NQ + k][lane] = f[k];
+      for (int u = 0; u < kKUnits; ++u) {
+        const int at = tile_at<DK>(kr + u * kKApart, kq);
+        v4i f[N];
+        if constexpr (K == kBf16) {
+          f[0] = v4i{static_cast<int>(w[u][0]), static_cast<int>(w[u][1]), static_cast<int>(w[u][2]), static_cast<int>(w[u][3])};
+        } else {
+          float x[8];
+          unit_values<K>(w[u], f32, x);
+          split8<N>(x, f);
         }
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          if (k_on) *reinterpret_cast<v4i*>(&t[k][at]) = f[k];
       }
-    }
-  };
-  // the rows of the chunk at i0, where there is one
-  const auto load = [&](int64_t i0) {
-    if (i0 < end) load_most(i0, tokens_at(i0));
+    };
+    put(KindOf<KK>{}, wk, rk.f32(), k_t);
+    if constexpr (!STATE) put(KindOf<KQ>{}, wq, rq.f32(), q_t);
   };
 
   // Two barriers per chunk: the products of staged operands lie between them
-  // (keys x queries, queries x state, the state's update), what follows from
-  // other waves' products (products x values) and the next chunk's staging
-  // behind them.  Whether a chunk's values are finite is told in two flags in
-  // turn: one is cleared while the other is read.
+  // (keys x queries, state x queries, the state's update), what needs other
+  // waves' products (values x products) and the next chunk's staging behind
+  // them.  Whether a chunk's values are finite is told in two flags in turn:
+  // one is cleared while the other is read.
   int64_t i0 = begin;
-  int tc = tokens_at(i0), flag = 0;
-  stage(i0, tc, flag);
-  for (;;) {
+  int tc = some ? tokens_at(i0) : 0, flag = 0;
+  if (some) stage(i0, tc, flag);
+  while (some) {
     const int64_t next = i0 + tc;
-    if (kEarly) load(next);
+    if (next < end) load(next, tokens_at(next));
     lds_barrier();
     const bool last = next == p.T && !p.rev;
 
-    v4f o[kOwn][ET];
+    v4f o[STATE ? 1 : kT];
+    v4i vf[kS][NV];
     if constexpr (!STATE) {
       const bool redo = tc > 1 && __builtin_amdgcn_readfirstlane(s_bad[flag]) != 0;
       if (threadIdx.x == 0) s_bad[flag ^ 1] = 0;
@@ -483,53 +411,50 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
         lds_barrier();
         tc = 1;
         flag ^= 1;
-        load_most(i0, 1);
-        load_keys(i0, 1);
+        load(i0, 1);
         stage(i0, 1, flag);
         continue;
       }
-      const auto query = [&](int t, int x, int hh, v4i (&f)[NQ]) {
+      const auto query = [&](int t, int x, v4i (&f)[NQ]) {
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) f[k] = q_lds[((t * kX + x) * 2 + hh) * NQ + k][lane];
+        for (int k = 0; k < NQ; ++k) f[k] = tile_read(q_t[k], (k_row ^ (x << 6)) + t * 16 * (2 * DK));
       };
       // --- keys x queries, decayed
-      constexpr int kU = (kT + kPer - 1) / kPer;
-      if (has_p) {
+      if (ps + pt < kT) {
         v4f acc[kU];
 #pragma unroll
         for (int u = 0; u < kU; ++u) acc[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int x = 0; x < kX; ++x)
+        for (int x = 0; x < kB; ++x) {
+          v4i kf[NK];
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            v4i kf[NK];
-            operand<KK>([&](int j) { return element(wn[x], rk.f32(), 4 * (j % 4) + 2 * hh + j / 4); }, kf);
+          for (int k = 0; k < NK; ++k) kf[k] = tile_read(k_t[k], (k_row ^ (x << 6)) + ps * 16 * (2 * DK));
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-              const int t = ps + pt + u * kPer;
-              if (t >= kT) continue;
-              v4i f[NQ];
-              query(t, x, hh, f);
-              acc[u] = mma<MODE>(kf, f, acc[u]);
-            }
+          for (int u = 0; u < kU; ++u) {
+            const int t = ps + pt + u * kPer;
+            if (t >= kT) continue;
+            v4i f[NQ];
+            query(t, x, f);
+            acc[u] = mma<MODE>(kf, f, acc[u]);
           }
+        }
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
           const int t = ps + pt + u * kPer;
           if (t >= kT) continue;
+          // decay from key 16 ps + 4 g + r to query 16 t + n; none from later keys
+          const float* const w = &pr[C - 16 * (t - ps) - n + 4 * g];
           float y[4];
-          if (t == ps) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = n >= 4 * g + r ? acc[u][r] * w_diag[r] : 0.0f;
-          } else {
-            const float wx = pw[16 * (t - ps - 1)];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = acc[u][r] * (w_off[r] * wx);
+          for (int r = 0; r < 4; ++r) {
+            y[r] = acc[u][r] * (alpha * beta * w[r]);
+            if (t == ps && n < 4 * g + r) y[r] = 0.0f;
           }
+          const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + t * 16 * (2 * C) + 8 * (g & 1);
 #pragma unroll
           for (int k = 0; k < MODE; ++k) {
             const uint2 v = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            reinterpret_cast<uint2*>(&p_lds[(t * kS + ps / 2) * MODE + k][lane])[ps & 1] = v;
+            *reinterpret_cast<uint2*>(&p_t[k][at]) = v;
             y[0] -= bf16_lo(v.x);
             y[1] -= bf16_hi(v.x);
             y[2] -= bf16_lo(v.y);
@@ -537,120 +462,100 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
           }
         }
       }
-      if ((ps & 1) && pt == 1) {  // the half of an operand that no tile fills
+      if ((ps & 1) && pt == (kPer > 1 ? 1 : 0)) {  // the half of an operand that no tile fills
+        const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + (ps - 1) * 16 * (2 * C) + 8 * (g & 1);
 #pragma unroll
-        for (int k = 0; k < MODE; ++k)
-          reinterpret_cast<uint2*>(&p_lds[((ps - 1) * kS + ps / 2) * MODE + k][lane])[1] = make_uint2(0u, 0u);
+        for (int k = 0; k < MODE; ++k) *reinterpret_cast<uint2*>(&p_t[k][at]) = make_uint2(0u, 0u);
       }
-      if (kEarly && next < end) load_keys(next, tokens_at(next));
-
-      // --- queries x the wave's half of the state; what other waves finish
+      // --- state x queries
       if (ewave) {
-        v4f a[kT][ET];
 #pragma unroll
-        for (int t = 0; t < kT; ++t)
+        for (int t = 0; t < kT; ++t) o[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int f = 0; f < ET; ++f) a[t][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int x = 0; x < kB; ++x) {
+          v4i sf[MODE];
+          float y[8];
 #pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          v4i sf[ET][MODE];
-#pragma unroll
-          for (int f = 0; f < ET; ++f) {
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = st[x][j / 4][f][j % 4];
-            split8<MODE>(y, sf[f]);
-          }
+          for (int j = 0; j < 8; ++j) y[j] = st[x][j / 4][j % 4];
+          split8<MODE>(y, sf);
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
-            v4i q[NQ];
-            query(t, x, half, q);
-#pragma unroll
-            for (int f = 0; f < ET; ++f) a[t][f] = mma<MODE>(q, sf[f], a[t][f]);
+            v4i f[NQ];
+            query(t, x, f);
+            o[t] = mma<MODE>(sf, f, o[t]);
           }
         }
-        // tiles 0 and 3 (of 4) or 0 (of 2) are finished by waves 0-3
 #pragma unroll
-        for (int u = 0; u < kOwn; ++u)
-#pragma unroll
-          for (int f = 0; f < ET; ++f) {
-            const int t0 = kT == 4 ? 3 * u : u, t1 = kT == 4 ? 1 + u : 1;
-            o[u][f] = half ? a[t1][f] : a[t0][f];
-            o_lds[((wave ^ 4) * kOwn + u) * ET + f][lane] = half ? a[t0][f] : a[t1][f];
-          }
+        for (int t = 0; t < kT; ++t) o[t] *= beta * pr[C - 16 * t - n];
       }
-      // the next chunk's rows, in the registers that the sums over all tiles had
-      if (!kEarly) load(next);
     }
 
     // --- keys x values into the state
     if (ewave) {
-      const float w = pw[last ? tc - 1 : tc];
 #pragma unroll
-      for (int x = 0; x < kX; ++x)
+      for (int c = 0; c < kS; ++c)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) vf[c][k] = tile_turn8(v_t[k], v_a0 + c * 32 * (2 * WC), v_a1 + c * 32 * (2 * WC));
+      // decayed, with the decays to the next chunk's first token or to the last one
+      v4i wf[kS][NKT];
+#pragma unroll
+      for (int c = 0; c < kS; ++c) {
+        if constexpr (STATE) {
+#pragma unroll
+          for (int k = 0; k < NKT; ++k) wf[c][k] = vf[c][k];
+        } else {
+          const float* const w = &pr[32 * c + 8 * g + C - tc + (last ? 1 : 0)];
+          float y[8];
+          sum8<NV>(vf[c], y);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] *= alpha * w[j];
+          split8<NKT>(y, wf[c]);
+        }
+      }
+      const float w = pr[C - tc + (last ? 1 : 0)];
+#pragma unroll
+      for (int x = 0; x < kB; ++x)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-#pragma unroll
-          for (int f = 0; f < ET; ++f)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) st[x][i][f][r] *= w;
+          st[x][i] *= w;
 #pragma unroll
           for (int c = 0; c < kS; ++c) {
-            v4i k[NKT];
+            v4i f[NK];
 #pragma unroll
-            for (int y = 0; y < NKT; ++y) k[y] = k_lds[STATE ? flag : 0][((x * 4 + 2 * half + i) * kS + c) * NKT + y][lane];
-#pragma unroll
-            for (int f = 0; f < ET; ++f) st[x][i][f] = mma<NKT>(k, vf[c][f], st[x][i][f]);
+            for (int k = 0; k < NK; ++k)
+              f[k] = tile_turn8(k_t[k], (k_a0 ^ (x << 6)) + 8 * i + c * 32 * (2 * DK), (k_a1 ^ (x << 6)) + 8 * i + c * 32 * (2 * DK));
+            st[x][i] = mma<NKT>(f, wf[c], st[x][i]);
           }
         }
     }
 
+    lds_barrier();
     if constexpr (!STATE) {
-      if (!kEarly && next < end) load_keys(next, tokens_at(next));
-      lds_barrier();
       if (ewave) {
+        // --- values x products
 #pragma unroll
-        for (int u = 0; u < kOwn; ++u) {
-          const int t = kT == 4 ? (half ? 1 + u : 3 * u) : half;
-          const float wx = pw[16 * t];
-#pragma unroll
-          for (int f = 0; f < ET; ++f) {
-            const v4f more = o_lds[(wave * kOwn + u) * ET + f][lane];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[u][f][r] = (o[u][f][r] + more[r]) * (w_row[r] * wx);
-          }
-          // --- products x values
+        for (int t = 0; t < kT; ++t)
 #pragma unroll
           for (int c = 0; c < kS; ++c) {
             if (2 * c > t) continue;
             v4i f[MODE];
 #pragma unroll
-            for (int k = 0; k < MODE; ++k) f[k] = p_lds[(t * kS + c) * MODE + k][lane];
-#pragma unroll
-            for (int e = 0; e < ET; ++e) o[u][e] = mma<MODE>(f, vf[c][e], o[u][e]);
+            for (int k = 0; k < MODE; ++k) f[k] = tile_read(p_t[k], (p_row ^ (c << 6)) + t * 16 * (2 * C));
+            o[t] = mma<MODE>(vf[c], f, o[t]);
           }
-        }
-        // --- store
+        // --- store: columns w0 + 4 g + r of token 16 t + n
         const int size = OF32 ? 4 : 2, ld = static_cast<int>(p.ldo) * size;
         const auto ro = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.o) + (first_row(i0, tc) * p.ldo + h * p.Dv) * size,
                                                           0, (tc - 1) * ld + p.Dv * size, kBufferWord3);
         const int step = p.rev ? -ld : ld;
-        uint32_t at = eon ? static_cast<uint32_t>((p.rev ? (tc - 1) * ld : 0) + 4 * g * step + e0 * size) : kOff;
-        asm volatile("" : "+v"(at));
+        const uint32_t at = static_cast<uint32_t>((p.rev ? (tc - 1) * ld : 0) + n * step + (w0 + 4 * g) * size);
 #pragma unroll
-        for (int u = 0; u < kOwn; ++u) {
-          const int t = kT == 4 ? (half ? 1 + u : 3 * u) : half;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t off = at + static_cast<uint32_t>((16 * t + r) * step);
-            if constexpr (OF32) {
-              if constexpr (ET == 2)
-                __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(o[u][0][r]), __float_as_uint(o[u][1][r])}, ro, off, 0, 0);
-              else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(o[u][0][r]), ro, off, 0, 0);
-            } else {
-              if constexpr (ET == 2) __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(o[u][0][r], o[u][1][r]), ro, off, 0, 0);
-              else __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(pack_bf16(o[u][0][r], 0.0f)), ro, off, 0, 0);
-            }
+        for (int t = 0; t < kT; ++t) {
+          const uint32_t off = at + static_cast<uint32_t>(16 * t * step);
+          if constexpr (OF32) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o[t]), ro, off, 0, 0);
+          } else {
+            __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(o[t][0], o[t][1]), pack_bf16(o[t][2], o[t][3])}, ro, off, 0, 0);
           }
         }
       }
@@ -664,45 +569,51 @@ __global__ __launch_bounds__(512) void linattn_chunk_kernel(const LinattnPass p)
 
   // the segment's own sum, or the state after the last token
   float* out = nullptr;
-  int64_t od = p.Dv, oe = 1;
-  if (STATE) {
-    out = p.joined + (static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk * p.Dv;
-  } else if (p.s_out != nullptr && seg + 1 == p.nseg) {
-    out = p.s_out + static_cast<int64_t>(bh) * p.Dk * p.Dv;
-    od = p.in_d;
-    oe = p.in_e;
-  }
-  if (out != nullptr && eon) {
+  if (STATE) out = p.s_out + (static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk * p.Dv;
+  else if (p.s_out != nullptr && seg + 1 == p.nseg) out = p.s_out + static_cast<int64_t>(bh) * p.Dk * p.Dv;
+  if (out != nullptr) {
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(out, 0, p.Dk * p.Dv * 4, kBufferWord3);
 #pragma unroll
-    for (int x = 0; x < kX; ++x)
+    for (int x = 0; x < kB; ++x)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        const int d = 32 * x + 8 * g + 4 * i;
+        const uint32_t at = ewave && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.Dv + w0 + n) : kOff;
 #pragma unroll
-        for (int f = 0; f < ET; ++f)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int d = 64 * x + 4 * pi<kFours>(4 * g + r) + 2 * half + i;
-            if (d < p.Dk) out[d * od + (e0 + f) * oe] = st[x][i][f][r];
-          }
+        for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[x][i][r]), rs, at + 4u * r * p.Dv, 0, 0);
+      }
   }
 }
 
-constexpr int chunk_tokens(int DK, Kind K, bool STATE) { return DK == 256 || (K != kBf16 && !STATE) ? 32 : 64; }
+// bf16 operands take chunks of 64 tokens, fp32's parts of 32, as do Dk above 128:
+// what LDS holds for two workgroups on a compute unit.
+constexpr int chunk_tokens(int DK, Kind K) { return DK >= 128 || K != kBf16 ? 32 : 64; }
 
+// `n` passes of the same widths, in 64s, and waves.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
-hipError_t launch_pass(const LinattnPass& p, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(p.B * p.H * p.nseg * p.tiles));
+hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
+  LinattnPasses ps{};
+  uint32_t groups = 0;
+  for (int i = 0; i < 3; ++i) {
+    ps.first[i] = groups;
+    if (i >= n) {
+      ps.first[i] = 0xFFFFFFFFu;
+      continue;
+    }
+    ps.p[i] = p[i];
+    groups += p[i].B * p[i].H * p[i].nseg * p[i].tiles;
+  }
   const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(512), 0, stream, p);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * p->waves), 0, stream, ps);
     return hipGetLastError();
   };
-#define MMF_DIMS(DK)                                                                                          \
-  return p.et == 1 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 1, chunk_tokens(DK, KQ, STATE), STATE>)    \
-                   : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 2, chunk_tokens(DK, KQ, STATE), STATE>)
-  if (p.Dk <= 64) MMF_DIMS(64);
-  if (p.Dk <= 128) MMF_DIMS(128);
+#define MMF_DIMS(DK)                                                                                                     \
+  return p->waves == 4 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 4, chunk_tokens(DK, KQ), STATE>) \
+                       : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 8, chunk_tokens(DK, KQ), STATE>)
+  if (p->Dk <= 64) MMF_DIMS(64);
+  if (p->Dk <= 128) MMF_DIMS(128);
+  MMF_DIMS(256);
 #undef MMF_DIMS
-  return go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, 256, 1, chunk_tokens(256, KQ, STATE), STATE>);
 }
 
 }  // namespace la

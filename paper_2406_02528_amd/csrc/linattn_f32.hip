@@ -1,10 +1,13 @@
-// Linear attention over chunks: fp32 inputs and outputs.
+// Linear attention over chunks: fp32 operands; o in fp32, and the states' sums.
 #include "linattn_chunk.h"
 
 namespace mmf {
-hipError_t launch_linattn_f32(const LinattnPass& p, bool state, hipStream_t stream) {
+hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return state ? launch_pass<kF32, kF32, kF32, true, 3, 3, true>(p, stream)
-               : launch_pass<kF32, kF32, kF32, true, 3, 3, false>(p, stream);
+  return launch_passes<kF32, kF32, kF32, true, 3, 3, false>(p, n, stream);
+}
+hipError_t launch_linattn_states_f32(const LinattnPass* p, int n, hipStream_t stream) {
+  using namespace la;
+  return launch_passes<kF32, kF32, kF32, true, 3, 3, true>(p, n, stream);
 }
 }  // namespace mmf
