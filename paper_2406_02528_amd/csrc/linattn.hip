@@ -64,20 +64,32 @@ __global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const Joins a)
   // a sum that nothing follows is not there unless s_out is wanted
   const uint32_t have = j.s_out != nullptr ? a.n : a.n - a.sub;
   const float full = static_cast<float>(power(l, a.tokens));
-  constexpr int kJoinAhead = 32 / N;   // loads in flight
-  for (uint32_t s = 0; s < a.n; s += kJoinAhead) {
-    vec v[kJoinAhead];
+  constexpr uint32_t kAhead = 32 / N;   // loads in flight
+  const float* from = u;
+  float* to = u;
+  uint32_t skip = 0;   // sums until the next state that is wanted
+  for (uint32_t s = 0; s < a.n; s += kAhead) {
+    vec v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i)
-      if (s + i < have) v[i] = load(u + (s + i) * a.size);
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      if (s + i < have) v[i] = load(from);
+      from += a.size;
+    }
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
+    for (uint32_t i = 0; i < kAhead; ++i) {
       if (s + i >= a.n) break;
-      if ((s + i) % a.sub == 0) *reinterpret_cast<vec*>(u + (s + i) * a.size) = e;
+      if (skip == 0) {
+        *reinterpret_cast<vec*>(to) = e;
+        skip = a.sub;
+      }
+      to += a.size;
+      --skip;
       if (s + i >= have) continue;
-      const int64_t left = a.T - (s + i) * a.tokens;   // tokens from here on
       float w = full;
-      if (left <= a.tokens) w = left <= 0 ? 1.0f : static_cast<float>(power(l, j.rev ? left : left - 1));
+      if (s + i + a.sub >= a.n) {   // the last segment: fewer tokens, or none
+        const int64_t left = a.T - (s + i) * a.tokens;
+        if (left <= a.tokens) w = left <= 0 ? 1.0f : static_cast<float>(power(l, j.rev ? left : left - 1));
+      }
 #pragma unroll
       for (int c = 0; c < N; ++c) e[c] = fmaf(w, e[c], v[i][c]);
     }
@@ -96,14 +108,17 @@ uint32_t tiles_of(int Dv) {
   const int w = 16 * waves_of(Dv);
   return static_cast<uint32_t>((Dv + w - 1) / w);
 }
-Plan plan_of(int64_t T, int64_t groups, int passes) {
+// state_bytes: of all the states that enter one segment.
+Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
   constexpr int64_t C = 64;
   const int64_t chunks = (T + C - 1) / C;
-  // rounds of workgroups x (chunks of a segment + about 3 for its start), and
-  // half as much again with the states' sums and their joining
+  // In tenths of a us: a chunk takes about 8 where a compute unit has one
+  // workgroup, two of them 12; a start 10; with segments, their sums about half
+  // of a pass each, and their states are written and read twice, at 4.5 TB/s.
   const auto cost = [&](int64_t s) {
-    const int64_t per = (chunks + s - 1) / s, rounds = (groups * passes * s + kSlots - 1) / kSlots;
-    return s == 1 ? 2 * rounds * (per + 3) : 3 * rounds * (per + 3) + 4;
+    const int64_t per = (chunks + s - 1) / s, each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
+    const int64_t work = each / 2 * (120 * per + 100) + each % 2 * (78 * per + 100);
+    return s == 1 && passes == 1 ? work : work + work / 3 + state_bytes * s * 4 / 450000 + 100;
   };
   int64_t best = 1;
   for (int64_t s = 2; s <= chunks && groups * (s - 1) < 2 * kSlots; ++s)
@@ -112,13 +127,14 @@ Plan plan_of(int64_t T, int64_t groups, int passes) {
   Plan plan;
   plan.nseg = static_cast<uint32_t>((chunks + per - 1) / per);
   plan.seg_tokens = per * C;
-  plan.sub = per % 2 == 0 && groups * plan.nseg <= kSlots ? 2 : 1;
+  plan.sub = 1;
+  while (per % (2 * plan.sub) == 0 && 2 * groups * plan.nseg * plan.sub <= kSlots / 2) plan.sub *= 2;
   return plan;
 }
-Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), 1); }
+Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), 1, 4 * B * H * dk * dv); }
 Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv) {
   const uint32_t a = tiles_of(dv), b = tiles_of(dk);
-  return plan_of(T, B * H * (a > b ? a : b), 3);
+  return plan_of(T, B * H * (a > b ? a : b), 3, 8 * B * H * dk * dv);
 }
 size_t sums_bytes(const Plan& plan, int64_t states, int dk, int dv) {
   return sizeof(float) * static_cast<size_t>(states) * plan.nseg * plan.sub * dk * dv;

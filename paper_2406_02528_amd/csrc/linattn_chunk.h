@@ -151,15 +151,24 @@ struct Rows {
   int width;
   bool f32_;
   __device__ __forceinline__ bool f32() const { return K == kEither ? f32_ : K == kF32; }
-  // `tc` rows from row `row` of head h, whose entries are `w`.
-  __device__ __forceinline__ void at(const LinattnOperand& x, int64_t row, int tc, int64_t h, int w, bool rev) {
+  char* seq;        // the head's entries of the sequence's first row
+  // Head h, whose entries are `w`, of the rows from `row` on.  Kept in registers:
+  // fetched again for each chunk, the arguments would be waited for each time.
+  __device__ __forceinline__ void init(const LinattnOperand& x, int64_t row, int64_t h, int w, bool rev) {
     f32_ = x.is_f32;
-    const int size = f32() ? 4 : 2, ld = static_cast<int>(x.ld) * size;
+    const int size = f32() ? 4 : 2;
     width = w;
-    step = rev ? -ld : ld;
-    base = rev ? static_cast<uint32_t>((tc - 1) * ld) : 0u;
-    char* const p = const_cast<char*>(static_cast<const char*>(x.p)) + (row * x.ld + h * w) * size;
-    r = __builtin_amdgcn_make_buffer_rsrc(p, 0, (tc - 1) * ld + w * size, kBufferWord3);
+    step = static_cast<int>(x.ld) * (rev ? -size : size);
+    seq = const_cast<char*>(static_cast<const char*>(x.p)) + (row * x.ld + h * w) * size;
+    uint64_t s = reinterpret_cast<uint64_t>(seq);
+    asm volatile("" : "+s"(s), "+s"(step), "+s"(width));
+    seq = reinterpret_cast<char*>(s);
+  }
+  // `tc` of them from row `row`.
+  __device__ __forceinline__ void at(int64_t row, int tc) {
+    const int ld = step < 0 ? -step : step;
+    base = step < 0 ? static_cast<uint32_t>((tc - 1) * ld) : 0u;
+    r = __builtin_amdgcn_make_buffer_rsrc(seq + row * ld, 0, (tc - 1) * ld + width * (f32() ? 4 : 2), kBufferWord3);
   }
   // Units of 8 elements: those of `threads` threads from token i, column d on,
   // U of them `apart` tokens from each other.
@@ -213,7 +222,7 @@ __device__ __forceinline__ bool not_finite(uint32_t top) { return (top & 0xFFFFu
 // each.  STATE: the segment's own sum only (no queries, no o; the values go to
 // LDS decayed).
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int C, bool STATE>
-__global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
+__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
   constexpr int kThreads = 64 * WAVES, WC = 16 * WAVES;
   constexpr int kB = DK / 32;        // contraction steps over Dk
   constexpr int kT = C / 16;         // tiles of tokens
@@ -222,6 +231,9 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   constexpr int kU = (kT + kPer - 1) / kPer;
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
   constexpr int NV = STATE ? NKT : KV == kBf16 ? 1 : MODE;
+  // A chunk's rows are asked for before the products of the chunk before; of fp32
+  // the queries behind them, which leaves the products their registers.
+  constexpr bool kEarly = STATE || KQ == kBf16;
   // units of 8 elements per thread (half the threads have one where a chunk has fewer)
   constexpr bool kHalf = C * DK / 8 < kThreads;
   constexpr int kKUnits = kHalf ? 1 : C * DK / 8 / kThreads, kVUnits = C * WC / 8 / kThreads;
@@ -254,7 +266,10 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
     const int64_t left = end - i;
     return i < single ? 1 : left < C ? static_cast<int>(left) : C;
   };
-  const auto first_row = [&](int64_t i0, int tc) { return b * p.T + (p.rev ? p.T - i0 - tc : i0); };
+  const bool rev = p.rev;
+  int64_t T = p.T;
+  asm volatile("" : "+s"(T));
+  const auto first_row = [&](int64_t i0, int tc) { return rev ? T - i0 - tc : i0; };   // in the sequence
 
   // --- a chunk's rows into registers
   const int kr = threadIdx.x / (DK / 8), kq = threadIdx.x % (DK / 8);   // row and chunk of the thread's first unit
@@ -265,19 +280,31 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   Rows<KQ> rq;
   Rows<KK> rk;
   Rows<KV> rv;
+  Rows<OF32 ? kF32 : kBf16> ro;      // of the output
+  rk.init(p.k, b * T, h, p.Dk, rev);
+  rv.init(p.v, b * T, h, p.Dv, rev);
+  if constexpr (!STATE) {
+    rq.init(p.q, b * T, h, p.Dk, rev);
+    ro.init({p.o, p.ldo, OF32}, b * T, h, p.Dv, rev);
+  }
   const auto load = [&](int64_t i0, int tc) {
     const int64_t row = first_row(i0, tc);
-    rk.at(p.k, row, tc, h, p.Dk, p.rev);
-    rk.load(kr, k_on ? 8 * kq : p.Dk, kKApart, wk);
-    rv.at(p.v, row, tc, h, p.Dv, p.rev);
+    rk.at(row, tc);
+    rk.load(kr, k_on ? 8 * kq : rk.width, kKApart, wk);
+    rv.at(row, tc);
     rv.load(vr, c0 + 8 * vq, kVApart, wv);
+  };
+  const auto load_queries = [&](int64_t i0, int tc) {
     if constexpr (!STATE) {
-      rq.at(p.q, row, tc, h, p.Dk, p.rev);
-      rq.load(kr, k_on ? 8 * kq : p.Dk, kKApart, wq);
+      rq.at(first_row(i0, tc), tc);
+      rq.load(kr, k_on ? 8 * kq : rq.width, kKApart, wq);
     }
   };
   const bool some = begin < end;   // a segment of a pass for states may have no tokens
-  if (some) load(begin, tokens_at(begin));
+  if (some) {
+    load(begin, tokens_at(begin));
+    load_queries(begin, tokens_at(begin));
+  }
 
   // powers of l: fp64, by squaring (any l, 0 among them)
   for (int i = threadIdx.x; i < 2 * C + 2; i += kThreads) {
@@ -323,8 +350,10 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   }
   lds_barrier();
 
-  const float alpha = p.alpha, beta = p.beta;
-  // lane's places in the tiles
+  float alpha = p.alpha, beta = p.beta;
+  asm volatile("" : "+s"(alpha), "+s"(beta));
+  // lane's places in the tiles (those with other steps over Dk are taken from
+  // them anew for each chunk, not kept in registers)
   const int k_row = tile_at<DK>(n, g);                                        // along: row n, slots 8 g + j
   const int p_row = tile_at<C>(n, g);
   const int t_row = 8 * g + (n >> 2);                                         // across: rows 8 g .. + 3, + 4 .. + 7
@@ -333,9 +362,23 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   const int v_a1 = tile_at<WC>(t_row + 4, 2 * wave + ((n & 3) >> 1)) + 8 * (n & 1);
   const int ps = wave % kT, pt = wave / kT;   // the wave's tile of keys, and its first tile of queries behind it
 
+  // The state's decay is kept beside it, as `held`: what the registers hold times
+  // held is the state.  Where the factor leaves the range that fp32 has to spare
+  // the registers take it over.
+  float held = 1.0f;
+  const auto next_held = [&](int tc, int last) {   // behind a chunk; 1: the registers take it over
+    const float x = held * pr[C - tc + last], a = __builtin_fabsf(x);
+    return a > 0x1p-20f && a < 0x1p20f ? x : 1.0f;
+  };
+  const auto take_over = [&](float by) {
+#pragma unroll
+    for (int x = 0; x < kB; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) st[x][i] *= by;
+  };
   // --- a chunk's rows from registers to LDS; whether its values are finite
   const auto stage = [&](int64_t i0, int tc, int flag) {
-    const int last = i0 + tc == p.T && !p.rev ? 1 : 0;  // the state behind the last token itself
+    const int last = i0 + tc == T && !rev ? 1 : 0;  // the state behind the last token itself
     uint32_t top = 0;
 #pragma unroll
     for (int u = 0; u < kVUnits; ++u) {
@@ -351,7 +394,7 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
         unit_values<KV>(wv[u], rv.f32(), x);
         v4i f[NV];
         if constexpr (STATE) {
-          const float w = alpha * pr[vr + u * kVApart + C - tc + last];
+          const float w = alpha * __builtin_amdgcn_rcpf(next_held(tc, last)) * pr[vr + u * kVApart + C - tc + last];
 #pragma unroll
           for (int j = 0; j < 8; ++j) x[j] *= w;
         } else {
@@ -397,10 +440,15 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   if (some) stage(i0, tc, flag);
   while (some) {
     const int64_t next = i0 + tc;
-    if (next < end) load(next, tokens_at(next));
+    if (next < end) {
+      load(next, tokens_at(next));
+      if (kEarly) load_queries(next, tokens_at(next));
+    }
     lds_barrier();
-    const bool last = next == p.T && !p.rev;
+    const bool last = next == T && !rev;
 
+    int k_row_ = k_row, k_a0_ = k_a0, k_a1_ = k_a1;
+    asm volatile("" : "+v"(k_row_), "+v"(k_a0_), "+v"(k_a1_));
     v4f o[STATE ? 1 : kT];
     v4i vf[kS][NV];
     if constexpr (!STATE) {
@@ -412,12 +460,13 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
         tc = 1;
         flag ^= 1;
         load(i0, 1);
+        load_queries(i0, 1);
         stage(i0, 1, flag);
         continue;
       }
       const auto query = [&](int t, int x, v4i (&f)[NQ]) {
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) f[k] = tile_read(q_t[k], (k_row ^ (x << 6)) + t * 16 * (2 * DK));
+        for (int k = 0; k < NQ; ++k) f[k] = tile_read(q_t[k], (k_row_ ^ (x << 6)) + t * 16 * (2 * DK));
       };
       // --- keys x queries, decayed
       if (ps + pt < kT) {
@@ -428,7 +477,7 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
         for (int x = 0; x < kB; ++x) {
           v4i kf[NK];
 #pragma unroll
-          for (int k = 0; k < NK; ++k) kf[k] = tile_read(k_t[k], (k_row ^ (x << 6)) + ps * 16 * (2 * DK));
+          for (int k = 0; k < NK; ++k) kf[k] = tile_read(k_t[k], (k_row_ ^ (x << 6)) + ps * 16 * (2 * DK));
 #pragma unroll
           for (int u = 0; u < kU; ++u) {
             const int t = ps + pt + u * kPer;
@@ -486,9 +535,13 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
           }
         }
 #pragma unroll
-        for (int t = 0; t < kT; ++t) o[t] *= beta * pr[C - 16 * t - n];
+        for (int t = 0; t < kT; ++t) o[t] *= beta * held * pr[C - 16 * t - n];
       }
     }
+    const float decayed = held * pr[C - tc + (last ? 1 : 0)];
+    held = next_held(tc, last ? 1 : 0);
+    if (__builtin_amdgcn_readfirstlane(held == 1.0f && decayed != 1.0f)) take_over(decayed);
+    const float into = alpha * __builtin_amdgcn_rcpf(held);
 
     // --- keys x values into the state
     if (ewave) {
@@ -508,27 +561,26 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
           float y[8];
           sum8<NV>(vf[c], y);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] *= alpha * w[j];
+          for (int j = 0; j < 8; ++j) y[j] *= into * w[j];
           split8<NKT>(y, wf[c]);
         }
       }
-      const float w = pr[C - tc + (last ? 1 : 0)];
 #pragma unroll
       for (int x = 0; x < kB; ++x)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          st[x][i] *= w;
 #pragma unroll
           for (int c = 0; c < kS; ++c) {
             v4i f[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k)
-              f[k] = tile_turn8(k_t[k], (k_a0 ^ (x << 6)) + 8 * i + c * 32 * (2 * DK), (k_a1 ^ (x << 6)) + 8 * i + c * 32 * (2 * DK));
+              f[k] = tile_turn8(k_t[k], (k_a0_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK), (k_a1_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK));
             st[x][i] = mma<NKT>(f, wf[c], st[x][i]);
           }
         }
     }
 
+    if (!kEarly && next < end) load_queries(next, tokens_at(next));
     lds_barrier();
     if constexpr (!STATE) {
       if (ewave) {
@@ -544,18 +596,15 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
             o[t] = mma<MODE>(vf[c], f, o[t]);
           }
         // --- store: columns w0 + 4 g + r of token 16 t + n
-        const int size = OF32 ? 4 : 2, ld = static_cast<int>(p.ldo) * size;
-        const auto ro = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.o) + (first_row(i0, tc) * p.ldo + h * p.Dv) * size,
-                                                          0, (tc - 1) * ld + p.Dv * size, kBufferWord3);
-        const int step = p.rev ? -ld : ld;
-        const uint32_t at = static_cast<uint32_t>((p.rev ? (tc - 1) * ld : 0) + n * step + (w0 + 4 * g) * size);
+        ro.at(first_row(i0, tc), tc);
+        const uint32_t at = ro.base + static_cast<uint32_t>(n * ro.step + (w0 + 4 * g) * (OF32 ? 4 : 2));
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
-          const uint32_t off = at + static_cast<uint32_t>(16 * t * step);
+          const uint32_t off = at + static_cast<uint32_t>(16 * t * ro.step);
           if constexpr (OF32) {
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o[t]), ro, off, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o[t]), ro.r, off, 0, 0);
           } else {
-            __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(o[t][0], o[t][1]), pack_bf16(o[t][2], o[t][3])}, ro, off, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(o[t][0], o[t][1]), pack_bf16(o[t][2], o[t][3])}, ro.r, off, 0, 0);
           }
         }
       }
@@ -568,6 +617,7 @@ __global__ __launch_bounds__(64 * WAVES, DK == 256 ? 2 : 4) void linattn_chunk_k
   }
 
   // the segment's own sum, or the state after the last token
+  take_over(held);
   float* out = nullptr;
   if (STATE) out = p.s_out + (static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk * p.Dv;
   else if (p.s_out != nullptr && seg + 1 == p.nseg) out = p.s_out + static_cast<int64_t>(bh) * p.Dk * p.Dv;
