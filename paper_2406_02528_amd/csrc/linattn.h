@@ -58,11 +58,10 @@ struct LinattnPass {
   int waves;              // of a workgroup, 16 columns each
   int64_t seg_tokens;
 };
-// Up to three passes of one kernel in a launch, one after the other in its
-// workgroups.
+// Up to three passes of one kernel in a launch, `count` workgroups each.
 struct LinattnPasses {
   LinattnPass p[3];
-  uint32_t first[3];
+  uint32_t n, count;
 };
 size_t linattn_chunk_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv);
 hipError_t launch_linattn_chunk(const LinattnArgs& a, float* joined, hipStream_t stream);

@@ -247,9 +247,14 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
-  const int which = blockIdx.x >= args.first[2] ? 2 : blockIdx.x >= args.first[1] ? 1 : 0;
+  // 8 workgroups of one pass, then the same 8 of the next: a segment's passes run
+  // on one XCD at about the same time and find each other's rows in its L2.
+  const uint32_t whole = args.count / 8 * 8;
+  const uint32_t unit = blockIdx.x / 8, rest = blockIdx.x - whole * args.n;
+  const bool in_whole = blockIdx.x < whole * args.n;
+  const uint32_t which = in_whole ? unit % args.n : rest / (args.count - whole);
   const LinattnPass& p = args.p[which];
-  uint32_t blk = blockIdx.x - args.first[which];
+  uint32_t blk = in_whole ? unit / args.n * 8 + blockIdx.x % 8 : whole + rest % (args.count - whole);
   const uint32_t tile = blk % p.tiles;
   blk /= p.tiles;
   const uint32_t seg = blk % p.nseg;
@@ -639,22 +644,15 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 // what LDS holds for two workgroups on a compute unit.
 constexpr int chunk_tokens(int DK, Kind K) { return DK >= 128 || K != kBf16 ? 32 : 64; }
 
-// `n` passes of the same widths, in 64s, and waves.
+// `n` passes of the same number of workgroups, widths in 64s, and waves.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
 hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
   LinattnPasses ps{};
-  uint32_t groups = 0;
-  for (int i = 0; i < 3; ++i) {
-    ps.first[i] = groups;
-    if (i >= n) {
-      ps.first[i] = 0xFFFFFFFFu;
-      continue;
-    }
-    ps.p[i] = p[i];
-    groups += p[i].B * p[i].H * p[i].nseg * p[i].tiles;
-  }
+  for (int i = 0; i < n; ++i) ps.p[i] = p[i];
+  ps.n = static_cast<uint32_t>(n);
+  ps.count = p->B * p->H * p->nseg * p->tiles;
   const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * p->waves), 0, stream, ps);
+    hipLaunchKernelGGL(kernel, dim3(ps.count * ps.n), dim3(64 * p->waves), 0, stream, ps);
     return hipGetLastError();
   };
 #define MMF_DIMS(DK)                                                                                                     \
