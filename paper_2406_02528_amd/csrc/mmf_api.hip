@@ -328,10 +328,13 @@ int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
   return MMF_OK;
 }
 
-// Up to this many tokens go through the state one by one.
-constexpr int64_t kLinattnSteps = 16;
+// Up to this many tokens go through the state one by one; more make a chunk.
+// 1 x 16 heads of 128, fp32: 8 tokens 8.8 us one by one, 11.9 as a chunk; 16
+// tokens 13.7 and 12.2; 64 sequences 40 and 47, 62 and 48.  bf16, whose products
+// have a third of the parts: 2 tokens 9.9 and 9.7 (64 sequences 30 and 26; 16 x
+// 2 heads of 256: 9.0 and 12.0), 4 tokens 9.0 and 9.0 (41 and 28; 12.6 and 11.2).
+int64_t linattn_steps(bool f32) { return f32 ? 8 : 2; }
 size_t linattn_fwd_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
-  if (T <= kLinattnSteps) return 0;
   return round_up(mmf::linattn_chunk_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
 }
 
@@ -1270,8 +1273,8 @@ int mmf_linattn_fwd(const void* qkv, int qkv_is_f32, const float* decay, float s
   const mmf::LinattnArgs a{qkv, qkv_is_f32 == 1, decay, scale, s0, o, s_last, B, T, H, static_cast<int>(dk),
                            static_cast<int>(dv)};
   return with_workspace(workspace, workspace_bytes, linattn_fwd_bytes(B, T, H, dk, dv), stream, [&](char* scratch) {
-    return hip_status(T <= kLinattnSteps ? mmf::launch_linattn_step(a, stream)
-                                         : mmf::launch_linattn_chunk(a, reinterpret_cast<float*>(scratch), stream));
+    return hip_status(T <= linattn_steps(a.is_f32) ? mmf::launch_linattn_step(a, stream)
+                                                     : mmf::launch_linattn_chunk(a, reinterpret_cast<float*>(scratch), stream));
   });
 }
 
