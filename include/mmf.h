@@ -578,8 +578,8 @@ int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *co
  * only); s0 [B][H][dk][dv] float32 or NULL (0); s_last [B][H][dk][dv] float32,
  * the state after the last token (NULL: not stored; may be the same array as
  * s0: the state is then updated in place).  No other overlap is allowed.
- * dk and dv: multiples of 16 up to 256; B*H at most 2^20, H (2 dk + dv) at most
- * 2^21 (MMF_ERR_SHAPE).
+ * dk and dv: multiples of 16 up to 256; B*H at most 2^20, B*H dk dv at most 2^33,
+ * H (2 dk + dv) at most 2^21, B*T below 2^31 (MMF_ERR_SHAPE).
  * B == 0 or T == 0 is a no-op, which leaves s_last as it was.  Workspace
  * (256-byte aligned, MMF_ERR_WORKSPACE; mmf_linattn_workspace_bytes, which may
  * be 0) or NULL: then allocated stream-ordered on `stream` and freed there.
@@ -674,7 +674,7 @@ int mmf_beam_reorder(const void *const *states, void *const *outs, const int64_t
  * Rows without an entry have loss 0 and gradient 0, and rows with dloss 0
  * gradient 0, whatever z holds (padding).  Else a row of z with a NaN or +inf,
  * or of -inf alone, gives NaN.  fp32, sums and losses in fp64, rounded once.
- * V up to 2^24, K up to 1024, M up to 2^22 (MMF_ERR_SHAPE); tau must be positive
+ * V up to 2^24, K up to 1024, M below 2^22 (MMF_ERR_SHAPE); tau must be positive
  * and finite (MMF_ERR_ARG).  M == 0 is a no-op.  Allocates nothing.
  */
 int mmf_distill_fwd(const void *z, int z_is_f32, const int32_t *idx, const void *t, int t_is_f32,

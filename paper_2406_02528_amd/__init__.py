@@ -920,7 +920,7 @@ def mmf_beam_select(logits: torch.Tensor, scores: torch.Tensor, done: torch.Tens
     (-1: none)."""
     here = _here()
     is_f32 = _kind(logits, "logits")
-    V = logits.shape[-1]
+    V = logits.shape[-1] if logits.dim() else 0
     _need_here(logits, "logits", logits.dtype, (B * W, V), here)
     _need_here(scores, "scores", torch.float32, (B, W), here)
     if done is not None:
@@ -945,7 +945,7 @@ def _state_ptrs(tensors, name, rows, here):
                 and set(map(_T.size, tensors, itertools.repeat(0))) <= {rows}):
             return (array.array("Q", list(map(_T.data_ptr, tensors))),
                     array.array("q", [n // rows if rows else 0 for n in map(_nbytes_of, tensors)]))
-    except (AttributeError, TypeError, RuntimeError):
+    except (AttributeError, IndexError, TypeError, RuntimeError):
         pass
     for i, t in enumerate(tensors):
         if not isinstance(t, torch.Tensor):
@@ -981,7 +981,7 @@ def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, s
 def _distill_args(z, idx, t, here):
     z_f32, t_f32 = _kind(z, "z"), _kind(t, "t")
     M, V = z.shape
-    K = idx.shape[1]
+    K = t.shape[-1] if t.dim() else 0
     _need_here(z, "z", z.dtype, (M, V), here)
     _need_here(idx, "idx", torch.int32, (M, K), here)
     _need_here(t, "t", t.dtype, (M, K), here)

@@ -314,7 +314,7 @@ int check_grads(const void* const* grads, const int* is_f32, const int64_t* coun
   return MMF_OK;
 }
 
-constexpr int64_t kMaxRows = int64_t(1) << 22;  // workgroups of 1024 threads of a launch
+constexpr int64_t kMaxRows = (int64_t(1) << 22) - 1;  // workgroups of 1024 threads of a launch
 
 // ---- linear attention ----
 constexpr int64_t kMaxStates = int64_t(1) << 20;  // B H: a few workgroups each stay within a launch
@@ -323,6 +323,8 @@ int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
     return MMF_ERR_SHAPE;
   if (B < 0 || T < 0 || H < 1 || B > kMaxMN || T > kMaxMN || (T > 0 && B > kMaxMN / T)) return MMF_ERR_SHAPE;
   if (H > kMaxStates || B > kMaxStates / H) return MMF_ERR_SHAPE;
+  // a lane for each four entries of the states stays within a launch
+  if (B * H * dk * dv > int64_t(1) << 33) return MMF_ERR_SHAPE;
   // 64 rows of fp32 within 2^29 bytes (linattn_chunk.h)
   if (H * (2 * dk + dv) > int64_t(1) << 21) return MMF_ERR_SHAPE;
   return MMF_OK;
