@@ -604,9 +604,11 @@ int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float s
  * than a few tokens: bf16 inputs as they are, everything in fp32 (fp32 inputs,
  * decayed products, states) as sums of bf16 parts, to 2^-16 of each factor
  * where the result is rounded to bf16 and 2^-24 where it is float32.  Inputs
- * should be finite: one that is not reaches its own token and the later ones
- * (backward: the earlier ones) of its sequence and head, there as NaN where the
- * formula has an infinity, and nothing else. */
+ * should be finite (and fp32 ones at most 3.38e38, the largest bf16).  One that
+ * is not reaches, in its sequence and head and as NaN where the formula has an
+ * infinity, what depends on it and nothing else: of k and v, o from its token on
+ * and the last state, and dq likewise; of q and dout, dk and dv up to its token
+ * and ds0; and its own token's outputs. */
 size_t mmf_linattn_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
 int mmf_linattn_bwd(const void *qkv, int qkv_is_f32, const float *decay, float scale,
                     const float *s0, const void *dout, int do_is_f32, const float *ds_last,
