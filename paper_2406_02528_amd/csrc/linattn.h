@@ -55,7 +55,7 @@ struct LinattnPass {
   int64_t T;
   int Dk, Dv;
   uint32_t nseg, tiles;   // segments; workgroups per state
-  int waves;              // of a workgroup, 16 columns each
+  int waves;              // of a workgroup, for 16 columns each: 4 or 8
   int64_t seg_tokens;
 };
 // Up to three passes of one kernel in a launch, `count` workgroups each.

@@ -18,11 +18,11 @@
 // segment's own sum, a second joins them into the states that enter the
 // segments, from which the pass itself starts.
 //
-// A workgroup of 8 (4) waves holds a state of Dk rows and 128 (64) columns in the
-// accumulators of its matrix instructions, 16 columns per wave.  A chunk's rows
-// are read once, 16 bytes of bf16 per lane and row, a chunk ahead of their use,
-// and go to LDS as they are (fp32: as bf16 parts); every operand of the products
-// comes from there, along the rows or, by the transposing read, across them.
+// A workgroup holds a state of Dk rows and 128 (64) columns in the accumulators of
+// its matrix instructions, 16 or 32 columns per wave.  A chunk's rows are read
+// once, 16 bytes of bf16 per lane and row, a chunk ahead of their use, and go to
+// LDS as they are (fp32: as bf16 parts); every operand of the products comes from
+// there, along the rows or, by the transposing read, across them.
 // With v_mfma_f32_16x16x32_bf16 (lane = 16 g + n, g = 0..3, n = 0..15; A: row n,
 // B: column n, eight contraction slots 8 g + j; D: column n, rows 4 g + r):
 //   keys x queries  A: keys as rows, B: queries; D: keys 4 g + r of query n, which
@@ -35,6 +35,14 @@
 // The state's tile (b, h) has row m = entry d = 32 b + 8 (m / 4) + 4 h + m % 4, so
 // that the rows a lane keeps of the two tiles h are the slots d = 32 b + 8 g + j
 // of the operand it is for the next chunk: the state never leaves its registers.
+// The keys x queries are formed once per workgroup: each wave forming its own in
+// registers (keys in the same order) saves a barrier, but took 83 us instead of
+// 76 (16384 bf16 tokens, 16 heads of 128), and 195 instead of 168 for the three
+// passes of 4 x 2048 fp32.
+//
+// A pass over few tokens is bound by what each chunk waits for (loads, LDS, two
+// barriers), over many by HBM: that forward moves 268 MB in 76 us, 3.5 TB/s, after
+// 134 MB in 42 us for the segments' sums.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
 // decayed products, the state, the weighted keys) go to the matrix cores as
@@ -218,17 +226,16 @@ __device__ __forceinline__ void look_bf16(uint32_t w, uint32_t& top) {
 __device__ __forceinline__ bool not_finite(uint32_t top) { return (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u; }
 
 // MODE: parts of fp32 values in the products of o.  NKT: parts of the decayed
-// values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of 16 columns
-// each.  STATE: the segment's own sum only (no queries, no o; the values go to
+// values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns
+// each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no o; the values go to
 // LDS decayed).
-template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int C, bool STATE>
-__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
-  constexpr int kThreads = 64 * WAVES, WC = 16 * WAVES;
+template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int CT, int C, bool STATE>
+__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
+  constexpr int kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
   constexpr int kB = DK / 32;        // contraction steps over Dk
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
-  constexpr int kPer = WAVES / kT;   // waves per tile of keys
-  constexpr int kU = (kT + kPer - 1) / kPer;
+  static_assert(STATE || (kT == 2 && WAVES >= 4), "the products' tiles are a wave's each");
   constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
   constexpr int NV = STATE ? NKT : KV == kBf16 ? 1 : MODE;
   // A chunk's rows are asked for before the products of the chunk before; of fp32
@@ -261,7 +268,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   const uint32_t bh = blk / p.nseg;
   if (STATE && seg >= p.segs) return;
   const int64_t b = bh / p.H, h = bh % p.H;
-  const int c0 = static_cast<int>(tile) * WC, w0 = c0 + 16 * wave;  // first column of the workgroup, of the wave
+  const int c0 = static_cast<int>(tile) * WC, w0 = c0 + 16 * CT * wave;  // first column of the workgroup, of the wave
   const bool ewave = w0 < p.Dv;      // widths are multiples of 16
 
   const int64_t begin = static_cast<int64_t>(seg) * p.seg_tokens;
@@ -323,35 +330,39 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
 
   // --- the state: st[b][h] rows 8 g + 4 h + r of 32 b, column w0 + n
-  v4f st[kB][2];
+  v4f st[CT][kB][2];
   const bool given = !STATE && p.e_in != nullptr;
   const auto re = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<float*>(given ? p.e_in + bh * p.e_bh + seg * p.e_seg : nullptr), 0, given ? p.Dk * p.Dv * 4 : 0, kBufferWord3);
+  // every tile of the state, as f(tile of columns, x, i)
+  const auto each = [&](auto&& f) {
 #pragma unroll
-  for (int x = 0; x < kB; ++x)
+    for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int d = 32 * x + 8 * g + 4 * i;
-      if constexpr (STATE) {
-        st[x][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int x = 0; x < kB; ++x)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f(ct, x, i);
+  };
+  each([&](int ct, int x, int i) {
+    v4f& e = st[ct][x][i];
+    if constexpr (STATE) {
+      e = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    } else {
+      const int d = 32 * x + 8 * g + 4 * i, col = w0 + 16 * ct + n;
+      const uint32_t at = col < p.Dv && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.e_d + col * p.e_e) : kOff;
+      if (p.e_d == 1) {
+        const Words<4> w = load_stream<4, false>(re, at);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = __uint_as_float(w.w[r]);
       } else {
-        const uint32_t at = ewave && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.e_d + (w0 + n) * p.e_e) : kOff;
-        if (p.e_d == 1) {
-          const Words<4> w = load_stream<4, false>(re, at);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) st[x][i][r] = __uint_as_float(w.w[r]);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) st[x][i][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(re, at + 4u * r * p.e_d, 0, 0));
-        }
+        for (int r = 0; r < 4; ++r) e[r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(re, at + 4u * r * p.e_d, 0, 0));
       }
     }
+  });
   if (!STATE && p.e_decay) {
     const float l = p.decay[h];
-#pragma unroll
-    for (int x = 0; x < kB; ++x)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) st[x][i] *= l;
+    each([&](int ct, int x, int i) { st[ct][x][i] *= l; });
   }
   lds_barrier();
 
@@ -363,9 +374,9 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   const int p_row = tile_at<C>(n, g);
   const int t_row = 8 * g + (n >> 2);                                         // across: rows 8 g .. + 3, + 4 .. + 7
   const int k_a0 = tile_at<DK>(t_row, n & 3), k_a1 = tile_at<DK>(t_row + 4, n & 3);
-  const int v_a0 = tile_at<WC>(t_row, 2 * wave + ((n & 3) >> 1)) + 8 * (n & 1);
-  const int v_a1 = tile_at<WC>(t_row + 4, 2 * wave + ((n & 3) >> 1)) + 8 * (n & 1);
-  const int ps = wave % kT, pt = wave / kT;   // the wave's tile of keys, and its first tile of queries behind it
+  const int v_a0 = tile_at<WC>(t_row, 2 * CT * wave + ((n & 3) >> 1)) + 8 * (n & 1);  // (the next 16 columns: ^ 32)
+  const int v_a1 = tile_at<WC>(t_row + 4, 2 * CT * wave + ((n & 3) >> 1)) + 8 * (n & 1);
+  const int ps = wave % kT, pt = ps + wave / kT;   // the wave's tile of keys x queries, if there is one
 
   // The state's decay is kept beside it, as `held`: what the registers hold times
   // held is the state.  Where the factor leaves the range that fp32 has to spare
@@ -375,12 +386,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
     const float x = held * pr[C - tc + last], a = __builtin_fabsf(x);
     return a > 0x1p-20f && a < 0x1p20f ? x : 1.0f;
   };
-  const auto take_over = [&](float by) {
-#pragma unroll
-    for (int x = 0; x < kB; ++x)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) st[x][i] *= by;
-  };
+  const auto take_over = [&](float by) { each([&](int ct, int x, int i) { st[ct][x][i] *= by; }); };
   // --- a chunk's rows from registers to LDS; whether its values are finite
   const auto stage = [&](int64_t i0, int tc, int flag) {
     const int last = i0 + tc == T && !rev ? 1 : 0;  // the state behind the last token itself
@@ -454,8 +460,8 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 
     int k_row_ = k_row, k_a0_ = k_a0, k_a1_ = k_a1;
     asm volatile("" : "+v"(k_row_), "+v"(k_a0_), "+v"(k_a1_));
-    v4f o[STATE ? 1 : kT];
-    v4i vf[kS][NV];
+    v4f o[STATE ? 1 : CT][kT];
+    v4i vf[CT][kS][NV];
     if constexpr (!STATE) {
       const bool redo = tc > 1 && __builtin_amdgcn_readfirstlane(s_bad[flag]) != 0;
       if (threadIdx.x == 0) s_bad[flag ^ 1] = 0;
@@ -474,73 +480,70 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
         for (int k = 0; k < NQ; ++k) f[k] = tile_read(q_t[k], (k_row_ ^ (x << 6)) + t * 16 * (2 * DK));
       };
       // --- keys x queries, decayed
-      if (ps + pt < kT) {
-        v4f acc[kU];
-#pragma unroll
-        for (int u = 0; u < kU; ++u) acc[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      if (pt < kT) {
+        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int x = 0; x < kB; ++x) {
-          v4i kf[NK];
+          v4i kf[NK], f[NQ];
 #pragma unroll
           for (int k = 0; k < NK; ++k) kf[k] = tile_read(k_t[k], (k_row_ ^ (x << 6)) + ps * 16 * (2 * DK));
-#pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const int t = ps + pt + u * kPer;
-            if (t >= kT) continue;
-            v4i f[NQ];
-            query(t, x, f);
-            acc[u] = mma<MODE>(kf, f, acc[u]);
-          }
+          query(pt, x, f);
+          acc = mma<MODE>(kf, f, acc);
         }
+        // decay from key 16 ps + 4 g + r to query 16 pt + n; none from later keys
+        const float* const w = &pr[C - 16 * (pt - ps) - n + 4 * g];
+        float y[4];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          const int t = ps + pt + u * kPer;
-          if (t >= kT) continue;
-          // decay from key 16 ps + 4 g + r to query 16 t + n; none from later keys
-          const float* const w = &pr[C - 16 * (t - ps) - n + 4 * g];
-          float y[4];
+        for (int r = 0; r < 4; ++r) {
+          y[r] = acc[r] * (alpha * beta * w[r]);
+          if (pt == ps && n < 4 * g + r) y[r] = 0.0f;
+        }
+        const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + pt * 16 * (2 * C) + 8 * (g & 1);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            y[r] = acc[u][r] * (alpha * beta * w[r]);
-            if (t == ps && n < 4 * g + r) y[r] = 0.0f;
-          }
-          const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + t * 16 * (2 * C) + 8 * (g & 1);
-#pragma unroll
-          for (int k = 0; k < MODE; ++k) {
-            const uint2 v = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            *reinterpret_cast<uint2*>(&p_t[k][at]) = v;
-            y[0] -= bf16_lo(v.x);
-            y[1] -= bf16_hi(v.x);
-            y[2] -= bf16_lo(v.y);
-            y[3] -= bf16_hi(v.y);
-          }
+        for (int k = 0; k < MODE; ++k) {
+          const uint2 v = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+          *reinterpret_cast<uint2*>(&p_t[k][at]) = v;
+          y[0] -= bf16_lo(v.x);
+          y[1] -= bf16_hi(v.x);
+          y[2] -= bf16_lo(v.y);
+          y[3] -= bf16_hi(v.y);
         }
       }
-      if ((ps & 1) && pt == (kPer > 1 ? 1 : 0)) {  // the half of an operand that no tile fills
-        const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + (ps - 1) * 16 * (2 * C) + 8 * (g & 1);
+      if (ps == 1 && pt == kT) {  // the half of an operand that no tile fills
+        const int at = tile_at<C>(n, 2 + (g >> 1)) + 8 * (g & 1);
 #pragma unroll
         for (int k = 0; k < MODE; ++k) *reinterpret_cast<uint2*>(&p_t[k][at]) = make_uint2(0u, 0u);
       }
       // --- state x queries
       if (ewave) {
 #pragma unroll
-        for (int t = 0; t < kT; ++t) o[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int t = 0; t < kT; ++t) o[ct][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int x = 0; x < kB; ++x) {
-          v4i sf[MODE];
-          float y[8];
+          v4i sf[CT][MODE];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = st[x][j / 4][j % 4];
-          split8<MODE>(y, sf);
+          for (int ct = 0; ct < CT; ++ct) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = st[ct][x][j / 4][j % 4];
+            split8<MODE>(y, sf[ct]);
+          }
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             v4i f[NQ];
             query(t, x, f);
-            o[t] = mma<MODE>(sf, f, o[t]);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma<MODE>(sf[ct], f, o[ct][t]);
           }
         }
 #pragma unroll
-        for (int t = 0; t < kT; ++t) o[t] *= beta * held * pr[C - 16 * t - n];
+        for (int t = 0; t < kT; ++t) {
+          const float w = beta * held * pr[C - 16 * t - n];
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[ct][t] *= w;
+        }
       }
     }
     const float decayed = held * pr[C - tc + (last ? 1 : 0)];
@@ -551,38 +554,38 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
     // --- keys x values into the state
     if (ewave) {
 #pragma unroll
-      for (int c = 0; c < kS; ++c)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) vf[c][k] = tile_turn8(v_t[k], v_a0 + c * 32 * (2 * WC), v_a1 + c * 32 * (2 * WC));
-      // decayed, with the decays to the next chunk's first token or to the last one
-      v4i wf[kS][NKT];
-#pragma unroll
       for (int c = 0; c < kS; ++c) {
-        if constexpr (STATE) {
+        // decayed, with the decays to the next chunk's first token or to the last one
+        v4i wf[CT][NKT];
 #pragma unroll
-          for (int k = 0; k < NKT; ++k) wf[c][k] = vf[c][k];
-        } else {
-          const float* const w = &pr[32 * c + 8 * g + C - tc + (last ? 1 : 0)];
-          float y[8];
-          sum8<NV>(vf[c], y);
+        for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] *= into * w[j];
-          split8<NKT>(y, wf[c]);
+          for (int k = 0; k < NV; ++k)
+            vf[ct][c][k] = tile_turn8(v_t[k], (v_a0 ^ (ct << 5)) + c * 32 * (2 * WC), (v_a1 ^ (ct << 5)) + c * 32 * (2 * WC));
+          if constexpr (STATE) {
+#pragma unroll
+            for (int k = 0; k < NKT; ++k) wf[ct][k] = vf[ct][c][k];
+          } else {
+            const float* const w = &pr[32 * c + 8 * g + C - tc + (last ? 1 : 0)];
+            float y[8];
+            sum8<NV>(vf[ct][c], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] *= into * w[j];
+            split8<NKT>(y, wf[ct]);
+          }
         }
-      }
 #pragma unroll
-      for (int x = 0; x < kB; ++x)
+        for (int x = 0; x < kB; ++x)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-          for (int c = 0; c < kS; ++c) {
+          for (int i = 0; i < 2; ++i) {
             v4i f[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k)
               f[k] = tile_turn8(k_t[k], (k_a0_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK), (k_a1_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK));
-            st[x][i] = mma<NKT>(f, wf[c], st[x][i]);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) st[ct][x][i] = mma<NKT>(f, wf[ct], st[ct][x][i]);
           }
-        }
+      }
     }
 
     if (!kEarly && next < end) load_queries(next, tokens_at(next));
@@ -598,18 +601,21 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
             v4i f[MODE];
 #pragma unroll
             for (int k = 0; k < MODE; ++k) f[k] = tile_read(p_t[k], (p_row ^ (c << 6)) + t * 16 * (2 * C));
-            o[t] = mma<MODE>(vf[c], f, o[t]);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma<MODE>(vf[ct][c], f, o[ct][t]);
           }
         // --- store: columns w0 + 4 g + r of token 16 t + n
         ro.at(first_row(i0, tc), tc);
-        const uint32_t at = ro.base + static_cast<uint32_t>(n * ro.step + (w0 + 4 * g) * (OF32 ? 4 : 2));
 #pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          const uint32_t off = at + static_cast<uint32_t>(16 * t * ro.step);
-          if constexpr (OF32) {
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o[t]), ro.r, off, 0, 0);
-          } else {
-            __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(o[t][0], o[t][1]), pack_bf16(o[t][2], o[t][3])}, ro.r, off, 0, 0);
+        for (int ct = 0; ct < CT; ++ct) {
+          const int col = w0 + 16 * ct;
+          const uint32_t at = col < p.Dv ? ro.base + static_cast<uint32_t>(n * ro.step + (col + 4 * g) * (OF32 ? 4 : 2)) : kOff;
+#pragma unroll
+          for (int t = 0; t < kT; ++t) {
+            const uint32_t off = at + static_cast<uint32_t>(16 * t * ro.step);
+            const v4f& y = o[ct][t];
+            if constexpr (OF32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, y), ro.r, off, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, ro.r, off, 0, 0);
           }
         }
       }
@@ -628,21 +634,20 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   else if (p.s_out != nullptr && seg + 1 == p.nseg) out = p.s_out + static_cast<int64_t>(bh) * p.Dk * p.Dv;
   if (out != nullptr) {
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(out, 0, p.Dk * p.Dv * 4, kBufferWord3);
+    each([&](int ct, int x, int i) {
+      const int d = 32 * x + 8 * g + 4 * i, col = w0 + 16 * ct + n;
+      const uint32_t at = col < p.Dv && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.Dv + col) : kOff;
 #pragma unroll
-    for (int x = 0; x < kB; ++x)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int d = 32 * x + 8 * g + 4 * i;
-        const uint32_t at = ewave && d < p.Dk ? 4u * static_cast<uint32_t>(d * p.Dv + w0 + n) : kOff;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[x][i][r]), rs, at + 4u * r * p.Dv, 0, 0);
-      }
+      for (int r = 0; r < 4; ++r)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[ct][x][i][r]), rs, at + 4u * r * p.Dv, 0, 0);
+    });
   }
 }
 
-// bf16 operands take chunks of 64 tokens, fp32's parts of 32, as do Dk above 128:
-// what LDS holds for two workgroups on a compute unit.
-constexpr int chunk_tokens(int DK, Kind K) { return DK >= 128 || K != kBf16 ? 32 : 64; }
+// Tokens of a chunk: 64 where the sums of narrow bf16 states alone are wanted (16
+// x 1024, 8 heads of 64: 17.5 us, with 32 19.7), else 32 (the three passes of that
+// 44.5 us, with 64 62: too many registers).
+constexpr int chunk_tokens(int DK, Kind K, bool state) { return state && DK == 64 && K == kBf16 ? 64 : 32; }
 
 // `n` passes of the same number of workgroups, widths in 64s, and waves.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
@@ -651,17 +656,24 @@ hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
   for (int i = 0; i < n; ++i) ps.p[i] = p[i];
   ps.n = static_cast<uint32_t>(n);
   ps.count = p->B * p->H * p->nseg * p->tiles;
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(ps.count * ps.n), dim3(64 * p->waves), 0, stream, ps);
+  const auto go = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3(ps.count * ps.n), dim3(64 * waves), 0, stream, ps);
     return hipGetLastError();
   };
-#define MMF_DIMS(DK)                                                                                                     \
-  return p->waves == 4 ? go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 4, chunk_tokens(DK, KQ), STATE>) \
-                       : go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, 8, chunk_tokens(DK, KQ), STATE>)
-  if (p->Dk <= 64) MMF_DIMS(64);
-  if (p->Dk <= 128) MMF_DIMS(128);
-  MMF_DIMS(256);
-#undef MMF_DIMS
+#define MMF_FORM(DK, WAVES, CT) \
+  go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, WAVES, CT, chunk_tokens(DK, KQ, STATE), STATE>, WAVES)
+  if (p->Dk > 128) return p->waves == 4 ? MMF_FORM(256, 4, 1) : MMF_FORM(256, 8, 1);
+  // 128 columns: parts of fp32 as 32 per wave, so that what a wave reads from LDS
+  // serves twice as many (4 x 2048 fp32, backward: 194 -> 168 us; 2048, forward: 37
+  // -> 33); bf16, with fewer of them, as 16 per wave (16384: 76 us, 32 per wave 78)
+  if constexpr (STATE || KQ == kBf16) {
+    if (p->Dk > 64) return p->waves == 4 ? MMF_FORM(128, 4, 1) : MMF_FORM(128, 8, 1);
+    return p->waves == 4 ? MMF_FORM(64, 4, 1) : MMF_FORM(64, 8, 1);
+  } else {
+    if (p->Dk > 64) return p->waves == 4 ? MMF_FORM(128, 4, 1) : MMF_FORM(128, 4, 2);
+    return p->waves == 4 ? MMF_FORM(64, 4, 1) : MMF_FORM(64, 4, 2);
+  }
+#undef MMF_FORM
 }
 
 }  // namespace la
