@@ -113,14 +113,17 @@ __device__ __forceinline__ v4f mma(const v4i (&a)[NA], const v4i (&b)[NB], v4f a
 }
 
 // Tiles in LDS: rows of W bf16 values in chunks of 16 bytes, chunk q of a row at
-// q ^ swizzle(row).  The 8 lanes that one cycle serves, 8 rows at the same
-// chunk (along the rows) or 4 rows at 4 neighbouring ones (across), then touch
-// all banks once.  Rows 16 apart have the same swizzle, and chunks 4 b apart
-// differ in address bits that no other part of the sum reaches: ^ (b << 6).
+// q ^ swizzle(row).  A cycle serves 16 lanes of a 16-byte read, 32 of a transposing
+// one, and touches 64 banks: of the lanes 16 g + n along the rows n = 0 .. 3 and 12
+// .. 15 of one g with n = 4 .. 11 of the next, whose chunk is the neighbour (or the
+// other way round), so the swizzle takes rows 4 apart to 0, 2, 3, 1; across, 8 rows
+// at 2 chunks of 16 bytes, or of the keys at half of 4, which takes two cycles.
+// Rows 16 apart have the same swizzle, and chunks 4 b apart differ in address bits
+// that no other part of the sum reaches: ^ (b << 6).
 template <int W>
 __device__ __forceinline__ int tile_at(int row, int chunk) {
-  const int f = W == 32 ? (row >> 2) & 3
-              : W == 64 ? 4 * ((row >> 1) & 1) + ((row >> 2) & 3) : 4 * (row & 3) + ((row >> 2) & 3);
+  const int q = (row >> 3) & 1, low = 2 * (((row >> 2) & 1) ^ q) + q;
+  const int f = W == 32 ? low : W == 64 ? 4 * ((row >> 1) & 1) + low : 4 * (row & 3) + low;
   return row * (2 * W) + ((chunk ^ f) << 4);
 }
 __device__ __forceinline__ v4i tile_read(const char* tile, int at) { return *reinterpret_cast<const v4i*>(tile + at); }
