@@ -676,8 +676,8 @@ int mmf_beam_reorder(const void *const *states, void *const *outs, const int64_t
  * Rows without an entry have loss 0 and gradient 0, and rows with dloss 0
  * gradient 0, whatever z holds (padding).  Else a row of z with a NaN or +inf,
  * or of -inf alone, gives NaN.  fp32, sums and losses in fp64, rounded once.
- * V up to 2^24, K up to 1024, M below 2^22 (MMF_ERR_SHAPE); tau must be positive
- * and finite (MMF_ERR_ARG).  M == 0 is a no-op.  Allocates nothing.
+ * V up to 2^24, K up to 1024, M below 2^22 (MMF_ERR_SHAPE); tau must be at
+ * least 2^-126 and finite (MMF_ERR_ARG).  M == 0 is a no-op.  Allocates nothing.
  */
 int mmf_distill_fwd(const void *z, int z_is_f32, const int32_t *idx, const void *t, int t_is_f32,
                     float tau, float *loss, int64_t M, int64_t V, int64_t K, hipStream_t stream);

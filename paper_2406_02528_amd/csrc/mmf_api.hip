@@ -352,7 +352,8 @@ int check_beam(int64_t B, int64_t W, int64_t V, int64_t n) {
 // ---- distillation ----
 int check_distill(int64_t M, int64_t V, int64_t K, float tau) {
   if (M < 0 || M > kMaxRows || V < 1 || V > int64_t(1) << 24 || K < 1 || K > mmf::kDistillMaxK) return MMF_ERR_SHAPE;
-  if (!(tau > 0.0f) || tau == __builtin_inff()) return MMF_ERR_ARG;
+  // of a smaller one 1 / tau overflows
+  if (!(tau >= 0x1p-126f) || tau == __builtin_inff()) return MMF_ERR_ARG;
   return MMF_OK;
 }
 

@@ -20,7 +20,8 @@ def mmf():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("B,W,V,n", [(1, 1, 2 ** 18, 64), (1, 3, 2 ** 18, 1), (1, 64, 2 ** 15, 64), (200, 1, 300, 7),
-                                     (40, 16, 1025, 16), (1, 2, 32, 64)], ids=str)
+                                     (40, 16, 1025, 16), (1, 2, 32, 64), (1, 48, 2000, 64), (2, 32, 3000, 64),
+                                     (1, 64, 64, 64)], ids=str)
 def test_largest_selections(mmf, B, W, V, n):
     log(f"[beam] {B} {W} {V} {n}")
     z, s, g = draw(B, W, V, F32, V + n)

@@ -127,7 +127,7 @@ def test_distill_arguments(mmf):
     for f in (distill, distill_bwd):
         for bad in ({"M": -1}, {"M": 2 ** 22}, {"V": 0}, {"V": 2 ** 24 + 1}, {"K": 0}, {"K": 1025}):
             assert f(lib, **bad) == SHAPE, bad
-        for tau in (0.0, -1.0, float("inf"), float("nan")):
+        for tau in (0.0, -1.0, 1e-39, float("inf"), float("nan")):
             assert f(lib, tau=tau) == ARG
         assert f(lib, zf=2) == f(lib, tf=-1) == DTYPE
     for name in ("z", "idx", "t", "loss"):
