@@ -110,14 +110,18 @@ uint32_t tiles_of(int Dv) {
 }
 // state_bytes: of all the states that enter one segment.
 Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
-  constexpr int64_t C = 64;
+  constexpr int64_t C = 32;
   const int64_t chunks = (T + C - 1) / C;
-  // In tenths of a us: a chunk takes about 8 where a compute unit has one
-  // workgroup, two of them 12; a start 10; with segments, their sums about half
-  // of a pass each, and their states are written and read twice, at 4.5 TB/s.
+  // In tenths of a us: 32 tokens take about 4 where a compute unit has one
+  // workgroup, two of them 6; a start 10; with segments, their sums about half
+  // of a pass each, and their states are written and read twice, at 4.5 TB/s.  The
+  // backward's sums are counted in any case: ds0 takes them.  (Forwards of fp32, us,
+  // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
+  // 16: 56, 71, 60; 4 x 2048, 8: 133, 149, 156; backward of that, 4: 232, 238, 241;
+  // 16384 bf16, 32: 132, 150.)
   const auto cost = [&](int64_t s) {
     const int64_t per = (chunks + s - 1) / s, each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
-    const int64_t work = each / 2 * (120 * per + 100) + each % 2 * (78 * per + 100);
+    const int64_t work = each / 2 * (60 * per + 100) + each % 2 * (39 * per + 100);
     return s == 1 && passes == 1 ? work : work + work / 3 + state_bytes * s * 4 / 450000 + 100;
   };
   int64_t best = 1;
