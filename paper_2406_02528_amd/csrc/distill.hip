@@ -6,16 +6,18 @@
 //   dz = dloss tau (q - p at idx)
 //
 // A workgroup takes a row and keeps it in registers, so that the maximum, the
-// sum and the gradient are one pass over memory; rows of more than 65536 are
-// read again for the gradient.  Rows are vectors of 8 values that start on 16
-// bytes in z and dz alike, and the few values before and after them.  What
-// the teacher's entries need (their softmax, z at their tokens, which of them
-// share a token) is done while the row's loads are in flight; their
+// sum and the gradient are one pass over memory; rows of more than 32768 bf16 or
+// 65536 fp32 logits are read again for the gradient.  Rows are vectors of 8 values
+// that start on 16 bytes in z and dz alike, and the few values before and after
+// them.  What the teacher's entries need (their softmax, z at their tokens, which
+// of them share a token) is done while the row's loads are in flight; their
 // gradients are written again after the row's, behind a barrier.
 //
 // fp32 with the sums of 8 exponentials and the rest in fp64; the loss and the
 // gradient at the entries in fp64 (p ln p - p ln q and q - p cancel where the
-// student agrees).  Bound by HBM: one read of z, one write of dz.
+// student agrees).  Bound by HBM, one read of z and one write of dz: 8192 x 32000
+// bf16, 64 entries, in 192 us, 5.5 TB/s; few rows by the row's chain of loads,
+// maxima and sums (77 x 50001 fp32, the loss alone: 10 us).
 #include "distill.h"
 #include "mmf_device.h"
 #include "row_vec.h"
@@ -33,11 +35,31 @@ __device__ __forceinline__ float value(const T* p) {
 
 // The teacher's entries of a row: token (-1: none, or one that a lower entry
 // has), z there, p (of all entries of that token).
+constexpr int kScan = 16;   // tokens that a comparison with all of them reads at once
 struct Entries {
-  int idx[kDistillMaxK];
+  alignas(16) int idx[kDistillMaxK];   // up to the next multiple of kScan none
   float z[kDistillMaxK];
   double p[kDistillMaxK];
 };
+
+// f(k, whether entry k has token i) for the K entries in order; reads of 16 bytes
+// that do not wait for one another (one at a time they took 8 us for 64 entries).
+template <typename F>
+__device__ __forceinline__ void scan(const Entries& en, int K, int i, F&& f) {
+  static_assert(kDistillMaxK % kScan == 0, "whole groups");
+  for (int k = 0; k < K; k += kScan) {
+    int4 x[kScan / 4];
+#pragma unroll
+    for (int g = 0; g < kScan / 4; ++g) x[g] = *reinterpret_cast<const int4*>(&en.idx[k + 4 * g]);
+#pragma unroll
+    for (int g = 0; g < kScan / 4; ++g) {
+      f(k + 4 * g, x[g].x == i);
+      f(k + 4 * g + 1, x[g].y == i);
+      f(k + 4 * g + 2, x[g].z == i);
+      f(k + 4 * g + 3, x[g].w == i);
+    }
+  }
+}
 
 template <int W>
 struct Slots {
@@ -66,7 +88,6 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
   constexpr int W = THREADS / kWave, E = 8;
   __shared__ Entries en;
   __shared__ Slots<W> sl;
-  __shared__ int s_twice;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t m = blockIdx.x;
   const int V = static_cast<int>(a.V), K = static_cast<int>(a.K);
@@ -89,9 +110,9 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
   // --- the teacher's entries
   const double inv = 1.0 / a.tau;
   const float c = static_cast<float>(kLog2e / a.tau);
-  if (tid == 0) s_twice = 0;
   float tm = -__builtin_inff();
   bool any = false;
+  for (int j = K + tid; j < (K + kScan - 1) / kScan * kScan; j += THREADS) en.idx[j] = -1;
   for (int j = tid; j < K; j += THREADS) {
     int i = a.idx[m * K + j];
     const float t = a.t_is_f32 ? static_cast<const float*>(a.t)[m * K + j]
@@ -116,12 +137,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
     }
     return;
   }
-  if (dz != nullptr) {  // entries of one token
-    for (int j = tid; j < K; j += THREADS) {
+  uint32_t twice = 0;   // which of the thread's entries, in turn, share their token with others
+  static_assert(kDistillMaxK <= 32 * THREADS, "a bit for each");
+  if (dz != nullptr) {
+    for (int j = tid, n = 0; j < K; j += THREADS, ++n) {
       const int i = en.idx[j];
-      bool same = false;
-      for (int k = 0; k < K; ++k) same |= k != j && en.idx[k] == i;
-      if (same && i >= 0) s_twice = 1;
+      int same = 0;
+      scan(en, K, i, [&](int, bool is) { same += is; });
+      if (same > 1 && i >= 0) twice |= 1u << n;
     }
   }
 
@@ -257,18 +280,19 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
   if (tid == 0 && a.loss != nullptr) a.loss[m] = static_cast<float>(sum_of<W>(sl.loss) * a.tau * a.tau);
   if (dz == nullptr) return;
   // --- and at the teacher's tokens
-  for (int j = tid; j < K; j += THREADS) {
+  for (int j = tid, n = 0; j < K; j += THREADS, ++n) {
     const int i = en.idx[j];
     if (i < 0) continue;
     double p = en.p[j];
-    if (s_twice != 0) {  // the lowest entry of a token for all of them
+    if ((twice >> n) & 1) {  // the lowest entry of a token for all of them
       bool first = true;
       p = 0.0;
-      for (int k = 0; k < K; ++k)
-        if (en.idx[k] == i) {
+      scan(en, K, i, [&](int k, bool is) {
+        if (is) {
           first &= k >= j;
           p += en.p[k];
         }
+      });
       if (!first) continue;
     }
     put(i, static_cast<float>((__builtin_amdgcn_exp2f((en.z[j] - zm) * c) / ze - p) * wt));
@@ -281,13 +305,24 @@ hipError_t launch(const DistillArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(a.M)), dim3(threads), 0, stream, a);
     return hipGetLastError();
   };
+  // The fewest threads that hold a row in registers: rows end at the same time in
+  // them all, so it is the rows beside each other on a compute unit that hide each
+  // other's waits (8192 bf16 rows of 2000: 1, 2, 4 vectors per thread 32, 36, 43
+  // us; of 8000: 256 threads 52, 512 95; of 32000: 512 threads 200, 1024 273).
   const int64_t nv = a.V / 8;  // the most whole vectors of a row
+  if (nv <= 256) return go(distill_kernel<T, D, 256, 1, NT>, 256);
   if (nv <= 2 * 256) return go(distill_kernel<T, D, 256, 2, NT>, 256);
   if (nv <= 4 * 256) return go(distill_kernel<T, D, 256, 4, NT>, 256);
   if (nv <= 4 * 512) return go(distill_kernel<T, D, 512, 4, NT>, 512);
-  if (nv <= 8 * 512) return go(distill_kernel<T, D, 512, 8, NT>, 512);
-  if (nv <= 8 * 1024) return go(distill_kernel<T, D, 1024, 8, NT>, 1024);
-  return go(distill_kernel<T, D, 1024, 0, NT>, 1024);
+  if (NT || nv <= 8 * 512) return go(distill_kernel<T, D, 512, 8, NT>, 512);
+  if constexpr (!NT) {
+    // one such row fills a compute unit's registers; of bf16, reading it again costs
+    // less than that (1024 rows of 36000 37 against 49 us, 4096 of 50001 203 against
+    // 218), of fp32 more (2048 of 50001 201 against 185)
+    if constexpr (sizeof(T) == 4)
+      if (nv <= 8 * 1024) return go(distill_kernel<T, D, 1024, 8, false>, 1024);
+    return go(distill_kernel<T, D, 1024, 0, false>, 1024);
+  }
 }
 
 }  // namespace
@@ -295,12 +330,12 @@ hipError_t launch(const DistillArgs& a, hipStream_t stream) {
 hipError_t launch_distill(const DistillArgs& a, hipStream_t stream) {
   // the loss alone: D does not matter
   const bool d32 = a.dz != nullptr && a.dz_is_f32;
-  const int64_t bytes = a.M * a.V * ((a.z_is_f32 ? 4 : 2) + (a.dz == nullptr ? 0 : d32 ? 4 : 2));
-  const bool nt = bytes >= kLastLevelBytes && a.V <= 65536 + 7;
-  if (a.z_is_f32) {
-    if (d32) return nt ? launch<float, float, true>(a, stream) : launch<float, float, false>(a, stream);
-    return nt ? launch<float, uint16_t, true>(a, stream) : launch<float, uint16_t, false>(a, stream);
-  }
+  if (a.z_is_f32) return d32 ? launch<float, float, false>(a, stream) : launch<float, uint16_t, false>(a, stream);
+  // Streams pass the caches where the arrays fill the last of them, of bf16 (8192
+  // rows of 32000: 186 against 200 us, of 16000 117 against 112; fp32 loses by it,
+  // 2048 rows of 50001 224 against 185), and not where a row is read again.
+  const int64_t bytes = a.M * a.V * (2 + (a.dz == nullptr ? 0 : d32 ? 4 : 2));
+  const bool nt = bytes >= kLastLevelBytes && a.V / 8 <= 8 * 512;
   if (d32) return nt ? launch<uint16_t, float, true>(a, stream) : launch<uint16_t, float, false>(a, stream);
   return nt ? launch<uint16_t, uint16_t, true>(a, stream) : launch<uint16_t, uint16_t, false>(a, stream);
 }
