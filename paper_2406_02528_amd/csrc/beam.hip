@@ -16,7 +16,14 @@
 // The n best of a piece: of the 64 lanes' own maxima, the n-th largest is at
 // most the piece's n-th largest logit, so only what reaches the largest such
 // bound of the four waves goes to LDS (of the logits that are equal to it, the
-// first n of each wave), where each counts those before it.
+// first n of each wave), where each counts those before it.  The smallest of the
+// waves' n/4-th largest is such a bound too, which for evenly spread logits leaves
+// little more than n (50000 fp32, n = 64: 66 -> 33 us; for n = 4 its search costs
+// more than it saves, 9.3 -> 9.7); the first one limits the list whatever they are.
+//
+// 32 x 8 rows of 50000 bf16: 17 us for the pieces, bound by the vector unit (about
+// 25 instructions for 64 logits), 8 for the merging, bound by its steps in line.
+// Reordering those beams' states of 1 MB each, two layers: 118 us, 5.2 TB/s.
 #include "beam.h"
 #include "mmf_device.h"
 #include "row_vec.h"
@@ -77,7 +84,9 @@ struct Scratch {
   int pieces, piece;
 };
 
-// Candidates of a piece that LDS holds, and those that are ranked by counting.
+constexpr int kFew = 8;
+// Candidates of a piece that LDS holds, and those that are ranked by counting
+// (n = 32 of 64 rows of 32000: 30 us; one after the other, for any number, 46).
 constexpr int list_size(int vals, int n) { return kWaves * ((n - 1) * vals + n); }
 constexpr int kCounted = 1024;
 
@@ -86,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectAr
   extern __shared__ uint64_t s_list[];
   __shared__ float s_max[kWaves];
   __shared__ double s_sum[kWaves];
-  __shared__ uint32_t s_bound[kWaves];
+  __shared__ uint32_t s_bound[kWaves], s_part[kWaves];
   __shared__ uint64_t s_key[kWaves];
   __shared__ int s_count;
   const int piece = blockIdx.x % s.pieces;
@@ -121,15 +130,20 @@ __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectAr
   // the others in the upper half only: the lower is 0, or of negative ones all ones
   const uint32_t top = begin + static_cast<int>(threadIdx.x) < end ? order_of(m) : 0u;
   m = wave_max_f32(m);
-  uint32_t bound_w = nth_largest<sizeof(T) == 4 ? 0 : 16>(top, a.n);
-  if (sizeof(T) == 2 && bound_w != 0 && (bound_w >> 31) == 0) bound_w |= 0xFFFFu;
+  const auto reached_by = [&](int n) {
+    const uint32_t x = nth_largest<sizeof(T) == 4 ? 0 : 16>(top, n);
+    return sizeof(T) == 2 && x != 0 && (x >> 31) == 0 ? x | 0xFFFFu : x;
+  };
+  const uint32_t bound_w = reached_by(a.n), part_w = a.n > kFew ? reached_by((a.n + kWaves - 1) / kWaves) : 0u;
   if (lane == 0) {
     s_max[wave] = m;
     s_bound[wave] = bound_w;
+    s_part[wave] = part_w;
   }
   __syncthreads();
   m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const uint32_t bound_o = max(max(s_bound[0], s_bound[1]), max(s_bound[2], s_bound[3]));
+  const uint32_t bound_o = max(max(max(s_bound[0], s_bound[1]), max(s_bound[2], s_bound[3])),
+                               min(min(s_part[0], s_part[1]), min(s_part[2], s_part[3])));
   const float bound = bound_o != 0 ? logit_of(bound_o) : -__builtin_inff();
 
   // what reaches the bound; all of a piece that no wave has n lanes of
@@ -204,8 +218,8 @@ __device__ __forceinline__ uint64_t order_of(double s) {
 }
 
 constexpr int kFinalWaves = 16;
-constexpr int kStaged = 6144;   // keys of a batch's lists that LDS holds
-constexpr int kRanked = 512;    // candidates of a batch that are ranked by counting
+constexpr int kStaged = 6144;   // keys of a batch's lists that LDS holds (64 beams of 1000 tokens, n = 64: 86 us, from memory 106)
+constexpr int kRanked = 128;    // candidates of a batch that are ranked by counting (8 x 16: 17.8 us, merged 18.5; 16 x 16: 23.8, 20.8)
 
 // A wave merges the lists of a row (a lane per piece); the beams' are then ranked
 // by counting, or, of many, merged by wave 0 (a lane per beam).
@@ -359,7 +373,8 @@ __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(const Set s, con
 }
 
 // Logits per thread: few where there are few rows, as long as a wave holds a
-// row's pieces.
+// row's pieces (4 rows of 32000 fp32: 8.9 us, with 16 per thread 9.2; 32 rows 12.8
+// and 12.5, 256 rows of 50000 38 and 24).
 constexpr int kMaxPieces = kWave;
 int vals_of(int64_t rows, int V) {
   const int64_t small = (V + 4 * kThreads - 1) / (4 * kThreads);
