@@ -183,7 +183,8 @@ hipError_t join(const Join* j, int n, const LinattnPass& p, const Plan& plan, hi
   a.size = static_cast<int64_t>(p.Dk) * p.Dv;
   a.tokens = plan.seg_tokens / plan.sub;
   a.T = p.T;
-  // a lane's entries side by side where the lanes are still many
+  // a lane's entries side by side where the lanes are still many (the forward of 4 x
+  // 2048 bf16, 16 heads of 128: 84 -> 76 us, of 16384 137 -> 130; few lanes: equal)
   const bool wide = a.size * a.states * n >= int64_t(1) << 20;
   const int64_t lanes = a.size / (wide ? 4 : 1);
   const dim3 grid(a.states * static_cast<uint32_t>((lanes + kJoinBlock - 1) / kJoinBlock), static_cast<uint32_t>(n));
