@@ -13,7 +13,9 @@ Also the GLU channel mixer's gated up-projection, the MLGRU token mixer
 the training forward and backward of the layer, and what a block's training
 step needs around it: the residual addition fused into the quantiser, the GLU
 mixer's and the recurrence's training forms, and the global gradient norm with
-clipping.
+clipping.  And linear attention with a decay per head (forward and backward), a
+step of beam search (selection, reordering of states) and distillation from a
+teacher's best tokens (loss and gradient).
 
 Functions carry the names of the C entry points.  There is no fallback: if
 the library is not built, importing this package raises ``ImportError``.
