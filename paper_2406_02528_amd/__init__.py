@@ -973,9 +973,10 @@ def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, s
         dst, orows = _state_ptrs(outs, "outs", B * W, here)
         if orows != rows or [t.dtype for t in outs] != [t.dtype for t in states]:
             raise ValueError("outs must have the types and shapes of states")
-    full = [p for p, r in zip(dst, rows) if r]
-    if len(set(full)) != len(full):
-        raise ValueError("a tensor to write is in the list twice")
+    if len(set(dst)) != len(dst):  # empty tensors may share an address
+        full = [p for p, r in zip(dst, rows) if r]
+        if len(set(full)) != len(full):
+            raise ValueError("a tensor to write is in the list twice")
     _check(_lib.mmf_beam_reorder(_at(src), _at(dst), _at(rows), len(src), _ptr(parents), B, W,
                                  _stream_here(stream, here)))
 
