@@ -226,7 +226,11 @@ __device__ __forceinline__ void look_bf16(uint32_t w, uint32_t& top) {
   typedef unsigned short v2us __attribute__((ext_vector_type(2)));
   top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, top), __builtin_bit_cast(v2us, w & 0x7FFF7FFFu)));
 }
-__device__ __forceinline__ bool not_finite(uint32_t top) { return (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u; }
+// Of fp32 the largest magnitude's bits: not finite is what its first part is not.
+template <Kind K>
+__device__ __forceinline__ bool not_finite(uint32_t top) {
+  return K == kBf16 ? (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u : top >= 0x7F7F8000u;
+}
 
 // MODE: parts of fp32 values in the products of o.  NKT: parts of the decayed
 // values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns
@@ -413,14 +417,14 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
           for (int j = 0; j < 8; ++j) x[j] *= w;
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) top = max(top, (__float_as_uint(x[j]) & 0x7FFFFFFFu) >> 16);
+          for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
         }
         split8<NV>(x, f);
 #pragma unroll
         for (int k = 0; k < NV; ++k) *reinterpret_cast<v4i*>(&v_t[k][at]) = f[k];
       }
     }
-    if (!STATE && __any(not_finite(top)) && lane == 0) s_bad[flag] = 1;
+    if (!STATE && __any(not_finite<KV>(top)) && lane == 0) s_bad[flag] = 1;
     const auto put = [&](auto kind, const auto& w, bool f32, auto& t) {
       constexpr Kind K = decltype(kind)::value;
       constexpr int N = sizeof(t) / sizeof(t[0]);

@@ -148,6 +148,24 @@ def test_what_is_not_finite_stays_where_it_belongs(mmf, part, T, at, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("part", ["q", "k", "v"])
+@pytest.mark.parametrize("value", [3.4e38, -3.395e38])
+def test_fp32_above_the_largest_bf16(mmf, part, value):
+    """Finite, but with no finite first part: as what is not finite."""
+    B, T, H, dk, dv, at = 1, 100, 2, 32, 48, 70
+    p = inputs(B, T, H, dk, dv, F32, seed=3, decay=[0.9, 0.5])
+    ref, A = forward(p)[0], forward(p, torch.abs)[0]
+    o_clean = run_fwd(mmf, p)[0]
+    p["qkv"][at, {"q": 0, "k": H * dk, "v": 2 * H * dk}[part] + 3] = value   # of head 0
+    o, s = run_fwd(mmf, p)
+    bound = (T + dk + 48) * U * A + 1e-37
+    within(o[:at], ref[:at], bound[:at], "o before")
+    if part == "q":
+        within(o[at + 1:], ref[at + 1:], bound[at + 1:], "o behind")
+    assert torch.equal(o[:, dv:], o_clean[:, dv:]) and s[:, 1].isfinite().all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,at", [(3, 1), (100, 40), (700, 300)])
 def test_gradients_that_are_not_finite(mmf, T, at):
     B, H, dk, dv = 2, 2, 32, 48
