@@ -522,11 +522,11 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
         for (int k = 0; k < MODE; ++k) *reinterpret_cast<uint2*>(&p_t[k][at]) = make_uint2(0u, 0u);
       }
       // --- state x queries
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int t = 0; t < kT; ++t) o[ct][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
       if (ewave) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int t = 0; t < kT; ++t) o[ct][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int x = 0; x < kB; ++x) {
           v4i sf[CT][MODE];
@@ -611,19 +611,21 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma<MODE>(vf[ct][c], f, o[ct][t]);
           }
-        // --- store: columns w0 + 4 g + r of token 16 t + n
-        ro.at(first_row(i0, tc), tc);
+      }
+      // --- store: columns w0 + 4 g + r of token 16 t + n.  By every wave, those
+      // without columns past the resource: with a branch around the stores the
+      // next chunk's staging would wait for them too, not for its loads alone.
+      ro.at(first_row(i0, tc), tc);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const int col = w0 + 16 * ct;
-          const uint32_t at = col < p.Dv ? ro.base + static_cast<uint32_t>(n * ro.step + (col + 4 * g) * (OF32 ? 4 : 2)) : kOff;
+      for (int ct = 0; ct < CT; ++ct) {
+        const int col = w0 + 16 * ct;
+        const uint32_t at = col < p.Dv ? ro.base + static_cast<uint32_t>(n * ro.step + (col + 4 * g) * (OF32 ? 4 : 2)) : kOff;
 #pragma unroll
-          for (int t = 0; t < kT; ++t) {
-            const uint32_t off = at + static_cast<uint32_t>(16 * t * ro.step);
-            const v4f& y = o[ct][t];
-            if constexpr (OF32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, y), ro.r, off, 0, 0);
-            else __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, ro.r, off, 0, 0);
-          }
+        for (int t = 0; t < kT; ++t) {
+          const uint32_t off = at + static_cast<uint32_t>(16 * t * ro.step);
+          const v4f& y = o[ct][t];
+          if constexpr (OF32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, y), ro.r, off, 0, 0);
+          else __builtin_amdgcn_raw_buffer_store_b64(v2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, ro.r, off, 0, 0);
         }
       }
     }
