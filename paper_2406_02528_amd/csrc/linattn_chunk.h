@@ -456,6 +456,9 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   int64_t i0 = begin;
   int tc = some ? tokens_at(i0) : 0, flag = 0;
   if (some) stage(i0, tc, flag);
+  // The state is there before the loop: a wait for it inside would be one for the
+  // next chunk's loads, in every chunk.
+  if constexpr (!STATE) each([&](int ct, int x, int i) { asm volatile("" : "+v"(st[ct][x][i])); });
   while (some) {
     const int64_t next = i0 + tc;
     if (next < end) {
