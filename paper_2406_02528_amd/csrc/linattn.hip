@@ -118,7 +118,7 @@ Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
   // backward's sums are counted in any case: ds0 takes them.  (Forwards of fp32, us,
   // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
   // 16: 56, 71, 60; 4 x 2048, 8: 133, 149, 156; backward of that, 4: 232, 238, 241;
-  // 16384 bf16, 32: 132, 150.)
+  // 16384 bf16, 32: 132, 16: 150.)
   const auto cost = [&](int64_t s) {
     const int64_t per = (chunks + s - 1) / s, each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
     const int64_t work = each / 2 * (60 * per + 100) + each % 2 * (39 * per + 100);

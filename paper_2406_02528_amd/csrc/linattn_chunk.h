@@ -36,13 +36,15 @@
 // that the rows a lane keeps of the two tiles h are the slots d = 32 b + 8 g + j
 // of the operand it is for the next chunk: the state never leaves its registers.
 // The keys x queries are formed once per workgroup: each wave forming its own in
-// registers (keys in the same order) saves a barrier, but took 83 us instead of
-// 76 (16384 bf16 tokens, 16 heads of 128), and 195 instead of 168 for the three
-// passes of 4 x 2048 fp32.
+// registers (keys in the same order) saves a barrier, but took a tenth longer
+// (16384 bf16 tokens, 16 heads of 128; a sixth for the three passes of 4 x 2048
+// fp32).  Two buffers for bf16 chunks in LDS, and one barrier instead of two,
+// gained nothing.
 //
-// A pass over few tokens is bound by what each chunk waits for (loads, LDS, two
-// barriers), over many by HBM: that forward moves 268 MB in 76 us, 3.5 TB/s, after
-// 134 MB in 42 us for the segments' sums.
+// Over many tokens a pass is bound by HBM: that forward moves 302 MB in 71 us, 4.3
+// TB/s, after 168 MB in 42 us for the segments' sums, 4.0 TB/s.  Over few it is
+// bound by a chunk's chain of loads, LDS and products: 2.5 us of bf16, 5 of fp32,
+// whose parts take six products for one.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
 // decayed products, the state, the weighted keys) go to the matrix cores as
@@ -676,8 +678,8 @@ hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
   go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, WAVES, CT, chunk_tokens(DK, KQ, STATE), STATE>, WAVES)
   if (p->Dk > 128) return p->waves == 4 ? MMF_FORM(256, 4, 1) : MMF_FORM(256, 8, 1);
   // 128 columns: parts of fp32 as 32 per wave, so that what a wave reads from LDS
-  // serves twice as many (4 x 2048 fp32, backward: 194 -> 168 us; 2048, forward: 37
-  // -> 33); bf16, with fewer of them, as 16 per wave (16384: 76 us, 32 per wave 78)
+  // serves twice as many (4 x 2048 fp32, backward: 184 -> 163 us; 2048, forward: 36
+  // -> 33); bf16, with fewer of them, as 16 per wave (16384: 71 us, 32 per wave 72)
   if constexpr (STATE || KQ == kBf16) {
     if (p->Dk > 64) return p->waves == 4 ? MMF_FORM(128, 4, 1) : MMF_FORM(128, 8, 1);
     return p->waves == 4 ? MMF_FORM(64, 4, 1) : MMF_FORM(64, 8, 1);
