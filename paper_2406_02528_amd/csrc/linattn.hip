@@ -3,6 +3,8 @@
 #include "linattn.h"
 #include "mmf_device.h"
 
+#include <initializer_list>
+
 namespace mmf {
 
 hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream);
@@ -108,8 +110,15 @@ uint32_t tiles_of(int Dv) {
   const int w = 16 * waves_of(Dv);
   return static_cast<uint32_t>((Dv + w - 1) / w);
 }
-// state_bytes: of all the states that enter one segment.
-Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
+// The backward's passes go in one launch where their kernels are the same: widths
+// in the same class, workgroups of the same size.
+bool one_launch(int dk, int dv) {
+  const auto width = [](int d) { return d <= 64 ? 0 : d <= 128 ? 1 : 2; };
+  return width(dk) == width(dv) && waves_of(dk) == waves_of(dv);
+}
+// launches: their passes, 1 (the forward), 3 or 2 and 1; state_bytes: of all the
+// states that enter one segment.
+Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int64_t state_bytes) {
   constexpr int64_t C = 32;
   const int64_t chunks = (T + C - 1) / C;
   // In tenths of a us: 32 tokens take about 4 where a compute unit has one
@@ -118,11 +127,16 @@ Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
   // backward's sums are counted in any case: ds0 takes them.  (Forwards of fp32, us,
   // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
   // 16: 56, 71, 60; 4 x 2048, 8: 133, 149, 156; backward of that, 4: 232, 238, 241;
-  // 16384 bf16, 32: 132, 16: 150.)
+  // 16384 bf16, 32: 132, 16: 150.  Backward in two launches, 4 x 1857, 12 heads of 96
+  // x 48, 5: 133; 3, as for one: 190.)
   const auto cost = [&](int64_t s) {
-    const int64_t per = (chunks + s - 1) / s, each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
-    const int64_t work = each / 2 * (60 * per + 100) + each % 2 * (39 * per + 100);
-    return s == 1 && passes == 1 ? work : work + work / 3 + state_bytes * s * 4 / 450000 + 100;
+    const int64_t per = (chunks + s - 1) / s;
+    int64_t work = 0;
+    for (const int passes : launches) {
+      const int64_t each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
+      work += each / 2 * (60 * per + 100) + each % 2 * (39 * per + 100);
+    }
+    return s == 1 && *launches.begin() == 1 ? work : work + work / 3 + state_bytes * s * 4 / 450000 + 100;
   };
   int64_t best = 1;
   for (int64_t s = 2; s <= chunks && groups * (s - 1) < 2 * kSlots; ++s)
@@ -135,10 +149,11 @@ Plan plan_of(int64_t T, int64_t groups, int passes, int64_t state_bytes) {
   while (per % (2 * plan.sub) == 0 && 2 * groups * plan.nseg * plan.sub <= kSlots / 2) plan.sub *= 2;
   return plan;
 }
-Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), 1, 4 * B * H * dk * dv); }
+Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), {1}, 4 * B * H * dk * dv); }
 Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv) {
   const uint32_t a = tiles_of(dv), b = tiles_of(dk);
-  return plan_of(T, B * H * (a > b ? a : b), 3, 8 * B * H * dk * dv);
+  const int64_t groups = B * H * (a > b ? a : b), bytes = 8 * B * H * dk * dv;
+  return one_launch(dk, dv) ? plan_of(T, groups, {3}, bytes) : plan_of(T, groups, {2, 1}, bytes);
 }
 size_t sums_bytes(const Plan& plan, int64_t states, int dk, int dv) {
   return sizeof(float) * static_cast<size_t>(states) * plan.nseg * plan.sub * dk * dv;
@@ -304,8 +319,7 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
     return bf16 ? launch_linattn_bf16(first, n, false, stream)
            : f32 ? launch_linattn_bwd_f32(first, n, stream) : launch_linattn_bwd_any(first, n, stream);
   };
-  const auto width = [](int d) { return d <= 64 ? 0 : d <= 128 ? 1 : 2; };
-  if (width(a.dk) == width(a.dv) && p[0].waves == p[2].waves) return passes(p, 3);
+  if (one_launch(a.dk, a.dv)) return passes(p, 3);
   if (hipError_t e = passes(p, 2)) return e;
   return passes(p + 2, 1);
 }
