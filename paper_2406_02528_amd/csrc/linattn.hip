@@ -122,7 +122,7 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int
   constexpr int64_t C = 32;
   const int64_t chunks = (T + C - 1) / C;
   // In tenths of a us: 32 tokens take about 4 where a compute unit has one
-  // workgroup, two of them 6; a start 10; with segments, their sums about half
+  // workgroup, two of them 6; a start 10; with segments, their sums about a third
   // of a pass each, and their states are written and read twice, at 4.5 TB/s.  The
   // backward's sums are counted in any case: ds0 takes them.  (Forwards of fp32, us,
   // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
@@ -145,6 +145,8 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int
   Plan plan;
   plan.nseg = static_cast<uint32_t>((chunks + per - 1) / per);
   plan.seg_tokens = per * C;
+  // finer sums where compute units stand free (that 1 x 2048 in 8 segments 82 -> 77
+  // us; in 16, which leave none, 60 -> 64)
   plan.sub = 1;
   while (per % (2 * plan.sub) == 0 && 2 * groups * plan.nseg * plan.sub <= kSlots / 2) plan.sub *= 2;
   return plan;
