@@ -36,17 +36,18 @@ __device__ __forceinline__ float value(const T* p) {
 // The teacher's entries of a row: token (-1: none, or one that a lower entry
 // has), z there, p (of all entries of that token).
 constexpr int kScan = 16;   // tokens that a comparison with all of them reads at once
+constexpr int entries_room(int K) { return (K + kScan - 1) / kScan * kScan; }
+constexpr size_t kEntryBytes = sizeof(double) + sizeof(float) + sizeof(int);
 struct Entries {
-  alignas(16) int idx[kDistillMaxK];   // up to the next multiple of kScan none
-  float z[kDistillMaxK];
-  double p[kDistillMaxK];
+  double* p;
+  float* z;
+  int* idx;   // those behind the last: none
 };
 
 // f(k, whether entry k has token i) for the K entries in order; reads of 16 bytes
 // that do not wait for one another (one at a time they took 8 us for 64 entries).
 template <typename F>
 __device__ __forceinline__ void scan(const Entries& en, int K, int i, F&& f) {
-  static_assert(kDistillMaxK % kScan == 0, "whole groups");
   for (int k = 0; k < K; k += kScan) {
     int4 x[kScan / 4];
 #pragma unroll
@@ -86,11 +87,12 @@ __device__ __forceinline__ double sum_of(const double* s) {
 template <typename T, typename D, int THREADS, int HELD, bool NT>
 __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a) {
   constexpr int W = THREADS / kWave, E = 8;
-  __shared__ Entries en;
+  extern __shared__ double s_entries[];   // kEntryBytes for each of K, rounded up
   __shared__ Slots<W> sl;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t m = blockIdx.x;
-  const int V = static_cast<int>(a.V), K = static_cast<int>(a.K);
+  const int V = static_cast<int>(a.V), K = static_cast<int>(a.K), room = entries_room(K);
+  const Entries en{s_entries, reinterpret_cast<float*>(s_entries + room), reinterpret_cast<int*>(s_entries + room) + room};
   const T* const z = static_cast<const T*>(a.z) + m * V;
   D* const dz = a.dz != nullptr ? static_cast<D*>(a.dz) + m * V : nullptr;
   // values before the first whole vector, whole vectors, values after them
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
   const float c = static_cast<float>(kLog2e / a.tau);
   float tm = -__builtin_inff();
   bool any = false;
-  for (int j = K + tid; j < (K + kScan - 1) / kScan * kScan; j += THREADS) en.idx[j] = -1;
+  for (int j = K + tid; j < room; j += THREADS) en.idx[j] = -1;
   for (int j = tid; j < K; j += THREADS) {
     int i = a.idx[m * K + j];
     const float t = a.t_is_f32 ? static_cast<const float*>(a.t)[m * K + j]
@@ -302,18 +304,20 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
 template <typename T, typename D, bool NT>
 hipError_t launch(const DistillArgs& a, hipStream_t stream) {
   const auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(a.M)), dim3(threads), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(a.M)), dim3(threads), entries_room(static_cast<int>(a.K)) * kEntryBytes, stream, a);
     return hipGetLastError();
   };
-  // The fewest threads that hold a row in registers: rows end at the same time in
-  // them all, so it is the rows beside each other on a compute unit that hide each
-  // other's waits (8192 bf16 rows of 2000: 1, 2, 4 vectors per thread 32, 36, 43
-  // us; of 8000: 256 threads 52, 512 95; of 32000: 512 threads 200, 1024 273).
+  // The fewest threads that hold a row in registers: a row's steps wait for one
+  // another, and the rows beside it on a compute unit hide that (8192 bf16 rows, 16
+  // entries: of 1000 in 64 threads 18 us, in 256 30; of 2000 22, 31; of 4000 in 128
+  // 34, in 256 39; of 8000 in 128 or 256 57; of 16000 in 256 95, in 512 105; of 32000
+  // in 512 200, in 1024 273.  64 rows: equal to a tenth).
   const int64_t nv = a.V / 8;  // the most whole vectors of a row
-  if (nv <= 256) return go(distill_kernel<T, D, 256, 1, NT>, 256);
-  if (nv <= 2 * 256) return go(distill_kernel<T, D, 256, 2, NT>, 256);
-  if (nv <= 4 * 256) return go(distill_kernel<T, D, 256, 4, NT>, 256);
-  if (nv <= 4 * 512) return go(distill_kernel<T, D, 512, 4, NT>, 512);
+  if (nv <= 2 * 64) return go(distill_kernel<T, D, 64, 2, NT>, 64);
+  if (nv <= 4 * 64) return go(distill_kernel<T, D, 64, 4, NT>, 64);
+  if (nv <= 4 * 128) return go(distill_kernel<T, D, 128, 4, NT>, 128);
+  if (nv <= 8 * 128) return go(distill_kernel<T, D, 128, 8, NT>, 128);
+  if (nv <= 8 * 256) return go(distill_kernel<T, D, 256, 8, NT>, 256);
   if (NT || nv <= 8 * 512) return go(distill_kernel<T, D, 512, 8, NT>, 512);
   if constexpr (!NT) {
     // one such row fills a compute unit's registers; of bf16, reading it again costs
