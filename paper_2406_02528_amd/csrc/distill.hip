@@ -33,8 +33,7 @@ __device__ __forceinline__ float value(const T* p) {
   else return bf16_to_f32(*p);
 }
 
-// The teacher's entries of a row: token (-1: none, or one that a lower entry
-// has), z there, p (of all entries of that token).
+// The teacher's entries of a row in LDS: token (-1: none), z there, t and then p.
 constexpr int kScan = 16;   // tokens that a comparison with all of them reads at once
 constexpr int entries_room(int K) { return (K + kScan - 1) / kScan * kScan; }
 constexpr size_t kEntryBytes = sizeof(double) + sizeof(float) + sizeof(int);
@@ -87,7 +86,7 @@ __device__ __forceinline__ double sum_of(const double* s) {
 template <typename T, typename D, int THREADS, int HELD, bool NT>
 __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a) {
   constexpr int W = THREADS / kWave, E = 8;
-  extern __shared__ double s_entries[];   // kEntryBytes for each of K, rounded up
+  extern __shared__ __attribute__((aligned(16))) double s_entries[];   // kEntryBytes for each of K, rounded up
   __shared__ Slots<W> sl;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t m = blockIdx.x;
