@@ -10,6 +10,7 @@ namespace mmf {
 hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_bf16(const LinattnPass* p, int n, bool last, hipStream_t stream);
 hipError_t launch_linattn_bwd_f32(const LinattnPass* p, int n, hipStream_t stream);
+hipError_t launch_linattn_bwd_f32_last(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_bwd_any(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_states_f32(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_states_bf16(const LinattnPass* p, int n, hipStream_t stream);
@@ -19,6 +20,7 @@ namespace {
 
 constexpr int64_t kSlots = 512;   // workgroups that run at once: two on a compute unit
 constexpr int kJoinBlock = 256;
+constexpr int64_t kFewTokens = 128;   // launch_linattn_bwd
 
 __device__ __forceinline__ double power(double x, int64_t n) {
   double y = 1.0;
@@ -116,15 +118,15 @@ bool one_launch(int dk, int dv) {
   const auto width = [](int d) { return d <= 64 ? 0 : d <= 128 ? 1 : 2; };
   return width(dk) == width(dv) && waves_of(dk) == waves_of(dv);
 }
-// launches: their passes, 1 (the forward), 3 or 2 and 1; state_bytes: of all the
-// states that enter one segment.
-Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int64_t state_bytes) {
+// launches: their passes, 1 (the forward), 3 or 2 and 1; sums: wanted of a single
+// segment too; state_bytes: of all the states that enter one segment.
+Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, bool sums, int64_t state_bytes) {
   constexpr int64_t C = 32;
   const int64_t chunks = (T + C - 1) / C;
   // In tenths of a us: 32 tokens take about 4 where a compute unit has one
   // workgroup, two of them 6; a start 10; with segments, their sums about a third
-  // of a pass each, and their states are written and read twice, at 4.5 TB/s.  The
-  // backward's sums are counted in any case: ds0 takes them.  (Forwards of fp32, us,
+  // of a pass each, 7 at least, and their states are joined at 4.5 TB/s after 5.
+  // (Forwards of fp32, us,
   // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
   // 16: 56, 71, 60; 4 x 2048, 8: 133, 149, 156; backward of that, 4: 232, 238, 241;
   // 16384 bf16, 32: 132, 16: 150.  Backward in two launches, 4 x 1857, 12 heads of 96
@@ -136,7 +138,7 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int
       const int64_t each = (groups * passes * s + kSlots / 2 - 1) / (kSlots / 2);
       work += each / 2 * (60 * per + 100) + each % 2 * (39 * per + 100);
     }
-    return s == 1 && *launches.begin() == 1 ? work : work + work / 3 + state_bytes * s * 4 / 450000 + 100;
+    return s == 1 && !sums ? work : work + (work > 210 ? work / 3 : 70) + state_bytes * s * 2 / 450000 + 50;
   };
   int64_t best = 1;
   for (int64_t s = 2; s <= chunks && groups * (s - 1) < 2 * kSlots; ++s)
@@ -151,11 +153,11 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, int
   while (per % (2 * plan.sub) == 0 && 2 * groups * plan.nseg * plan.sub <= kSlots / 2) plan.sub *= 2;
   return plan;
 }
-Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), {1}, 4 * B * H * dk * dv); }
-Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv) {
+Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), {1}, false, 4 * B * H * dk * dv); }
+Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv, bool sums) {
   const uint32_t a = tiles_of(dv), b = tiles_of(dk);
   const int64_t groups = B * H * (a > b ? a : b), bytes = 8 * B * H * dk * dv;
-  return one_launch(dk, dv) ? plan_of(T, groups, {3}, bytes) : plan_of(T, groups, {2, 1}, bytes);
+  return one_launch(dk, dv) ? plan_of(T, groups, {3}, sums, bytes) : plan_of(T, groups, {2, 1}, sums, bytes);
 }
 size_t sums_bytes(const Plan& plan, int64_t states, int dk, int dv) {
   return sizeof(float) * static_cast<size_t>(states) * plan.nseg * plan.sub * dk * dv;
@@ -258,16 +260,23 @@ hipError_t launch_linattn_chunk(const LinattnArgs& a, float* scratch, hipStream_
 }
 
 size_t linattn_bwd_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
-  return 2 * sums_bytes(plan_bwd(B, T, H, dk, dv), B * H, dk, dv);
+  const size_t a = sums_bytes(plan_bwd(B, T, H, dk, dv, false), B * H, dk, dv);
+  const size_t b = sums_bytes(plan_bwd(B, T, H, dk, dv, true), B * H, dk, dv);
+  return 2 * (a > b ? a : b);
 }
 
 hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream_t stream) {
-  const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv);
+  const bool bf16 = !a.is_f32 && !a.do_is_f32, f32 = a.is_f32 && a.do_is_f32;
+  // Of one segment dv's state behind its last token is ds0, if it is as exact as
+  // the sums, from which ds0 comes else: of bf16 (64 x 64 tokens, 8 heads of 64: 18
+  // us, by the sums 32), and of few fp32 tokens, whose passes then take three parts
+  // (that 30, 36; 8 x 128, 16 heads of 128: 38, 47).
+  const bool exact = bf16 || (f32 && a.T <= kFewTokens);
+  const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv, a.ds0 != nullptr && !exact);
   const int64_t size = a.is_f32 ? 4 : 2, ld = a.H * (2 * a.dk + a.dv);
   const char* const x = static_cast<const char*>(a.qkv);
   const LinattnOperand q{x, ld, a.is_f32}, k{x + a.H * a.dk * size, ld, a.is_f32},
       v{x + 2 * a.H * a.dk * size, ld, a.is_f32}, d{a.dout, a.H * a.dv, a.do_is_f32};
-  const bool bf16 = !a.is_f32 && !a.do_is_f32, f32 = a.is_f32 && a.do_is_f32;
   LinattnPass base{};
   base.decay = a.decay;
   base.B = static_cast<uint32_t>(a.B);
@@ -299,7 +308,9 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
   float* const us = scratch;
   float* const ug = scratch + sums_bytes(plan, a.B * a.H, a.dk, a.dv) / sizeof(float);
   const bool some = plan.nseg > 1;
-  if (some || a.ds0 != nullptr) {
+  const bool by_dv = exact && !some && a.ds0 != nullptr;
+  if (by_dv) p[2].s_out = a.ds0;
+  if (some || (a.ds0 != nullptr && !by_dv)) {
     LinattnPass u[2];
     Join j[2];
     int n = 0;
@@ -318,10 +329,12 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
     p[2] = from_joined(p[2], plan, ug, false);
   }
   const auto passes = [&](const LinattnPass* first, int n) {
-    return bf16 ? launch_linattn_bf16(first, n, false, stream)
-           : f32 ? launch_linattn_bwd_f32(first, n, stream) : launch_linattn_bwd_any(first, n, stream);
+    return bf16 ? launch_linattn_bf16(first, n, by_dv, stream)
+           : f32 ? (by_dv ? launch_linattn_bwd_f32_last : launch_linattn_bwd_f32)(first, n, stream)
+                 : launch_linattn_bwd_any(first, n, stream);
   };
-  if (one_launch(a.dk, a.dv)) return passes(p, 3);
+  // dv by itself where it writes over what dk reads
+  if (one_launch(a.dk, a.dv) && !(by_dv && a.ds0 == a.ds_last)) return passes(p, 3);
   if (hipError_t e = passes(p, 2)) return e;
   return passes(p + 2, 1);
 }

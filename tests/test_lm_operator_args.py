@@ -182,10 +182,12 @@ def test_few_tokens_go_one_by_one_and_more_as_chunks():
     bare = lambda r: [k.split("::")[-1] for k in kernels(r)]  # noqa: E731
     dims = lambda T: (2, T, 4, 64, 64)  # noqa: E731
     rs = record([fwd_call(1, dims(8)), fwd_call(1, dims(9)), fwd_call(0, dims(2)), fwd_call(0, dims(3)),
-                 fwd_call(1, dims(5000)), bwd_call(0, 0, dims(1)), bwd_call(1, 0, dims(5000))])
+                 fwd_call(1, dims(5000)), bwd_call(0, 0, dims(1), 2 * P), bwd_call(1, 1, dims(128), 2 * P),
+                 bwd_call(0, 0, dims(1), P), bwd_call(1, 0, dims(1)), bwd_call(1, 0, dims(1), None), bwd_call(1, 0, dims(5000))])
     assert all(r["status"] == OK and r["allocs"] == r["frees"] == 0 for r in rs)
-    assert [bare(r) for r in rs] == [[step], [chunk], [step], [chunk], [chunk, join, chunk], [chunk, join, chunk],
-                                    [chunk, join, chunk]]
+    sums = [chunk, join, chunk]   # [chunk, chunk]: ds0 in the place of ds_last
+    assert [bare(r) for r in rs] == [[step], [chunk], [step], [chunk], sums, [chunk], [chunk], [chunk, chunk], sums, [chunk],
+                                    sums]
 
 
 @pytest.mark.parametrize("dims", [(2 ** 20, 1, 1, 16, 16), (2 ** 20, 70, 1, 64, 128), (2 ** 17, 70, 1, 256, 256),
