@@ -236,10 +236,12 @@ __device__ __forceinline__ bool not_finite(uint32_t top) {
 
 // MODE: parts of fp32 values in the products of o.  NKT: parts of the decayed
 // values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns
-// each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no o; the values go to
-// LDS decayed).
+// each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no
+// o; the values go to LDS decayed).  Registers: two workgroups on a compute unit
+// for the passes, three of 8 waves for the sums.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int CT, int C, bool STATE>
-__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : 4) void linattn_chunk_kernel(const LinattnPasses args) {
+__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : 4) void linattn_chunk_kernel(
+    const LinattnPasses args) {
   constexpr int kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
   constexpr int kB = DK / 32;        // contraction steps over Dk
   constexpr int kT = C / 16;         // tiles of tokens
