@@ -160,7 +160,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
         for (int e = 0; e < E; ++e) zm = fmaxf(zm, in[i].get(e));
       }
   } else {
-    // the sum as well, against the thread's own running maximum
+    // The sum as well, against the thread's own running maximum.  While that is -inf
+    // (masked tokens alone), against 0: the sum stays 0, or the NaN of one there.
     for (int v = tid; v < nv; v += THREADS) {
       RowVec<T, E> x;
       x.load(rz, v);
@@ -171,9 +172,10 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
         ze *= __builtin_amdgcn_exp2f((zm - vm) * c);
         zm = vm;
       }
+      const float from = zm == -__builtin_inff() ? 0.0f : zm;
       float s = 0.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((x.get(e) - zm) * c);
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((x.get(e) - from) * c);
       ze += s;
     }
   }
@@ -205,9 +207,9 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs a
     zx = __builtin_amdgcn_exp2f((zx - zm) * c);
     if (own >= 0) ze += zx;
   } else {
-    // a thread without a value above -inf has no sum
-    ze = own_max == -__builtin_inff() ? (zm == own_max ? __builtin_nan("") : 0.0)
-                                      : ze * __builtin_amdgcn_exp2f((own_max - zm) * c);
+    // of a thread without a value above -inf 0 or NaN, which the factor 0 keeps; of a
+    // row without one NaN
+    ze = zm == -__builtin_inff() ? __builtin_nan("") : ze * __builtin_amdgcn_exp2f((own_max - zm) * c);
     zx = __builtin_amdgcn_exp2f((zx - zm) * c);
     if (own >= 0) ze += zx;
   }
