@@ -63,6 +63,7 @@ struct LinattnPasses {
   LinattnPass p[3];
   uint32_t n, count;
 };
+// Of at least one token (as the launches).
 size_t linattn_chunk_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv);
 hipError_t launch_linattn_chunk(const LinattnArgs& a, float* joined, hipStream_t stream);
 // Backward: dqkv bf16; s0, ds_last, ds0 may be nullptr, ds0 may be ds_last.

@@ -1260,7 +1260,7 @@ int mmf_glu_bwd(const void* dp, int dp_is_f32, const void* x, int x_is_f32, cons
 }
 
 size_t mmf_linattn_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
-  if (check_linattn(B, T, H, dk, dv) != MMF_OK) return 0;
+  if (check_linattn(B, T, H, dk, dv) != MMF_OK || B == 0 || T == 0) return 0;
   return linattn_fwd_bytes(B, T, H, dk, dv);
 }
 
@@ -1282,7 +1282,7 @@ int mmf_linattn_fwd(const void* qkv, int qkv_is_f32, const float* decay, float s
 }
 
 size_t mmf_linattn_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
-  if (check_linattn(B, T, H, dk, dv) != MMF_OK) return 0;
+  if (check_linattn(B, T, H, dk, dv) != MMF_OK || B == 0 || T == 0) return 0;
   return round_up(mmf::linattn_bwd_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
 }
 
