@@ -602,9 +602,8 @@ int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float s
  *
  * Both directions form their products on the matrix cores where there are more
  * than a few tokens: bf16 inputs as they are, everything in fp32 (fp32 inputs,
- * decayed products, states) as sums of bf16 parts, to 2^-16 of each factor
- * where the result is rounded to bf16 and 2^-24 where it is float32.  Inputs
- * should be finite (and fp32 ones at most 3.38e38, the largest bf16).  One that
+ * decayed products, states) as sums of three bf16 parts, to 2^-24 of each
+ * factor, whatever type the result is rounded to.  Inputs should be finite (and fp32 ones at most 3.38e38, the largest bf16).  One that
  * is not reaches, in its sequence and head and as NaN where the formula has an
  * infinity, what depends on it and nothing else: of k and v, o from its token on
  * and the last state, and dq likewise; of q and dout, dk and dv up to its token

@@ -8,9 +8,8 @@
 namespace mmf {
 
 hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream);
-hipError_t launch_linattn_bf16(const LinattnPass* p, int n, bool last, hipStream_t stream);
+hipError_t launch_linattn_bf16(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_bwd_f32(const LinattnPass* p, int n, hipStream_t stream);
-hipError_t launch_linattn_bwd_f32_last(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_bwd_any(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_states_f32(const LinattnPass* p, int n, hipStream_t stream);
 hipError_t launch_linattn_states_bf16(const LinattnPass* p, int n, hipStream_t stream);
@@ -20,7 +19,6 @@ namespace {
 
 constexpr int64_t kSlots = 512;   // workgroups that run at once: two on a compute unit
 constexpr int kJoinBlock = 256;
-constexpr int64_t kFewTokens = 128;   // launch_linattn_bwd
 
 __device__ __forceinline__ double power(double x, int64_t n) {
   double y = 1.0;
@@ -245,18 +243,15 @@ hipError_t launch_linattn_chunk(const LinattnArgs& a, float* scratch, hipStream_
     p.e_e = 1;
     p.e_decay = true;
     p.s_out = a.s_last;
-    return a.is_f32 ? launch_linattn_f32(&p, 1, stream) : launch_linattn_bf16(&p, 1, a.s_last != nullptr, stream);
+    return (a.is_f32 ? launch_linattn_f32 : launch_linattn_bf16)(&p, 1, stream);
   }
-  // of bf16 the last state comes from the sums, which are more exact than what
-  // a bf16 o needs of the state within a segment
-  const bool joined_last = !a.is_f32 && a.s_last != nullptr;
-  const LinattnPass u = sums_of(p, plan, scratch, joined_last);
+  const LinattnPass u = sums_of(p, plan, scratch, false);
   if (hipError_t e = (a.is_f32 ? launch_linattn_states_f32 : launch_linattn_states_bf16)(&u, 1, stream)) return e;
-  const Join j{scratch, a.s0, joined_last ? a.s_last : nullptr, false};
+  const Join j{scratch, a.s0, nullptr, false};
   if (hipError_t e = join(&j, 1, p, plan, stream)) return e;
   p = from_joined(p, plan, scratch, false);
-  p.s_out = joined_last ? nullptr : a.s_last;
-  return a.is_f32 ? launch_linattn_f32(&p, 1, stream) : launch_linattn_bf16(&p, 1, false, stream);
+  p.s_out = a.s_last;
+  return (a.is_f32 ? launch_linattn_f32 : launch_linattn_bf16)(&p, 1, stream);
 }
 
 size_t linattn_bwd_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
@@ -267,12 +262,11 @@ size_t linattn_bwd_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
 
 hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream_t stream) {
   const bool bf16 = !a.is_f32 && !a.do_is_f32, f32 = a.is_f32 && a.do_is_f32;
-  // Of one segment dv's state behind its last token is ds0, if it is as exact as
-  // the sums, from which ds0 comes else: of bf16 (64 x 64 tokens, 8 heads of 64: 18
-  // us, by the sums 32), and of few fp32 tokens, whose passes then take three parts
-  // (that 30, 36; 8 x 128, 16 heads of 128: 38, 47).
-  const bool exact = bf16 || (f32 && a.T <= kFewTokens);
-  const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv, a.ds0 != nullptr && !exact);
+  // Of one segment and one type dv's state behind its last token is ds0, which
+  // comes from the sums else (64 x 64 tokens, 8 heads of 64, bf16: 18 us, by the
+  // sums 32; fp32 30, 36).
+  const bool alike = bf16 || f32;
+  const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv, a.ds0 != nullptr && !alike);
   const int64_t size = a.is_f32 ? 4 : 2, ld = a.H * (2 * a.dk + a.dv);
   const char* const x = static_cast<const char*>(a.qkv);
   const LinattnOperand q{x, ld, a.is_f32}, k{x + a.H * a.dk * size, ld, a.is_f32},
@@ -308,7 +302,7 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
   float* const us = scratch;
   float* const ug = scratch + sums_bytes(plan, a.B * a.H, a.dk, a.dv) / sizeof(float);
   const bool some = plan.nseg > 1;
-  const bool by_dv = exact && !some && a.ds0 != nullptr;
+  const bool by_dv = alike && !some && a.ds0 != nullptr;
   if (by_dv) p[2].s_out = a.ds0;
   if (some || (a.ds0 != nullptr && !by_dv)) {
     LinattnPass u[2];
@@ -329,9 +323,7 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
     p[2] = from_joined(p[2], plan, ug, false);
   }
   const auto passes = [&](const LinattnPass* first, int n) {
-    return bf16 ? launch_linattn_bf16(first, n, by_dv, stream)
-           : f32 ? (by_dv ? launch_linattn_bwd_f32_last : launch_linattn_bwd_f32)(first, n, stream)
-                 : launch_linattn_bwd_any(first, n, stream);
+    return (bf16 ? launch_linattn_bf16 : f32 ? launch_linattn_bwd_f32 : launch_linattn_bwd_any)(first, n, stream);
   };
   // dv by itself where it writes over what dk reads
   if (one_launch(a.dk, a.dv) && !(by_dv && a.ds0 == a.ds_last)) return passes(p, 3);

@@ -5,10 +5,10 @@
 namespace mmf {
 hipError_t launch_linattn_bwd_any(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_passes<kEither, kEither, kEither, false, 2, 2, false>(p, n, stream);
+  return launch_passes<kEither, kEither, kEither, false, false>(p, n, stream);
 }
 hipError_t launch_linattn_states_any(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_passes<kEither, kEither, kEither, true, 3, 3, true>(p, n, stream);
+  return launch_passes<kEither, kEither, kEither, true, true>(p, n, stream);
 }
 }  // namespace mmf

@@ -4,6 +4,6 @@
 namespace mmf {
 hipError_t launch_linattn_bwd_f32(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_passes<kF32, kF32, kF32, false, 2, 2, false>(p, n, stream);
+  return launch_passes<kF32, kF32, kF32, false, false>(p, n, stream);
 }
 }  // namespace mmf

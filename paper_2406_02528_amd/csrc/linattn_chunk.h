@@ -47,11 +47,12 @@
 // whose parts take six products for one.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
-// decayed products, the state, the weighted keys) go to the matrix cores as
-// sums of 2 or 3 bf16 parts (2^-16 or 2^-24 relative), with the products of
-// parts down to the same size: 3 parts where the result is fp32 (o from fp32
-// inputs, states), 2 where it is rounded to bf16.  Sums are fp32; powers of l
-// come from fp64.
+// decayed products, the state, the decayed values) go to the matrix cores as
+// sums of three bf16 parts (2^-24 relative), with the products of parts down to
+// the same size: six for one.  Also where the result is rounded to bf16, since
+// what is left of terms that cancel would else be that of 17 bits (two parts and
+// three products: 16384 bf16 129 us where this takes 140, the backward of 4 x 2048
+// fp32 230 and 295).  Sums are fp32; powers of l come from fp64.
 #pragma once
 #include "linattn.h"
 #include "mmf_device.h"
@@ -103,14 +104,16 @@ __device__ __forceinline__ void sum8(const v4i (&p)[N], float* x) {
   }
 }
 
-// acc += a b over the parts' products of relative size above 2^(-8 L).
-template <int L, int NA, int NB>
+constexpr int kParts = 3;   // of an fp32 value
+
+// acc += a b over the parts' products of relative size above 2^-24.
+template <int NA, int NB>
 __device__ __forceinline__ v4f mma(const v4i (&a)[NA], const v4i (&b)[NB], v4f acc) {
 #pragma unroll
   for (int i = NA - 1; i >= 0; --i)
 #pragma unroll
     for (int j = NB - 1; j >= 0; --j)
-      if (i + j < L) acc = mfma(a[i], b[j], acc);
+      if (i + j < kParts) acc = mfma(a[i], b[j], acc);
   return acc;
 }
 
@@ -234,12 +237,10 @@ __device__ __forceinline__ bool not_finite(uint32_t top) {
   return K == kBf16 ? (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u : top >= 0x7F7F8000u;
 }
 
-// MODE: parts of fp32 values in the products of o.  NKT: parts of the decayed
-// values in the state's.  DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns
-// each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no
+// DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no
 // o; the values go to LDS decayed).  Registers: two workgroups on a compute unit
 // for the passes, three of 8 waves for the sums.
-template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, int DK, int WAVES, int CT, int C, bool STATE>
+template <Kind KQ, Kind KK, Kind KV, bool OF32, int DK, int WAVES, int CT, int C, bool STATE>
 __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : 4) void linattn_chunk_kernel(
     const LinattnPasses args) {
   constexpr int kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
@@ -247,8 +248,8 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
   static_assert(STATE || (kT == 2 && WAVES >= 4), "the products' tiles are a wave's each");
-  constexpr int NQ = KQ == kBf16 ? 1 : MODE, NK = KK == kBf16 ? 1 : MODE;
-  constexpr int NV = STATE ? NKT : KV == kBf16 ? 1 : MODE;
+  constexpr int NQ = KQ == kBf16 ? 1 : kParts, NK = KK == kBf16 ? 1 : kParts;
+  constexpr int NV = KV == kBf16 && !STATE ? 1 : kParts;
   // A chunk's rows are asked for before the products of the chunk before; of fp32
   // the queries behind them, which leaves the products their registers.
   constexpr bool kEarly = STATE || KQ == kBf16;
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   __shared__ __attribute__((aligned(16))) char q_t[STATE ? 1 : NQ][STATE ? 16 : C * DK * 2];
   __shared__ __attribute__((aligned(16))) char k_t[NK][C * DK * 2];
   __shared__ __attribute__((aligned(16))) char v_t[NV][C * WC * 2];
-  __shared__ __attribute__((aligned(16))) char p_t[STATE ? 1 : MODE][STATE ? 16 : C * C * 2];
+  __shared__ __attribute__((aligned(16))) char p_t[STATE ? 1 : kParts][STATE ? 16 : C * C * 2];
   __shared__ float pr[2 * C + 2];    // l^(C - i); 1 behind i = C
   __shared__ int s_bad[2];
 
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 #pragma unroll
           for (int k = 0; k < NK; ++k) kf[k] = tile_read(k_t[k], (k_row_ ^ (x << 6)) + ps * 16 * (2 * DK));
           query(pt, x, f);
-          acc = mma<MODE>(kf, f, acc);
+          acc = mma(kf, f, acc);
         }
         // decay from key 16 ps + 4 g + r to query 16 pt + n; none from later keys
         const float* const w = &pr[C - 16 * (pt - ps) - n + 4 * g];
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
         }
         const int at = tile_at<C>(n, 2 * ps + (g >> 1)) + pt * 16 * (2 * C) + 8 * (g & 1);
 #pragma unroll
-        for (int k = 0; k < MODE; ++k) {
+        for (int k = 0; k < kParts; ++k) {
           const uint2 v = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
           *reinterpret_cast<uint2*>(&p_t[k][at]) = v;
           y[0] -= bf16_lo(v.x);
@@ -526,7 +527,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
       if (ps == 1 && pt == kT) {  // the half of an operand that no tile fills
         const int at = tile_at<C>(n, 2 + (g >> 1)) + 8 * (g & 1);
 #pragma unroll
-        for (int k = 0; k < MODE; ++k) *reinterpret_cast<uint2*>(&p_t[k][at]) = make_uint2(0u, 0u);
+        for (int k = 0; k < kParts; ++k) *reinterpret_cast<uint2*>(&p_t[k][at]) = make_uint2(0u, 0u);
       }
       // --- state x queries
 #pragma unroll
@@ -536,20 +537,20 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
       if (ewave) {
 #pragma unroll
         for (int x = 0; x < kB; ++x) {
-          v4i sf[CT][MODE];
+          v4i sf[CT][kParts];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
             float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = st[ct][x][j / 4][j % 4];
-            split8<MODE>(y, sf[ct]);
+            split8<kParts>(y, sf[ct]);
           }
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             v4i f[NQ];
             query(t, x, f);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma<MODE>(sf[ct], f, o[ct][t]);
+            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma(sf[ct], f, o[ct][t]);
           }
         }
 #pragma unroll
@@ -570,7 +571,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 #pragma unroll
       for (int c = 0; c < kS; ++c) {
         // decayed, with the decays to the next chunk's first token or to the last one
-        v4i wf[CT][NKT];
+        v4i wf[CT][kParts];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
@@ -578,14 +579,14 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
             vf[ct][c][k] = tile_turn8(v_t[k], (v_a0 ^ (ct << 5)) + c * 32 * (2 * WC), (v_a1 ^ (ct << 5)) + c * 32 * (2 * WC));
           if constexpr (STATE) {
 #pragma unroll
-            for (int k = 0; k < NKT; ++k) wf[ct][k] = vf[ct][c][k];
+            for (int k = 0; k < kParts; ++k) wf[ct][k] = vf[ct][c][k];
           } else {
             const float* const w = &pr[32 * c + 8 * g + C - tc + (last ? 1 : 0)];
             float y[8];
             sum8<NV>(vf[ct][c], y);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] *= into * w[j];
-            split8<NKT>(y, wf[ct]);
+            split8<kParts>(y, wf[ct]);
           }
         }
 #pragma unroll
@@ -597,7 +598,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
             for (int k = 0; k < NK; ++k)
               f[k] = tile_turn8(k_t[k], (k_a0_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK), (k_a1_ ^ (x << 6)) + 8 * i + c * 32 * (2 * DK));
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) st[ct][x][i] = mma<NKT>(f, wf[ct], st[ct][x][i]);
+            for (int ct = 0; ct < CT; ++ct) st[ct][x][i] = mma(f, wf[ct], st[ct][x][i]);
           }
       }
     }
@@ -612,11 +613,11 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 #pragma unroll
           for (int c = 0; c < kS; ++c) {
             if (2 * c > t) continue;
-            v4i f[MODE];
+            v4i f[kParts];
 #pragma unroll
-            for (int k = 0; k < MODE; ++k) f[k] = tile_read(p_t[k], (p_row ^ (c << 6)) + t * 16 * (2 * C));
+            for (int k = 0; k < kParts; ++k) f[k] = tile_read(p_t[k], (p_row ^ (c << 6)) + t * 16 * (2 * C));
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma<MODE>(vf[ct][c], f, o[ct][t]);
+            for (int ct = 0; ct < CT; ++ct) o[ct][t] = mma(vf[ct][c], f, o[ct][t]);
           }
       }
       // --- store: columns w0 + 4 g + r of token 16 t + n.  By every wave, those
@@ -666,7 +667,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
 constexpr int chunk_tokens(int DK, Kind K, bool state) { return state && DK == 64 && K == kBf16 ? 64 : 32; }
 
 // `n` passes of the same number of workgroups, widths in 64s, and waves.
-template <Kind KQ, Kind KK, Kind KV, bool OF32, int MODE, int NKT, bool STATE>
+template <Kind KQ, Kind KK, Kind KV, bool OF32, bool STATE>
 hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
   LinattnPasses ps{};
   for (int i = 0; i < n; ++i) ps.p[i] = p[i];
@@ -677,7 +678,7 @@ hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
     return hipGetLastError();
   };
 #define MMF_FORM(DK, WAVES, CT) \
-  go(linattn_chunk_kernel<KQ, KK, KV, OF32, MODE, NKT, DK, WAVES, CT, chunk_tokens(DK, KQ, STATE), STATE>, WAVES)
+  go(linattn_chunk_kernel<KQ, KK, KV, OF32, DK, WAVES, CT, chunk_tokens(DK, KQ, STATE), STATE>, WAVES)
   if (p->Dk > 128) return p->waves == 4 ? MMF_FORM(256, 4, 1) : MMF_FORM(256, 8, 1);
   // 128 columns: parts of fp32 as 32 per wave, so that what a wave reads from LDS
   // serves twice as many (4 x 2048 fp32, backward: 184 -> 163 us; 2048, forward: 36

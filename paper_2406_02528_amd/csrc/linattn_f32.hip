@@ -4,10 +4,10 @@
 namespace mmf {
 hipError_t launch_linattn_f32(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_passes<kF32, kF32, kF32, true, 3, 3, false>(p, n, stream);
+  return launch_passes<kF32, kF32, kF32, true, false>(p, n, stream);
 }
 hipError_t launch_linattn_states_f32(const LinattnPass* p, int n, hipStream_t stream) {
   using namespace la;
-  return launch_passes<kF32, kF32, kF32, true, 3, 3, true>(p, n, stream);
+  return launch_passes<kF32, kF32, kF32, true, true>(p, n, stream);
 }
 }  // namespace mmf
