@@ -574,10 +574,11 @@ int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *co
  * row b*T + t: q of all heads [H][dk], then k [H][dk], then v [H][dv] (one
  * BitLinear of the stacked latent weights, as f | c | g for the MLGRU).
  * qkv: bf16 bits or float32 (qkv_is_f32); o [B*T][H][dv] in the same type; decay
- * [H] float32 (constants of the model, any numbers; 0 keeps the token itself
- * only); s0 [B][H][dk][dv] float32 or NULL (0); s_last [B][H][dk][dv] float32,
- * the state after the last token (NULL: not stored; may be the same array as
- * s0: the state is then updated in place).  No other overlap is allowed.
+ * [H] float32 (constants of the model; 0 keeps the token itself only; any numbers
+ * whose powers up to the T-th are in fp32's range: -1 to 1, or little beyond);
+ * s0 [B][H][dk][dv] float32 or NULL (0); s_last [B][H][dk][dv] float32, the state
+ * after the last token (NULL: not stored; may be the same array as s0: the state
+ * is then updated in place).  No other overlap is allowed.
  * dk and dv: multiples of 16 up to 256; B*H at most 2^20, B*H dk dv at most 2^33,
  * H (2 dk + dv) at most 2^21, B*T below 2^31 (MMF_ERR_SHAPE).
  * B == 0 or T == 0 is a no-op, which leaves s_last as it was.  Workspace
@@ -603,11 +604,14 @@ int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float s
  * Both directions form their products on the matrix cores where there are more
  * than a few tokens: bf16 inputs as they are, everything in fp32 (fp32 inputs,
  * decayed products, states) as sums of three bf16 parts, to 2^-24 of each
- * factor, whatever type the result is rounded to.  Inputs should be finite (and fp32 ones at most 3.38e38, the largest bf16).  One that
- * is not reaches, in its sequence and head and as NaN where the formula has an
- * infinity, what depends on it and nothing else: of k and v, o from its token on
- * and the last state, and dq likewise; of q and dout, dk and dv up to its token
- * and ds0; and its own token's outputs. */
+ * factor, whatever type the result is rounded to.  The products q_i . k_s (of dq
+ * dout_i . v_s, of dk v_i . dout_s, of dv k_i . q_s) of tokens up to 31 apart are
+ * formed, and have to be in fp32's range as the states have.  Inputs should be
+ * finite (and fp32 ones at most 3.38e38, the largest bf16).  One that is not
+ * reaches, in its sequence and head and as NaN where the formula has an infinity,
+ * what depends on it and nothing else: of k and v, o from its token on and the
+ * last state, and dq likewise; of q and dout, dk and dv up to its token and ds0;
+ * and its own token's outputs. */
 size_t mmf_linattn_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
 int mmf_linattn_bwd(const void *qkv, int qkv_is_f32, const float *decay, float scale,
                     const float *s0, const void *dout, int do_is_f32, const float *ds_last,

@@ -51,8 +51,8 @@
 // sums of three bf16 parts (2^-24 relative), with the products of parts down to
 // the same size: six for one.  Also where the result is rounded to bf16, since
 // what is left of terms that cancel would else be that of 17 bits (two parts and
-// three products: 16384 bf16 129 us where this takes 140, the backward of 4 x 2048
-// fp32 230 and 295).  Sums are fp32; powers of l come from fp64.
+// three products: 16384 bf16 129 us where this takes 136, the backward of 4 x 2048
+// fp32 230 and 283).  Sums are fp32; powers of l come from fp64.
 #pragma once
 #include "linattn.h"
 #include "mmf_device.h"
@@ -390,15 +390,6 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   const int v_a1 = tile_at<WC>(t_row + 4, 2 * CT * wave + ((n & 3) >> 1)) + 8 * (n & 1);
   const int ps = wave % kT, pt = ps + wave / kT;   // the wave's tile of keys x queries, if there is one
 
-  // The state's decay is kept beside it, as `held`: what the registers hold times
-  // held is the state.  Where the factor leaves the range that fp32 has to spare
-  // the registers take it over.
-  float held = 1.0f;
-  const auto next_held = [&](int tc, int last) {   // behind a chunk; 1: the registers take it over
-    const float x = held * pr[C - tc + last], a = __builtin_fabsf(x);
-    return a > 0x1p-20f && a < 0x1p20f ? x : 1.0f;
-  };
-  const auto take_over = [&](float by) { each([&](int ct, int x, int i) { st[ct][x][i] *= by; }); };
   // --- a chunk's rows from registers to LDS; whether its values are finite
   const auto stage = [&](int64_t i0, int tc, int flag) {
     const int last = i0 + tc == T && !rev ? 1 : 0;  // the state behind the last token itself
@@ -417,7 +408,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
         unit_values<KV>(wv[u], rv.f32(), x);
         v4i f[NV];
         if constexpr (STATE) {
-          const float w = alpha * __builtin_amdgcn_rcpf(next_held(tc, last)) * pr[vr + u * kVApart + C - tc + last];
+          const float w = alpha * pr[vr + u * kVApart + C - tc + last];
 #pragma unroll
           for (int j = 0; j < 8; ++j) x[j] *= w;
         } else {
@@ -555,16 +546,17 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
         }
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
-          const float w = beta * held * pr[C - 16 * t - n];
+          const float w = beta * pr[C - 16 * t - n];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) o[ct][t] *= w;
         }
       }
     }
-    const float decayed = held * pr[C - tc + (last ? 1 : 0)];
-    held = next_held(tc, last ? 1 : 0);
-    if (__builtin_amdgcn_readfirstlane(held == 1.0f && decayed != 1.0f)) take_over(decayed);
-    const float into = alpha * __builtin_amdgcn_rcpf(held);
+    // The state's decay over the chunk, taken by the registers: kept beside them as a
+    // factor, values would enter divided by it, and large ones overflow (and 16384 bf16
+    // took 140 us with it, 136 without).
+    const float decayed = pr[C - tc + (last ? 1 : 0)];
+    each([&](int ct, int x, int i) { st[ct][x][i] *= decayed; });
 
     // --- keys x values into the state
     if (ewave) {
@@ -585,7 +577,7 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
             float y[8];
             sum8<NV>(vf[ct][c], y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] *= into * w[j];
+            for (int j = 0; j < 8; ++j) y[j] *= alpha * w[j];
             split8<kParts>(y, wf[ct]);
           }
         }
@@ -645,7 +637,6 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   }
 
   // the segment's own sum, or the state after the last token
-  take_over(held);
   float* out = nullptr;
   if (STATE) out = p.s_out + (static_cast<int64_t>(bh) * p.nseg + seg) * p.Dk * p.Dv;
   else if (p.s_out != nullptr && seg + 1 == p.nseg) out = p.s_out + static_cast<int64_t>(bh) * p.Dk * p.Dv;
