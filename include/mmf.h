@@ -654,7 +654,8 @@ int mmf_beam_select(const void *logits, int logits_is_f32, const float *scores,
  * bytes of a row (multiples of 16 below 2^31, B times one at most 2^33,
  * MMF_ERR_SHAPE).
  * outs[i] may be states[i]: rows that stay where they are are then neither read
- * nor written.  No other overlap.  parents [B][W] int32 on the device (n = W
+ * nor written.  No other overlap, nor any between the arrays of different entries
+ * of which one is written (two arrays are not exchanged this way).  parents [B][W] int32 on the device (n = W
  * above); a row whose entry is not in 0 .. W-1 stays itself.  W: 1 to 64.
  * Allocates nothing. */
 int mmf_beam_reorder(const void *const *states, void *const *outs, const int64_t *row_bytes,

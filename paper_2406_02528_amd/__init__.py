@@ -961,8 +961,8 @@ def _state_ptrs(tensors, name, rows, here):
 def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, stream=None) -> None:
     """outs[i] row (b, j) = states[i] row (b, parents[b][j]) for a list of tensors
     [B*W][...] of any type (rows of a multiple of 16 bytes); outs None: in place.
-    parents i32 [B][W].  outs[i] has the type and shape of states[i]; no two of
-    them may overlap."""
+    parents i32 [B][W].  outs[i] has the type and shape of states[i] and may be
+    states[i]; no two of outs may overlap, nor one of them another's state."""
     here = _here()
     states = _listed(states, "states")
     _need_here(parents, "parents", torch.int32, (B, W), here)
@@ -977,6 +977,11 @@ def mmf_beam_reorder(states, parents: torch.Tensor, B: int, W: int, outs=None, s
         full = [p for p, r in zip(dst, rows) if r]
         if len(set(full)) != len(full):
             raise ValueError("a tensor to write is in the list twice")
+    if outs is not None and not set(dst).isdisjoint(src):  # some in place, or one that another is read from
+        full = [(p, q) for p, q, r in zip(src, dst, rows) if r]
+        written = {q for _, q in full}
+        if any(p in written for p, q in full if p != q):
+            raise ValueError("a tensor to write is one that another reads")
     _check(_lib.mmf_beam_reorder(_at(src), _at(dst), _at(rows), len(src), _ptr(parents), B, W,
                                  _stream_here(stream, here)))
 
