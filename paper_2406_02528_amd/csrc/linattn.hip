@@ -31,9 +31,8 @@ __device__ __forceinline__ double power(double x, int64_t n) {
 
 // The states that enter the segments: E_0 is s_in (with its decay to the first
 // token where the pass is forward), E_{s+1} = l^tokens E_s + u_s.  E_s takes the
-// place of u_s for the multiples s of `sub`; s_out (nullptr: not wanted) is the
-// state behind the last token (forward: of the token itself, backward: with
-// its decay).
+// place of u_s; s_out (nullptr: not wanted; backward alone) is the state behind
+// the last token, with its decay.
 struct Join {
   float* u;         // [states][n][size]
   const float* s_in;
@@ -43,7 +42,7 @@ struct Join {
 struct Joins {
   Join j[2];
   const float* decay;
-  uint32_t states, H, n, sub;
+  uint32_t states, H, n;
   int64_t size, tokens, T;
 };
 
@@ -64,12 +63,11 @@ __global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const Joins a)
   }
   float* const u = j.u + bh * a.n * a.size + at;
   // a sum that nothing follows is not there unless s_out is wanted
-  const uint32_t have = j.s_out != nullptr ? a.n : a.n - a.sub;
+  const uint32_t have = j.s_out != nullptr ? a.n : a.n - 1;
   const float full = static_cast<float>(power(l, a.tokens));
   constexpr uint32_t kAhead = 32 / N;   // loads in flight
   const float* from = u;
   float* to = u;
-  uint32_t skip = 0;   // sums until the next state that is wanted
   for (uint32_t s = 0; s < a.n; s += kAhead) {
     vec v[kAhead];
 #pragma unroll
@@ -80,18 +78,11 @@ __global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const Joins a)
 #pragma unroll
     for (uint32_t i = 0; i < kAhead; ++i) {
       if (s + i >= a.n) break;
-      if (skip == 0) {
-        *reinterpret_cast<vec*>(to) = e;
-        skip = a.sub;
-      }
+      *reinterpret_cast<vec*>(to) = e;
       to += a.size;
-      --skip;
       if (s + i >= have) continue;
       float w = full;
-      if (s + i + a.sub >= a.n) {   // the last segment: fewer tokens, or none
-        const int64_t left = a.T - (s + i) * a.tokens;
-        if (left <= a.tokens) w = left <= 0 ? 1.0f : static_cast<float>(power(l, j.rev ? left : left - 1));
-      }
+      if (s + i + 1 == a.n) w = static_cast<float>(power(l, a.T - (s + i) * a.tokens));   // may have fewer tokens
 #pragma unroll
       for (int c = 0; c < N; ++c) e[c] = fmaf(w, e[c], v[i][c]);
     }
@@ -99,10 +90,9 @@ __global__ __launch_bounds__(kJoinBlock) void linattn_join_kernel(const Joins a)
   if (j.s_out != nullptr) *reinterpret_cast<vec*>(j.s_out + bh * a.size + at) = e;
 }
 
-// How both directions are cut: segments, and the finer ones whose sums are
-// joined (their kernel runs two workgroups on a compute unit).
+// How both directions are cut.
 struct Plan {
-  uint32_t nseg, sub;
+  uint32_t nseg;
   int64_t seg_tokens;
 };
 int waves_of(int Dv) { return Dv <= 64 ? 4 : 8; }
@@ -145,10 +135,6 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, boo
   Plan plan;
   plan.nseg = static_cast<uint32_t>((chunks + per - 1) / per);
   plan.seg_tokens = per * C;
-  // finer sums where compute units stand free (that 1 x 2048 in 8 segments 82 -> 77
-  // us; in 16, which leave none, 60 -> 64)
-  plan.sub = 1;
-  while (per % (2 * plan.sub) == 0 && 2 * groups * plan.nseg * plan.sub <= kSlots / 2) plan.sub *= 2;
   return plan;
 }
 Plan plan_fwd(int64_t B, int64_t T, int64_t H, int dk, int dv) { return plan_of(T, B * H * tiles_of(dv), {1}, false, 4 * B * H * dk * dv); }
@@ -158,7 +144,7 @@ Plan plan_bwd(int64_t B, int64_t T, int64_t H, int dk, int dv, bool sums) {
   return one_launch(dk, dv) ? plan_of(T, groups, {3}, sums, bytes) : plan_of(T, groups, {2, 1}, sums, bytes);
 }
 size_t sums_bytes(const Plan& plan, int64_t states, int dk, int dv) {
-  return sizeof(float) * static_cast<size_t>(states) * plan.nseg * plan.sub * dk * dv;
+  return sizeof(float) * static_cast<size_t>(states) * plan.nseg * dk * dv;
 }
 
 LinattnPass cut(LinattnPass p, const Plan& plan) {
@@ -168,37 +154,34 @@ LinattnPass cut(LinattnPass p, const Plan& plan) {
   p.seg_tokens = plan.seg_tokens;
   return p;
 }
-// The same over the finer segments for the sums alone.
-LinattnPass sums_of(LinattnPass p, const Plan& plan, float* u, bool all) {
-  p.nseg = plan.nseg * plan.sub;
-  p.seg_tokens = plan.seg_tokens / plan.sub;
-  p.segs = all ? p.nseg : p.nseg - plan.sub;
+// The same for the sums alone; all: that of the last segment too.
+LinattnPass sums_of(LinattnPass p, float* u, bool all) {
+  p.segs = all ? p.nseg : p.nseg - 1;
   p.s_out = u;
   return p;
 }
 // The pass from the joined states u of sums [dk][dv]; `turned`: its state is
 // their transpose.
-LinattnPass from_joined(LinattnPass p, const Plan& plan, const float* u, bool turned) {
+LinattnPass from_joined(LinattnPass p, const float* u, bool turned) {
   const int64_t size = static_cast<int64_t>(p.Dk) * p.Dv;
   p.e_in = u;
-  p.e_bh = size * plan.nseg * plan.sub;
-  p.e_seg = size * plan.sub;
+  p.e_bh = size * p.nseg;
+  p.e_seg = size;
   p.e_d = turned ? 1 : p.Dv;
   p.e_e = turned ? p.Dk : 1;
   p.e_decay = false;
   return p;
 }
 
-hipError_t join(const Join* j, int n, const LinattnPass& p, const Plan& plan, hipStream_t stream) {
+hipError_t join(const Join* j, int n, const LinattnPass& p, hipStream_t stream) {
   Joins a{};
   for (int i = 0; i < n; ++i) a.j[i] = j[i];
   a.decay = p.decay;
   a.states = p.B * p.H;
   a.H = p.H;
-  a.n = plan.nseg * plan.sub;
-  a.sub = plan.sub;
+  a.n = p.nseg;
   a.size = static_cast<int64_t>(p.Dk) * p.Dv;
-  a.tokens = plan.seg_tokens / plan.sub;
+  a.tokens = p.seg_tokens;
   a.T = p.T;
   // a lane's entries side by side where the lanes are still many (the forward of 4 x
   // 2048 bf16, 16 heads of 128: 84 -> 76 us, of 16384 137 -> 130; few lanes: equal)
@@ -245,11 +228,11 @@ hipError_t launch_linattn_chunk(const LinattnArgs& a, float* scratch, hipStream_
     p.s_out = a.s_last;
     return (a.is_f32 ? launch_linattn_f32 : launch_linattn_bf16)(&p, 1, stream);
   }
-  const LinattnPass u = sums_of(p, plan, scratch, false);
+  const LinattnPass u = sums_of(p, scratch, false);
   if (hipError_t e = (a.is_f32 ? launch_linattn_states_f32 : launch_linattn_states_bf16)(&u, 1, stream)) return e;
   const Join j{scratch, a.s0, nullptr, false};
-  if (hipError_t e = join(&j, 1, p, plan, stream)) return e;
-  p = from_joined(p, plan, scratch, false);
+  if (hipError_t e = join(&j, 1, p, stream)) return e;
+  p = from_joined(p, scratch, false);
   p.s_out = a.s_last;
   return (a.is_f32 ? launch_linattn_f32 : launch_linattn_bf16)(&p, 1, stream);
 }
@@ -309,18 +292,18 @@ hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream
     Join j[2];
     int n = 0;
     if (some) {
-      u[n] = sums_of(p[3], plan, us, false);
+      u[n] = sums_of(p[3], us, false);
       j[n++] = {us, a.s0, nullptr, false};
     }
-    u[n] = sums_of(p[4], plan, ug, a.ds0 != nullptr);
+    u[n] = sums_of(p[4], ug, a.ds0 != nullptr);
     j[n++] = {ug, a.ds_last, a.ds0, true};
     const auto states = bf16 ? launch_linattn_states_bf16 : f32 ? launch_linattn_states_f32 : launch_linattn_states_any;
     if (hipError_t e = states(u, n, stream)) return e;
-    if (hipError_t e = join(j, n, p[4], plan, stream)) return e;
-    if (some) p[0] = from_joined(p[0], plan, us, true);
+    if (hipError_t e = join(j, n, p[4], stream)) return e;
+    if (some) p[0] = from_joined(p[0], us, true);
     // from here on ds_last may be overwritten by ds0
-    p[1] = from_joined(p[1], plan, ug, true);
-    p[2] = from_joined(p[2], plan, ug, false);
+    p[1] = from_joined(p[1], ug, true);
+    p[2] = from_joined(p[2], ug, false);
   }
   const auto passes = [&](const LinattnPass* first, int n) {
     return (bf16 ? launch_linattn_bf16 : f32 ? launch_linattn_bwd_f32 : launch_linattn_bwd_any)(first, n, stream);

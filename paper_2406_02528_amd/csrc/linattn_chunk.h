@@ -324,11 +324,8 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
       rq.load(kr, k_on ? 8 * kq : rq.width, kKApart, wq);
     }
   };
-  const bool some = begin < end;   // a segment of a pass for states may have no tokens
-  if (some) {
-    load(begin, tokens_at(begin));
-    load_queries(begin, tokens_at(begin));
-  }
+  load(begin, tokens_at(begin));
+  load_queries(begin, tokens_at(begin));
 
   // powers of l: fp64, by squaring (any l, 0 among them)
   for (int i = threadIdx.x; i < 2 * C + 2; i += kThreads) {
@@ -450,12 +447,12 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 :
   // them.  Whether a chunk's values are finite is told in two flags in turn:
   // one is cleared while the other is read.
   int64_t i0 = begin;
-  int tc = some ? tokens_at(i0) : 0, flag = 0;
-  if (some) stage(i0, tc, flag);
+  int tc = tokens_at(i0), flag = 0;
+  stage(i0, tc, flag);
   // The state is there before the loop: a wait for it inside would be one for the
   // next chunk's loads, in every chunk.
   if constexpr (!STATE) each([&](int ct, int x, int i) { asm volatile("" : "+v"(st[ct][x][i])); });
-  while (some) {
+  while (true) {
     const int64_t next = i0 + tc;
     if (next < end) {
       load(next, tokens_at(next));
