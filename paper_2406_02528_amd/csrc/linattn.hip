@@ -183,9 +183,11 @@ hipError_t join(const Join* j, int n, const LinattnPass& p, hipStream_t stream) 
   a.size = static_cast<int64_t>(p.Dk) * p.Dv;
   a.tokens = p.seg_tokens;
   a.T = p.T;
-  // a lane's entries side by side where the lanes are still many (the forward of 4 x
-  // 2048 bf16, 16 heads of 128: 84 -> 76 us, of 16384 137 -> 130; few lanes: equal)
-  const bool wide = a.size * a.states * n >= int64_t(1) << 20;
+  // Four entries side by side per lane where the lanes are still many (whole calls of
+  // bf16, heads of 128, one entry and four: forward of 2^16 entries, 1 x 4096 with 4
+  // heads, 32.4 us, 33.7; of 2^18, 16384 with 16 heads, 145.4, 146.0; of 2^19, 2 x 2048,
+  // 58.7, 57.8; of 2^20, 4 x 2048, 91.2, 87.3; backward of that 191, 180)
+  const bool wide = a.size * a.states * n >= int64_t(1) << 19;
   const int64_t lanes = a.size / (wide ? 4 : 1);
   const dim3 grid(a.states * static_cast<uint32_t>((lanes + kJoinBlock - 1) / kJoinBlock), static_cast<uint32_t>(n));
   if (wide) hipLaunchKernelGGL(linattn_join_kernel<4>, grid, dim3(kJoinBlock), 0, stream, a);
