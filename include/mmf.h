@@ -583,7 +583,10 @@ int mmf_grad_clip(const void *const *grads, const int *is_f32, const int64_t *co
  * H (2 dk + dv) at most 2^21, B*T below 2^31 (MMF_ERR_SHAPE).
  * B == 0 or T == 0 is a no-op, which leaves s_last as it was.  Workspace
  * (256-byte aligned, MMF_ERR_WORKSPACE; mmf_linattn_workspace_bytes, which may
- * be 0) or NULL: then allocated stream-ordered on `stream` and freed there.
+ * be 0) or NULL: then allocated stream-ordered on `stream` and freed there.  The
+ * size goes by the whole shape and does not grow with T alone (many short segments
+ * need more than few long ones): a buffer for several shapes is as large as the
+ * largest of their sizes, not as that of the longest.
  */
 size_t mmf_linattn_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
 int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float scale,
