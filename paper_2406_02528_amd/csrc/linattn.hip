@@ -17,7 +17,11 @@ hipError_t launch_linattn_states_any(const LinattnPass* p, int n, hipStream_t st
 
 namespace {
 
-constexpr int64_t kSlots = 512;   // workgroups that run at once: two on a compute unit
+// Workgroups that run at once: two on a compute unit, as for most forms of up to 128
+// key entries.  (Of more key entries one stands there, and the plan counts too few
+// rounds: 1 x 4000, 8 heads of 208 x 144 fp32 takes 120 us in 32 segments, 106 in 16;
+// bf16 81, 72.)
+constexpr int64_t kSlots = 512;
 constexpr int kJoinBlock = 256;
 
 __device__ __forceinline__ double power(double x, int64_t n) {
@@ -114,11 +118,11 @@ Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, boo
   // In tenths of a us: 32 tokens take about 4 where a compute unit has one
   // workgroup, two of them 6; a start 10; with segments, their sums about a third
   // of a pass each, 7 at least, and their states are joined at 4.5 TB/s after 5.
-  // (Forwards of fp32, us,
-  // at the segments taken and at half and twice as many: 1 x 2048, 16 heads of 128,
-  // 16: 56, 71, 60; 4 x 2048, 8: 133, 149, 156; backward of that, 4: 232, 238, 241;
-  // 16384 bf16, 32: 132, 16: 150.  Backward in two launches, 4 x 1857, 12 heads of 96
-  // x 48, 5: 133; 3, as for one: 190.)
+  // (us at the segments taken and at half and twice as many, fp32, heads of 128: forward
+  // of 1 x 2048, 16 heads, 16: 56, 76, 61; of 4 x 2048, 8: 128, 138, 152; backward of
+  // that, 4: 277, 331, 297; of 1 x 8000, 4 heads, 42: 92, 102, 101; forward of 16384 bf16,
+  // 16 heads, 32: 132, 146, 160.  Backward in two launches, 4 x 1857, 12 heads of 96 x
+  // 48, 5: 157; 3, as for one: 230.)
   const auto cost = [&](int64_t s) {
     const int64_t per = (chunks + s - 1) / s;
     int64_t work = 0;

@@ -238,10 +238,14 @@ __device__ __forceinline__ bool not_finite(uint32_t top) {
 }
 
 // DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no
-// o; the values go to LDS decayed).  Registers: two workgroups on a compute unit
-// for the passes, three of 8 waves for the sums.
+// o; the values go to LDS decayed).  Waves per SIMD: what leaves each form its
+// registers, so that none spills (bf16, 4 x 2048, 16 heads of 96 x 64, backward: 129.9
+// us where the 4-wave passes had four and the sums six, with 8 bytes of scratch each,
+// 132.0).  For passes a compute unit so holds two workgroups of 8 waves; of 4 waves
+// four of bf16 (three from 80 key entries on) and two of fp32; of more than 128 key
+// entries one of 8 waves, and of fp32, by its LDS, one of any.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int DK, int WAVES, int CT, int C, bool STATE>
-__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : 4) void linattn_chunk_kernel(
+__global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 && WAVES == 8 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : DK == 128 && WAVES == 4 ? 3 : 4) void linattn_chunk_kernel(
     const LinattnPasses args) {
   constexpr int kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
   constexpr int kB = DK / 32;        // contraction steps over Dk
