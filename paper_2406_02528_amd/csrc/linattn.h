@@ -12,6 +12,7 @@ namespace mmf {
 // [H][dv]; o [B*T][H][dv] in the type of qkv; s0, s_last [B][H][dk][dv]
 // (nullptr: 0, not stored; may be the same array).
 constexpr int kLinattnMaxDim = 256;
+constexpr int kLinattnChunk = 32;   // tokens of a chunk
 struct LinattnArgs {
   const void* qkv;
   bool is_f32;

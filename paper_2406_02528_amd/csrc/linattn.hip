@@ -113,7 +113,7 @@ bool one_launch(int dk, int dv) {
 // launches: their passes, 1 (the forward), 3 or 2 and 1; sums: wanted of a single
 // segment too; state_bytes: of all the states that enter one segment.
 Plan plan_of(int64_t T, int64_t groups, std::initializer_list<int> launches, bool sums, int64_t state_bytes) {
-  constexpr int64_t C = 32;
+  constexpr int64_t C = kLinattnChunk;
   const int64_t chunks = (T + C - 1) / C;
   // In tenths of a us: 32 tokens take about 4 where a compute unit has one
   // workgroup, two of them 6; a start 10; with segments, their sums about a third

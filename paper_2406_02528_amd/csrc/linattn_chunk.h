@@ -41,10 +41,11 @@
 // fp32).  Two buffers for bf16 chunks in LDS, and one barrier instead of two,
 // gained nothing.
 //
-// Over many tokens a pass is bound by HBM: that forward moves 302 MB in 71 us, 4.3
-// TB/s, after 168 MB in 42 us for the segments' sums, 4.0 TB/s.  Over few it is
-// bound by a chunk's chain of loads, LDS and products: 2.5 us of bf16, 5 of fp32,
-// whose parts take six products for one.
+// What bounds it is a chunk's chain of loads, splitting, LDS, products and two barriers:
+// 2.7 us of bf16, 5.3 of fp32, whose parts take six products for one, where a compute
+// unit has one workgroup.  Over many tokens two of them hide a part of each other:
+// that forward moves 303 MB in 95 us, 3.2 TB/s, the vector unit two thirds and the
+// matrix cores one third busy, after 163 MB in 43 us for the segments' sums.
 //
 // Numerics: bf16 inputs are exact operands.  fp32 values (fp32 inputs, the
 // decayed products, the state, the decayed values) go to the matrix cores as
@@ -237,17 +238,17 @@ __device__ __forceinline__ bool not_finite(uint32_t top) {
   return K == kBf16 ? (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u : top >= 0x7F7F8000u;
 }
 
-// DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns each.  C: tokens of a chunk.  STATE: the segment's own sum only (no queries, no
-// o; the values go to LDS decayed).  Waves per SIMD: what leaves each form its
-// registers, so that none spills (bf16, 4 x 2048, 16 heads of 96 x 64, backward: 129.9
-// us where the 4-wave passes had four and the sums six, with 8 bytes of scratch each,
-// 132.0).  For passes a compute unit so holds two workgroups of 8 waves; of 4 waves
+// DK: Dk padded to 64, 128, 256.  WAVES: of CT x 16 columns each.  STATE: the segment's
+// own sum only (no queries, no o; the values go to LDS decayed).  Waves per SIMD: what
+// leaves each form its registers, so that none spills (bf16, 4 x 2048, 16 heads of 96 x
+// 64, backward: 129.9 us; 132.0 where the 4-wave passes had four and the sums six, with
+// 8 bytes of scratch each).  For passes a compute unit so holds two workgroups of 8 waves; of 4 waves
 // four of bf16 (three from 80 key entries on) and two of fp32; of more than 128 key
 // entries one of 8 waves, and of fp32, by its LDS, one of any.
-template <Kind KQ, Kind KK, Kind KV, bool OF32, int DK, int WAVES, int CT, int C, bool STATE>
+template <Kind KQ, Kind KK, Kind KV, bool OF32, int DK, int WAVES, int CT, bool STATE>
 __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 && WAVES == 8 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : DK == 128 && WAVES == 4 ? 3 : 4) void linattn_chunk_kernel(
     const LinattnPasses args) {
-  constexpr int kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
+  constexpr int C = kLinattnChunk, kThreads = 64 * WAVES, WC = 16 * CT * WAVES;
   constexpr int kB = DK / 32;        // contraction steps over Dk
   constexpr int kT = C / 16;         // tiles of tokens
   constexpr int kS = C / 32;         // contraction steps over tokens
@@ -653,11 +654,6 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 && WA
   }
 }
 
-// Tokens of a chunk: 64 where the sums of narrow bf16 states alone are wanted (16
-// x 1024, 8 heads of 64: 17.5 us, with 32 19.7), else 32 (the three passes of that
-// 44.5 us, with 64 62: too many registers).
-constexpr int chunk_tokens(int DK, Kind K, bool state) { return state && DK == 64 && K == kBf16 ? 64 : 32; }
-
 // `n` passes of the same number of workgroups, widths in 64s, and waves.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, bool STATE>
 hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
@@ -670,11 +666,12 @@ hipError_t launch_passes(const LinattnPass* p, int n, hipStream_t stream) {
     return hipGetLastError();
   };
 #define MMF_FORM(DK, WAVES, CT) \
-  go(linattn_chunk_kernel<KQ, KK, KV, OF32, DK, WAVES, CT, chunk_tokens(DK, KQ, STATE), STATE>, WAVES)
+  go(linattn_chunk_kernel<KQ, KK, KV, OF32, DK, WAVES, CT, STATE>, WAVES)
   if (p->Dk > 128) return p->waves == 4 ? MMF_FORM(256, 4, 1) : MMF_FORM(256, 8, 1);
   // 128 columns: parts of fp32 as 32 per wave, so that what a wave reads from LDS
-  // serves twice as many (4 x 2048 fp32, backward: 184 -> 163 us; 2048, forward: 36
-  // -> 33); bf16, with fewer of them, as 16 per wave (16384: 71 us, 32 per wave 72)
+  // serves twice as many (whole calls: 4 x 2048 fp32, backward, 325 -> 292 us; forward
+  // 154 -> 131); bf16, with fewer of them, as 16 per wave (4 x 2048, backward, 175 us,
+  // 32 per wave 182; 16384 146, 149)
   if constexpr (STATE || KQ == kBf16) {
     if (p->Dk > 64) return p->waves == 4 ? MMF_FORM(128, 4, 1) : MMF_FORM(128, 8, 1);
     return p->waves == 4 ? MMF_FORM(64, 4, 1) : MMF_FORM(64, 8, 1);
