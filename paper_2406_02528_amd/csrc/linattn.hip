@@ -252,8 +252,8 @@ size_t linattn_bwd_bytes(int64_t B, int64_t T, int64_t H, int dk, int dv) {
 hipError_t launch_linattn_bwd(const LinattnBwdArgs& a, float* scratch, hipStream_t stream) {
   const bool bf16 = !a.is_f32 && !a.do_is_f32, f32 = a.is_f32 && a.do_is_f32;
   // Of one segment and one type dv's state behind its last token is ds0, which
-  // comes from the sums else (64 x 64 tokens, 8 heads of 64, bf16: 18 us, by the
-  // sums 32; fp32 30, 36).
+  // comes from the sums else (64 x 64 tokens, 8 heads of 64, bf16: 22 us, by the
+  // sums 35; fp32 37, 52; 7 x 600, 12 heads of 128, 66, 95; fp32 105, 133).
   const bool alike = bf16 || f32;
   const Plan plan = plan_bwd(a.B, a.T, a.H, a.dk, a.dv, a.ds0 != nullptr && !alike);
   const int64_t size = a.is_f32 ? 4 : 2, ld = a.H * (2 * a.dk + a.dv);

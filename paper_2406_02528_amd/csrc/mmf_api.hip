@@ -331,10 +331,11 @@ int check_linattn(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
 }
 
 // Up to this many tokens go through the state one by one; more make a chunk.
-// 1 x 16 heads of 128, fp32: 8 tokens 8.8 us one by one, 11.9 as a chunk; 16
-// tokens 13.7 and 12.2; 64 sequences 40 and 47, 62 and 48.  bf16, whose products
-// have a third of the parts: 2 tokens 9.9 and 9.7 (64 sequences 30 and 26; 16 x
-// 2 heads of 256: 9.0 and 12.0), 4 tokens 9.0 and 9.0 (41 and 28; 12.6 and 11.2).
+// 16 heads of 128, fp32: 8 tokens 8.2 us one by one, 11.3 as a chunk, 12 tokens 10.8
+// and 11.3; 64 sequences 45 and 47, 56 and 48; 16 x 2 heads of 256 13.5 and 15.3, 17.6
+// and 15.2.  bf16, whose products have half of the parts: 2 tokens 5.3 and 7.6, 4 tokens
+// 7.8 and 7.6; 64 sequences 36 and 36, 51 and 35; 16 x 2 heads of 256 9.0 and 12.3, 15.6
+// and 12.4.
 int64_t linattn_steps(bool f32) { return f32 ? 8 : 2; }
 size_t linattn_fwd_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
   return round_up(mmf::linattn_chunk_bytes(B, T, H, static_cast<int>(dk), static_cast<int>(dv)), kScratchAlign);
