@@ -609,7 +609,8 @@ int mmf_linattn_fwd(const void *qkv, int qkv_is_f32, const float *decay, float s
  * decayed products, states) as sums of three bf16 parts, to 2^-24 of each
  * factor, whatever type the result is rounded to.  The products q_i . k_s (of dq
  * dout_i . v_s, of dk v_i . dout_s, of dv k_i . q_s) of tokens up to 31 apart are
- * formed, and have to be in fp32's range as the states have.  Inputs should be
+ * formed before their decays and the scale, and those of q_i (dout_i, v_i, k_i) with
+ * a state up to 32 tokens away; they have to be in fp32's range.  Inputs should be
  * finite (and fp32 ones at most 3.38e38, the largest bf16).  One that is not
  * reaches, in its sequence and head and as NaN where the formula has an infinity,
  * what depends on it and nothing else: of k and v, o from its token on and the

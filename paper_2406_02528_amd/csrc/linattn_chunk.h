@@ -52,8 +52,8 @@
 // sums of three bf16 parts (2^-24 relative), with the products of parts down to
 // the same size: six for one.  Also where the result is rounded to bf16, since
 // what is left of terms that cancel would else be that of 17 bits (two parts and
-// three products: 16384 bf16 129 us where this takes 136, the backward of 4 x 2048
-// fp32 230 and 283).  Sums are fp32; powers of l come from fp64.
+// three products: 16384 bf16 130 us where this takes 142, the backward of 4 x 2048
+// fp32 219 and 283, of bf16 150 and 172).  Sums are fp32; powers of l come from fp64.
 #pragma once
 #include "linattn.h"
 #include "mmf_device.h"
@@ -242,9 +242,9 @@ __device__ __forceinline__ bool not_finite(uint32_t top) {
 // own sum only (no queries, no o; the values go to LDS decayed).  Waves per SIMD: what
 // leaves each form its registers, so that none spills (bf16, 4 x 2048, 16 heads of 96 x
 // 64, backward: 129.9 us; 132.0 where the 4-wave passes had four and the sums six, with
-// 8 bytes of scratch each).  For passes a compute unit so holds two workgroups of 8 waves; of 4 waves
-// four of bf16 (three from 80 key entries on) and two of fp32; of more than 128 key
-// entries one of 8 waves, and of fp32, by its LDS, one of any.
+// 8 bytes of scratch each).  For passes a compute unit so holds two workgroups of 8
+// waves; of 4 waves four of bf16 (three from 80 key entries on) and two of fp32; of more
+// than 128 key entries one of 8 waves, and of fp32, by its LDS, one of any.
 template <Kind KQ, Kind KK, Kind KV, bool OF32, int DK, int WAVES, int CT, bool STATE>
 __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 && WAVES == 8 ? 6 : 5) : DK == 256 || CT == 2 ? 2 : DK == 128 && WAVES == 4 ? 3 : 4) void linattn_chunk_kernel(
     const LinattnPasses args) {
@@ -555,8 +555,8 @@ __global__ __launch_bounds__(64 * WAVES, STATE && DK <= 128 ? (KK == kBf16 && WA
       }
     }
     // The state's decay over the chunk, taken by the registers: kept beside them as a
-    // factor, values would enter divided by it, and large ones overflow (and 16384 bf16
-    // took 140 us with it, 136 without).
+    // factor, values would enter divided by it, and large ones overflow (no less time
+    // either: 16384 bf16 145 us both ways, the backward of 4 x 2048 fp32 284 and 287).
     const float decayed = pr[C - tc + (last ? 1 : 0)];
     each([&](int ct, int x, int i) { st[ct][x][i] *= decayed; });
 
