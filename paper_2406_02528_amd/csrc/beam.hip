@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void beam_piece_kernel(const BeamSelectAr
   for (int i = 0; i < VALS; ++i) {
     const int t = begin + i * kThreads + threadIdx.x;
     v[i] = t < end && !done ? __uint_as_float(w[i]) : -__builtin_inff();
-    if (done && t == a.end) v[i] = 0.0f;
+    if (done && t == a.end && t < end) v[i] = 0.0f;   // (threads behind the end stand on the next piece's tokens)
   }
   if (threadIdx.x == 0) s_count = 0;
   float m = -__builtin_inff();
